@@ -15,3 +15,4 @@ from .trimul import (EPS, WEIGHT_NAMES, f64, layer_norm, sigmoid, pair_mask,  # 
 from .opm import (msa_mask, pair_counts, outer_sum, outer_product_mean,  # noqa: F401
                   outer_product_mean_tile)
 from .triattn import key_mask, scores, triangle_attention, chunked_attention  # noqa: F401
+from .crossattn import cross_attention, cross_attention_backward, softmax_weights  # noqa: F401

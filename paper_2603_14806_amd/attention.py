@@ -1,0 +1,207 @@
+"""Attention of queries over keys of another length (include/cross_attn.h):
+the C names, and cross_attention / cross_attention_backward, which check their
+tensors and allocate outputs and workspaces with torch.
+
+Every call runs on the device its tensors are on, on `stream` (a torch stream
+or a raw hipStream_t) or that device's current stream, and allocates there.
+"""
+import contextlib
+import ctypes
+
+import torch
+
+from . import trimul as _t
+from .trimul import TRI_MUL_BF16, TRI_MUL_F32, _check, _i32, _i64, _ptr, _vp
+
+_DTYPES = {torch.float32: TRI_MUL_F32, torch.bfloat16: TRI_MUL_BF16}
+
+
+class CrossAttnTensor(ctypes.Structure):
+    """cross_attn_tensor_t."""
+    _fields_ = [("data", _vp), ("batch", _i64), ("token", _i64), ("head", _i64)]
+
+
+class CrossAttnBias(ctypes.Structure):
+    """cross_attn_bias_t."""
+    _fields_ = [("data", _vp), ("batch", _i64), ("head", _i64), ("row", _i64)]
+
+
+class CrossAttnView(ctypes.Structure):
+    """cross_attn_view_t."""
+    _fields_ = [("batch", _i64), ("nq", _i64), ("nk", _i64), ("heads", _i32), ("kv_heads", _i32), ("d", _i32),
+                ("dtype", _i32), ("scale", ctypes.c_float), ("bias", CrossAttnBias), ("mask", _vp), ("mask_batch", _i64)]
+
+
+_view, _tensor, _size = ctypes.POINTER(CrossAttnView), ctypes.POINTER(CrossAttnTensor), ctypes.POINTER(ctypes.c_size_t)
+
+# name -> (restype, argtypes); the same order and meaning as include/cross_attn.h
+SIGNATURES = {
+    "cross_attn_workspace_size": (ctypes.c_int, [_view, _size]),
+    "cross_attn_forward": (ctypes.c_int, [_view, _tensor, _tensor, _tensor, _tensor, _vp, _vp, ctypes.c_size_t, _vp]),
+    "cross_attn_backward_workspace_size": (ctypes.c_int, [_view, _size]),
+    "cross_attn_backward": (ctypes.c_int, [_view] + [_tensor] * 4 + [_vp] + [_tensor] * 4 +
+                            [ctypes.POINTER(CrossAttnBias), _vp, ctypes.c_size_t, _vp]),
+}
+
+_lib = None
+
+
+def lib():
+    """libtrimul.so with this module's signatures set."""
+    global _lib
+    if _lib is None:
+        L = _t.lib()
+        for name, (res, args) in SIGNATURES.items():
+            f = getattr(L, name)
+            f.restype, f.argtypes = res, args
+        _lib = L
+    return _lib
+
+
+# ---------------------------------------------------------------- C names
+
+def _ref(t):
+    return None if t is None else ctypes.byref(t)
+
+
+def cross_attn_workspace_size(view):
+    n = ctypes.c_size_t()
+    _check(lib().cross_attn_workspace_size(_ref(view), ctypes.byref(n)))
+    return n.value
+
+
+def cross_attn_forward(view, q, k, v, out, stats, ws, ws_bytes, stream=None):
+    _check(lib().cross_attn_forward(_ref(view), _ref(q), _ref(k), _ref(v), _ref(out), _ptr(stats), _ptr(ws), ws_bytes,
+                                    _t._stream(stream)))
+
+
+def cross_attn_backward_workspace_size(view):
+    n = ctypes.c_size_t()
+    _check(lib().cross_attn_backward_workspace_size(_ref(view), ctypes.byref(n)))
+    return n.value
+
+
+def cross_attn_backward(view, q, k, v, out, stats, dout, dq, dk, dv, dbias, ws, ws_bytes, stream=None):
+    _check(lib().cross_attn_backward(_ref(view), _ref(q), _ref(k), _ref(v), _ref(out), _ptr(stats), _ref(dout),
+                                     _ref(dq), _ref(dk), _ref(dv), _ref(dbias), _ptr(ws), ws_bytes,
+                                     _t._stream(stream)))
+
+
+# ---------------------------------------------------------------- torch tensors
+
+def tensor(t):
+    """cross_attn_tensor_t of a [batch][tokens][heads][d] tensor (kept alive by the caller)."""
+    return CrossAttnTensor(_ptr(t), t.stride(0), t.stride(1), t.stride(2))
+
+
+def bias_tensor(t):
+    """cross_attn_bias_t of a [batch or 1][heads or 1][nq][nk] tensor: an axis of length 1 is shared."""
+    return CrossAttnBias(_ptr(t), 0 if t.shape[0] == 1 else t.stride(0), 0 if t.shape[1] == 1 else t.stride(1), t.stride(2))
+
+
+@contextlib.contextmanager
+def on_stream(device, stream):
+    """The device, and on it `stream` (None: the current one) as torch's current stream: what is allocated here
+    belongs to that stream, so that a workspace freed at the end is reused behind the kernels that use it."""
+    with torch.cuda.device(device):
+        if stream is None:
+            yield torch.cuda.current_stream(device).cuda_stream
+            return
+        s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device)
+        if s.device != device:
+            raise ValueError(f"stream of {s.device} for tensors on {device}")
+        with torch.cuda.stream(s):
+            yield s.cuda_stream
+
+
+def _heads_tensor(name, t, dtype, device, shape):
+    if t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be a {dtype} tensor on {device}, not {t.dtype} on {t.device}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    if t.shape[3] > 1 and t.stride(3) != 1:
+        raise ValueError(f"{name} must have unit stride along its last axis")
+
+
+def view(q, k, v, bias=None, mask=None, scale=None):
+    """cross_attn_view_t of the call (the tensors are kept alive by the caller), after checking shapes and types."""
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q, k and v must be [batch][tokens][heads][d]")
+    if q.dtype not in _DTYPES:
+        raise ValueError(f"q must be float32 or bfloat16, not {q.dtype}")
+    if q.device.type != "cuda":
+        raise ValueError("tensors passed to the library must live on the GPU")
+    batch, nq, heads, d = q.shape
+    nk, kv_heads = k.shape[1], k.shape[2]
+    _heads_tensor("q", q, q.dtype, q.device, q.shape)
+    _heads_tensor("k", k, q.dtype, q.device, (batch, nk, kv_heads, d))
+    _heads_tensor("v", v, q.dtype, q.device, (batch, nk, kv_heads, d))
+    w = CrossAttnView(batch, nq, nk, heads, kv_heads, d, _DTYPES[q.dtype], d ** -0.5 if scale is None else scale)
+    if bias is not None:
+        if bias.dtype != q.dtype or bias.device != q.device:
+            raise ValueError(f"bias must be a {q.dtype} tensor on {q.device}")
+        if bias.dim() == 3:
+            bias = bias[None]
+        if bias.dim() != 4 or bias.shape[0] not in (1, batch) or bias.shape[1] not in (1, heads) or tuple(bias.shape[2:]) != (nq, nk):
+            raise ValueError(f"bias must be [{batch} or 1][{heads} or 1][{nq}][{nk}], not {list(bias.shape)}")
+        if bias.numel():
+            if nk > 1 and bias.stride(3) != 1:
+                raise ValueError("bias must have unit stride along its last axis")
+            w.bias = bias_tensor(bias)
+    if mask is not None:
+        if mask.dtype not in (torch.uint8, torch.bool) or mask.device != q.device:
+            raise ValueError(f"mask must be a uint8 or bool tensor on {q.device}")
+        if mask.dim() == 1:
+            mask = mask[None]
+        if mask.dim() != 2 or mask.shape[0] not in (1, batch) or mask.shape[1] != nk or (nk > 1 and mask.stride(1) != 1):
+            raise ValueError(f"mask must be [{batch} or 1][{nk}] with unit stride along the keys")
+        if mask.numel():
+            w.mask = _ptr(mask)
+            w.mask_batch = 0 if mask.shape[0] == 1 else mask.stride(0)
+    return w
+
+
+def cross_attention(q, k, v, bias=None, mask=None, scale=None, return_stats=False, stream=None):
+    """out [batch][nq][heads][d] of q's type from q and k, v [batch][nk][kv_heads][d] (float32 or bfloat16; heads a
+    multiple of kv_heads, d a multiple of 8 up to 128; any strides that are multiples of 16 bytes).
+
+    bias: [batch or 1][heads or 1][nq][nk] (or without the first axis) of q's type whose rows are a multiple of 8
+    values apart (a view of a padded tensor is fine); an axis of length 1 is shared.  mask: [batch or 1][nk] or [nk],
+    uint8 or bool, nonzero where the key is present.  scale: default 1 / sqrt(d).  With return_stats also the
+    [2][batch][heads][nq] float32 statistics that cross_attention_backward takes."""
+    w = view(q, k, v, bias, mask, scale)
+    with on_stream(q.device, stream) as s:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        stats = torch.empty((2, w.batch, w.heads, w.nq), dtype=torch.float32, device=q.device) if return_stats else None
+        n = cross_attn_workspace_size(w)
+        ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+        cross_attn_forward(w, tensor(q), tensor(k), tensor(v), tensor(out), stats, ws, n, s)
+    return (out, stats) if return_stats else out
+
+
+def cross_attention_backward(q, k, v, out, stats, dout, bias=None, mask=None, scale=None, need_kv=True,
+                             need_bias=True, stream=None):
+    """(dq, dk, dv, dbias) for dout, from the forward's arguments, its out and its stats.  dk and dv are None
+    without need_kv, dbias is None without a bias or need_bias; dbias has the bias's shape, its rows padded to a
+    multiple of 8 values as the bias's are (the view returned ends at nk)."""
+    w = view(q, k, v, bias, mask, scale)
+    if need_bias and bias is not None and any(n > 1 and st == 0 for n, st in zip(bias.shape[:-1], bias.stride())):
+        raise ValueError("a bias that is repeated along an axis has that axis of length 1 for its gradient")
+    _heads_tensor("out", out, q.dtype, q.device, q.shape)
+    _heads_tensor("dout", dout, q.dtype, q.device, q.shape)
+    if stats.dtype != torch.float32 or stats.device != q.device or tuple(stats.shape) != (2, w.batch, w.heads, w.nq) or not stats.is_contiguous():
+        raise ValueError("stats must be the contiguous [2][batch][heads][nq] float32 tensor of the forward")
+    with on_stream(q.device, stream) as s:
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if need_kv else None
+        dv = torch.empty(v.shape, dtype=q.dtype, device=q.device) if need_kv else None
+        dbias, grad = None, None
+        if bias is not None and need_bias:
+            dbias = torch.empty(tuple(bias.shape[:-1]) + (-(-w.nk // 8) * 8,), dtype=q.dtype, device=q.device)[..., :w.nk]
+            if w.bias.data:
+                grad = bias_tensor(dbias if dbias.dim() == 4 else dbias[None])
+        n = cross_attn_backward_workspace_size(w)
+        ws = torch.empty(n, dtype=torch.uint8, device=q.device)
+        cross_attn_backward(w, tensor(q), tensor(k), tensor(v), tensor(out), stats, tensor(dout), tensor(dq),
+                            tensor(dk) if need_kv else None, tensor(dv) if need_kv else None, grad, ws, n, s)
+    return dq, dk, dv, dbias

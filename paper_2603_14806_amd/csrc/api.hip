@@ -14,6 +14,7 @@
 #include "tri_mul.h"
 #include "opm.h"
 #include "triattn.h"
+#include "cross_attn.h"
 #include "tri_mul_check.h"
 #include "common.h"
 #include "kernels.h"
@@ -1205,6 +1206,193 @@ int tri_attn_forward(const void* q, const void* k, const void* v, const void* bi
                      void* stream) {
     const tri_attn_view_t view{rows, n, heads, out_dtype, ld_bias, 0, n, 0, 1};
     return tri_attn_chunk(&view, q, k, v, bias, mask, nullptr, out, stream);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- cross attention
+
+namespace {
+
+constexpr int64_t kCrossMaxTokens = int64_t(1) << 24, kCrossMaxToken = int64_t(1) << 23;
+constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;    // work-groups of 256 threads: 2^32 threads at most
+
+int cross_bias(const cross_attn_view_t* v, const cross_attn_bias_t* b, const char* name) {
+    if (!aligned16(b->data)) return fail(TRI_MUL_EINVAL, "%s must be 16-byte aligned", name);
+    if (b->row < v->nk || b->row % 8 || b->row > kCrossMaxTokens) return fail(TRI_MUL_EINVAL, "row stride %lld of %s must be >= nk, a multiple of 8 and at most 2^24", (long long)b->row, name);
+    if (b->batch < 0 || b->head < 0 || b->batch % 8 || b->head % 8) return fail(TRI_MUL_EINVAL, "strides of %s must be multiples of 8, and not negative", name);
+    return TRI_MUL_OK;
+}
+
+int cross_check(const cross_attn_view_t* v) {
+    if (!v) return fail(TRI_MUL_EINVAL, "null view");
+    if (v->dtype != TRI_MUL_F32 && v->dtype != TRI_MUL_BF16) return fail(TRI_MUL_EINVAL, "bad dtype %d", v->dtype);
+    if (v->batch < 0 || v->nq < 0 || v->nk < 0) return fail(TRI_MUL_EINVAL, "negative size: batch = %lld, nq = %lld, nk = %lld", (long long)v->batch, (long long)v->nq, (long long)v->nk);
+    if (v->heads < 1 || v->kv_heads < 1 || v->heads % v->kv_heads) return fail(TRI_MUL_EINVAL, "heads = %d must be a positive multiple of kv_heads = %d", v->heads, v->kv_heads);
+    if (v->heads > 1024) return fail(TRI_MUL_EUNSUPPORTED, "heads = %d above 1024", v->heads);
+    if (v->d < 8 || v->d > 128 || v->d % 8) return fail(TRI_MUL_EUNSUPPORTED, "d = %d must be a multiple of 8 in [8, 128]", v->d);
+    if (!(v->scale > 0.f) || !std::isfinite(v->scale)) return fail(TRI_MUL_EINVAL, "scale must be positive and finite");
+    const int64_t group = v->heads / v->kv_heads;
+    if (v->nk > kCrossMaxTokens || v->nq > kCrossMaxTokens / group) return fail(TRI_MUL_EUNSUPPORTED, "nq * heads / kv_heads or nk above 2^24");
+    if (v->batch > kMaxGroups) return fail(TRI_MUL_EUNSUPPORTED, "batch above 2^24 - 1");
+    if (v->bias.data)
+        if (int rc = cross_bias(v, &v->bias, "bias")) return rc;
+    if (v->mask && v->mask_batch < 0) return fail(TRI_MUL_EINVAL, "negative mask stride");
+    return TRI_MUL_OK;
+}
+
+int64_t cross_cols(const cross_attn_view_t* v) { return v->nq * (v->heads / v->kv_heads); }
+// Biases of their own (the others share one) and how many entries and heads share each.
+int64_t cross_slots(const cross_attn_view_t* v) { return (v->bias.batch ? v->batch : 1) * (v->bias.head ? v->heads : 1); }
+int64_t cross_shared(const cross_attn_view_t* v) { return (v->bias.batch ? 1 : v->batch) * (v->bias.head ? 1 : v->heads); }
+
+int cross_tensor(const cross_attn_view_t* v, const cross_attn_tensor_t* t, const char* name, int64_t tokens, int heads,
+                 bool written) {
+    if (!t) return fail(TRI_MUL_EINVAL, "null %s", name);
+    if (v->batch == 0 || tokens == 0) return TRI_MUL_OK;
+    if (!t->data) return fail(TRI_MUL_EINVAL, "null %s", name);
+    if (!aligned16(t->data)) return fail(TRI_MUL_EINVAL, "%s must be 16-byte aligned", name);
+    const int64_t per = 16 / (int64_t)esize(v->dtype);
+    if (t->batch < 0 || t->token < 0 || t->head < 0 || t->batch % per || t->token % per || t->head % per)
+        return fail(TRI_MUL_EINVAL, "strides of %s must be multiples of 16 bytes, and not negative", name);
+    if (tokens > 1 && t->token < v->d) return fail(TRI_MUL_EINVAL, "token stride %lld of %s below d = %d", (long long)t->token, name, v->d);
+    if (t->token >= kCrossMaxToken) return fail(TRI_MUL_EUNSUPPORTED, "token stride %lld of %s is 2^23 or more", (long long)t->token, name);
+    if ((heads > 1 && t->head < v->d && (written || t->head)) || (v->batch > 1 && t->batch < v->d && (written || t->batch)))
+        return fail(TRI_MUL_EINVAL, "batch or head stride of %s below d = %d", name, v->d);
+    return TRI_MUL_OK;
+}
+
+trimul::CrossTensor cross_arg(const cross_attn_tensor_t* t) {
+    return t ? trimul::CrossTensor{t->data, t->batch, t->token, t->head} : trimul::CrossTensor{};
+}
+
+trimul::CrossArgs cross_args(const cross_attn_view_t* v, const cross_attn_tensor_t* q, const cross_attn_tensor_t* k,
+                             const cross_attn_tensor_t* vv, const cross_attn_tensor_t* out) {
+    trimul::CrossArgs a{};
+    a.q = cross_arg(q);
+    a.k = cross_arg(k);
+    a.v = cross_arg(vv);
+    a.out = cross_arg(out);
+    a.bias = {v->bias.data, v->bias.batch, v->bias.head, v->bias.row};
+    a.mask = v->mask;
+    a.mask_batch = v->mask_batch;
+    a.batch = v->batch;
+    a.nq = (int)v->nq;
+    a.nk = (int)v->nk;
+    a.heads = v->heads;
+    a.kv_heads = v->kv_heads;
+    a.group = v->heads / v->kv_heads;
+    a.d = v->d;
+    a.scale = v->scale;
+    a.splits = 1;
+    return a;
+}
+
+int cross_workspace(const void* ws, size_t ws_bytes, size_t need) {
+    if (!need) return TRI_MUL_OK;
+    if (!ws) return fail(TRI_MUL_EINVAL, "null workspace, %zu bytes needed", need);
+    if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(TRI_MUL_EINVAL, "workspace must be 256-byte aligned");
+    if (ws_bytes < need) return fail(TRI_MUL_ENOMEM, "workspace of %zu bytes < %zu needed", ws_bytes, need);
+    return TRI_MUL_OK;
+}
+
+// The backward's workspace: D of every query and head, then the partial sums of dbias.
+size_t cross_delta_bytes(const cross_attn_view_t* v) { return round256((size_t)v->batch * v->heads * v->nq * 4); }
+int cross_bias_splits(const cross_attn_view_t* v) {
+    return v->bias.data ? trimul::cross_dbias_splits(v->dtype, cross_slots(v), cross_shared(v), v->nq, v->nk) : 1;
+}
+
+}  // namespace
+
+extern "C" {
+
+int cross_attn_workspace_size(const cross_attn_view_t* v, size_t* bytes) {
+    if (int rc = cross_check(v)) return rc;
+    if (!bytes) return fail(TRI_MUL_EINVAL, "null bytes pointer");
+    const trimul::CrossPlan p = trimul::cross_plan(v->batch, v->kv_heads, cross_cols(v), v->nk);
+    *bytes = trimul::cross_part_floats(p, v->batch, v->nq, v->heads, v->d) * 4;
+    return ok();
+}
+
+int cross_attn_forward(const cross_attn_view_t* v, const cross_attn_tensor_t* q, const cross_attn_tensor_t* k,
+                       const cross_attn_tensor_t* vv, const cross_attn_tensor_t* out, float* stats, void* ws,
+                       size_t ws_bytes, void* stream) {
+    if (int rc = cross_check(v)) return rc;
+    if (int rc = cross_tensor(v, q, "q", v->nq, v->heads, false)) return rc;
+    if (int rc = cross_tensor(v, k, "k", v->nk, v->kv_heads, false)) return rc;
+    if (int rc = cross_tensor(v, vv, "v", v->nk, v->kv_heads, false)) return rc;
+    if (int rc = cross_tensor(v, out, "out", v->nq, v->heads, true)) return rc;
+    const trimul::CrossPlan p = trimul::cross_plan(v->batch, v->kv_heads, cross_cols(v), v->nk);
+    if (v->batch * v->kv_heads > kMaxGroups || v->batch * v->kv_heads * ((cross_cols(v) + p.cols - 1) / p.cols) * p.splits > kMaxGroups)
+        return fail(TRI_MUL_EUNSUPPORTED, "too many entries, heads and queries for one call");
+    if (int rc = cross_workspace(ws, ws_bytes, trimul::cross_part_floats(p, v->batch, v->nq, v->heads, v->d) * 4)) return rc;
+    if (v->batch == 0 || v->nq == 0) return ok();
+    trimul::CrossArgs a = cross_args(v, q, k, vv, out);
+    a.stats = stats;
+    a.part = static_cast<float*>(ws);
+    const hipError_t e = trimul::launch_cross_forward(v->dtype, a, p, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "attention kernel launch");
+    return ok();
+}
+
+int cross_attn_backward_workspace_size(const cross_attn_view_t* v, size_t* bytes) {
+    if (int rc = cross_check(v)) return rc;
+    if (!bytes) return fail(TRI_MUL_EINVAL, "null bytes pointer");
+    *bytes = cross_delta_bytes(v) + trimul::cross_dbias_part_floats(v->dtype, cross_bias_splits(v), cross_slots(v), v->nq, v->nk) * 4;
+    return ok();
+}
+
+int cross_attn_backward(const cross_attn_view_t* v, const cross_attn_tensor_t* q, const cross_attn_tensor_t* k,
+                        const cross_attn_tensor_t* vv, const cross_attn_tensor_t* out, const float* stats,
+                        const cross_attn_tensor_t* dout, const cross_attn_tensor_t* dq,
+                        const cross_attn_tensor_t* dk, const cross_attn_tensor_t* dv,
+                        const cross_attn_bias_t* dbias, void* ws, size_t ws_bytes, void* stream) {
+    if (int rc = cross_check(v)) return rc;
+    if (int rc = cross_tensor(v, q, "q", v->nq, v->heads, false)) return rc;
+    if (int rc = cross_tensor(v, k, "k", v->nk, v->kv_heads, false)) return rc;
+    if (int rc = cross_tensor(v, vv, "v", v->nk, v->kv_heads, false)) return rc;
+    if (int rc = cross_tensor(v, out, "out", v->nq, v->heads, false)) return rc;
+    if (int rc = cross_tensor(v, dout, "dout", v->nq, v->heads, false)) return rc;
+    if (int rc = cross_tensor(v, dq, "dq", v->nq, v->heads, true)) return rc;
+    if (!dk != !dv) return fail(TRI_MUL_EINVAL, "dk and dv are both given or both NULL");
+    if (dk) {
+        if (int rc = cross_tensor(v, dk, "dk", v->nk, v->kv_heads, true)) return rc;
+        if (int rc = cross_tensor(v, dv, "dv", v->nk, v->kv_heads, true)) return rc;
+    }
+    if (dbias) {
+        if (!v->bias.data || !dbias->data) return fail(TRI_MUL_EINVAL, "dbias without a bias, or without data");
+        if (int rc = cross_bias(v, dbias, "dbias")) return rc;
+        if ((v->bias.batch && v->batch > 1 && !dbias->batch) || (v->bias.head && v->heads > 1 && !dbias->head))
+            return fail(TRI_MUL_EINVAL, "dbias shared along an axis that the bias is not shared along");
+    }
+    const bool queries = v->batch > 0 && v->nq > 0;
+    if (queries && !stats) return fail(TRI_MUL_EINVAL, "null stats");
+    const int splits = cross_bias_splits(v);
+    const int64_t bh = v->batch * v->kv_heads;
+    if (bh > kMaxGroups || bh * ((cross_cols(v) + 127) / 128) > kMaxGroups || bh * ((v->nk + 127) / 128) > kMaxGroups ||
+        (dbias && (cross_slots(v) > kMaxGroups || cross_slots(v) * splits * ((v->nq + 127) / 128) > kMaxGroups ||
+                   cross_slots(v) * splits * ((v->nq + 127) / 128) * ((v->nk + 31) / 32) > kMaxGroups)))
+        return fail(TRI_MUL_EUNSUPPORTED, "too many entries, heads, queries and keys for one call");
+    size_t need = 0;
+    if (int rc = cross_attn_backward_workspace_size(v, &need)) return rc;
+    if (int rc = cross_workspace(ws, ws_bytes, need)) return rc;
+    trimul::CrossArgs a = cross_args(v, q, k, vv, out);
+    a.dout = cross_arg(dout);
+    a.dq = cross_arg(dq);
+    a.dk = cross_arg(dk);
+    a.dv = cross_arg(dv);
+    if (dbias) a.dbias = {dbias->data, dbias->batch, dbias->head, dbias->row};
+    a.stats = const_cast<float*>(stats);
+    a.delta = static_cast<float*>(ws);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + cross_delta_bytes(v));
+    a.splits = splits;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e = hipSuccess;
+    if (queries) e = trimul::launch_cross_backward_q(v->dtype, a, s);
+    if (e == hipSuccess && dk && v->batch > 0 && v->nk > 0) e = trimul::launch_cross_backward_kv(v->dtype, a, s);
+    if (e == hipSuccess && dbias && v->nq > 0 && v->nk > 0 && cross_slots(v) > 0) e = trimul::launch_cross_backward_bias(v->dtype, a, s);
+    if (e != hipSuccess) return hip_fail(e, "attention backward kernel launch");
+    return ok();
 }
 
 int tri_mul_check_contract_loads(int a_mode, int b_mode, int64_t M, int64_t N, int64_t K, int64_t lda,

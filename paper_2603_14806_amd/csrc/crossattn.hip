@@ -1,0 +1,348 @@
+// Attention of queries over keys of another length, forward: one pass over
+// the keys with a running maximum M, sum L and unnormalised output,
+//
+//     x_ij = scale q_i . k_j + bias_ij,   out_i = sum_j exp(x_ij - M_i) v_j / L_i
+//
+// Scores are computed transposed, S^T = K Q^T, so that a lane holds one query
+// and KC / 2 consecutive keys of each chunk of KC: maximum and sum are its own
+// registers' and its partner's (lane ^ 32), its bias is contiguous, and the
+// weights feed O^T += V^T P^T from the registers they are in.
+#include "crossattn.h"
+
+namespace trimul {
+namespace {
+
+template <typename T>
+__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+    else *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
+}
+
+// WK = 1: a wave takes 32 columns and every chunk, the chunks staged by all
+// four waves (double-buffered).  WK = 4: 32 columns, wave w takes chunks w,
+// w + 4, ..., stages them for itself, and the four results are merged at the end.
+template <typename T, int DP, int KC, int WK, bool BIAS>
+__global__ __launch_bounds__(256) void k_cross_forward(const CrossArgs a, int ctiles) {
+    using TL = Tile<T, DP, KC>;
+    constexpr int NT = 256 / WK, NB = KC / 32, ND = DP / 32, NS = DP / 16;
+    __shared__ __align__(16) char mem[(WK == 1 ? 2 : 4) * 2 * TL::kBytes];
+    __shared__ float red[WK == 1 ? 1 : 2][WK == 1 ? 1 : 4][32];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, ql = lane & 31, hi = lane >> 5;
+    const int t = WK == 1 ? threadIdx.x : lane;
+
+    int64_t blk = blockIdx.x;
+    const int split = (int)(blk % a.splits);
+    blk /= a.splits;
+    const int ct = (int)(blk % ctiles);
+    blk /= ctiles;
+    const int hk = (int)(blk % a.kv_heads);
+    const int64_t b = blk / a.kv_heads;
+    const int ncols = a.nq * a.group;
+    const int cw = ct * (128 / WK) + (WK == 1 ? 32 * w : 0);      // the wave's first column
+    const bool wave_live = cw < ncols;
+    const bool valid = cw + ql < ncols;
+    const int col = min(cw + ql, ncols - 1);
+    const int qi = col / a.group, h = hk * a.group + (col - qi * a.group);
+
+    Frag<T> qf[NS];
+    {
+        const T* row = (const T*)a.q.data + b * a.q.batch + (int64_t)qi * a.q.token + h * a.q.head;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) load_row(row, s, hi, a.d, qf[s]);
+    }
+    const T* kb = (const T*)a.k.data + b * a.k.batch + hk * a.k.head;
+    const T* vb = (const T*)a.v.data + b * a.v.batch + hk * a.v.head;
+    const T* brow = BIAS ? (const T*)a.bias.data + b * a.bias.batch + h * a.bias.head + (int64_t)qi * a.bias.row : nullptr;
+    const uint8_t* mask = a.mask ? a.mask + b * a.mask_batch : nullptr;
+    const int ks = split * a.split_keys, ke = min(a.nk, ks + a.split_keys);
+    const int nchunks = (ke - ks + KC - 1) / KC;
+
+    // without a bias x stays in units of q . k and the scale is part of the exponential's factor
+    const float coef = BIAS ? kLog2e : a.scale * kLog2e;
+    f32x16_t o[ND];
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
+    float M = -INFINITY, L = 0.f;
+
+    Part<T, DP, KC, NT> kp, vp;
+    KeyByte kbyte;
+    BiasRow<T, KC> bp;
+    auto load = [&](int c) {
+        const int k0 = ks + c * KC;
+        kp.load(kb, a.k.token, k0, a.nk, a.d, t);
+        vp.load(vb, a.v.token, k0, a.nk, a.d, t);
+        kbyte.load(mask, k0, a.nk, lane);
+    };
+    const int c0 = WK == 1 ? 0 : w;
+    if (c0 < nchunks) {
+        load(c0);
+        if (BIAS) bp.load(brow, ks + c0 * KC + (KC / 2) * hi, a.nk);
+    }
+    for (int c = c0; c < nchunks; c += WK) {
+        char* kt = mem + (WK == 1 ? (c & 1) : w) * 2 * TL::kBytes;
+        char* vt = kt + TL::kBytes;
+        const int k0 = ks + c * KC;
+        uint64_t bits = kbyte.bits(k0, ke, lane);
+        if (KC == 32) bits &= 0xffffffffull;
+        const bool some = bits != (KC == 64 ? ~0ull : 0xffffffffull);
+        if (WK > 1) {   // a wave's LDS operations run in order; only the compiler has to be kept from moving them
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        kp.stage(kt, t, some, bits);
+        vp.stage(vt, t, some, bits);
+        if (c + WK < nchunks) load(c + WK);
+        if (WK == 1) {
+            __syncthreads();
+        } else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        if (bits != 0 && wave_live) {
+            f32x16_t s[NB];
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[n][r] = 0.f;
+#pragma unroll
+                for (int i = 0; i < NS; ++i) {
+                    Frag<T> f;
+                    TL::rows(kt, lane, n, i, f);
+                    s[n] = mma(f, qf[i], s[n]);
+                }
+            }
+            float cm = -INFINITY;
+            const uint32_t mine = (uint32_t)(bits >> ((KC / 2) * hi));
+            auto scores = [&](bool masked) {
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        float4 bv;
+                        if (BIAS) bv = bp.get(n, g);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float x = s[n][4 * g + e];
+                            if (BIAS) x = __builtin_fmaf(x, a.scale, f4_get(bv, e));
+                            if (masked) x = (mine >> (16 * n + 4 * g + e)) & 1 ? x : -INFINITY;
+                            s[n][4 * g + e] = x;
+                        }
+                        cm = fmaxf(fmaxf(cm, s[n][4 * g]), s[n][4 * g + 1]);
+                        cm = fmaxf(fmaxf(cm, s[n][4 * g + 2]), s[n][4 * g + 3]);
+                    }
+            };
+            if (some) scores(true);
+            else scores(false);
+            if (BIAS && c + WK < nchunks) bp.load(brow, k0 + WK * KC + (KC / 2) * hi, a.nk);
+            cm = fmaxf(cm, xor32(cm));
+            const float Mn = fmaxf(M, cm);
+            const float Ms = Mn == -INFINITY ? 0.f : Mn;      // no key yet: every x is -inf and every weight 0
+            const float alpha = __builtin_amdgcn_exp2f((M - Ms) * coef);
+            L *= alpha;
+#pragma unroll
+            for (int i = 0; i < ND; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
+            M = Mn;
+            const float nsh = -Ms * coef;
+            float ps = 0.f;
+            if (__any(!(fabsf(nsh) <= kFmaMax))) {
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        s[n][r] = __builtin_amdgcn_exp2f((s[n][r] - Ms) * coef);
+                        ps += s[n][r];
+                    }
+            } else {
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        s[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], coef, nsh));
+                        ps += s[n][r];
+                    }
+            }
+            L += ps;
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int tt = 0; tt < 2; ++tt) {
+                    Frag<T> pf;
+                    take8(s[n], tt, pf);
+#pragma unroll
+                    for (int i = 0; i < ND; ++i) {
+                        Frag<T> vf;
+                        TL::cols(vt, lane, n, tt, i, vf);
+                        o[i] = mma(vf, pf, o[i]);
+                    }
+                }
+        } else if (BIAS && c + WK < nchunks) {
+            bp.load(brow, k0 + WK * KC + (KC / 2) * hi, a.nk);
+        }
+    }
+
+    float Lt = L + xor32(L);
+    constexpr int NG = ND * 4;              // groups of four channels a lane holds
+    int g0 = 0, g1 = NG;
+    if constexpr (WK > 1) {
+        float* buf = reinterpret_cast<float*>(mem);
+        if (!hi) {
+            red[0][w][ql] = M;
+            red[1][w][ql] = Lt;
+        }
+        __syncthreads();                    // also: every wave is done with its tiles
+        const float Mn = fmaxf(fmaxf(red[0][0][ql], red[0][1][ql]), fmaxf(red[0][2][ql], red[0][3][ql]));
+        const float Ms = Mn == -INFINITY ? 0.f : Mn;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += red[1][i][ql] * __builtin_amdgcn_exp2f((red[0][i][ql] - Ms) * coef);
+        const float f = __builtin_amdgcn_exp2f((M - Ms) * coef);
+#pragma unroll
+        for (int i = 0; i < ND; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) buf[(w * ND * 16 + 16 * i + r) * 64 + lane] = o[i][r] * f;
+        __syncthreads();
+        M = Mn;
+        Lt = sum;
+        g0 = w * ND;
+        g1 = g0 + ND;                       // each wave adds and writes a quarter of the channels
+#pragma unroll
+        for (int j = 0; j < ND; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float x = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x += buf[(i * ND * 16 + 4 * (g0 + j) + e) * 64 + lane];
+                o[j / 4][4 * (j % 4) + e] = x;
+            }
+    }
+    if (!valid) return;
+    const int64_t row = (b * a.heads + h) * a.nq + qi;
+    if (a.splits > 1) {
+        const int64_t rows = a.batch * a.heads * a.nq, at = (int64_t)split * rows + row;
+        float* po = a.part + at * a.d;
+#pragma unroll
+        for (int j = 0; j < (WK > 1 ? ND : NG); ++j) {
+            const int c = 8 * (g0 + j) + 4 * hi;
+            if (c < a.d)
+                *reinterpret_cast<float4*>(po + c) = make_float4(o[j / 4][4 * (j % 4)], o[j / 4][4 * (j % 4) + 1],
+                                                                 o[j / 4][4 * (j % 4) + 2], o[j / 4][4 * (j % 4) + 3]);
+        }
+        if (!hi && (WK == 1 || w == 0)) {
+            float* pm = a.part + (int64_t)a.splits * rows * a.d;
+            pm[at] = M;
+            pm[(int64_t)a.splits * rows + at] = Lt;
+        }
+        return;
+    }
+    const float inv = Lt == 0.f ? 0.f : 1.f / Lt;
+    T* po = (T*)a.out.data + b * a.out.batch + (int64_t)qi * a.out.token + h * a.out.head;
+#pragma unroll
+    for (int j = 0; j < (WK > 1 ? ND : NG); ++j) {
+        const int c = 8 * (g0 + j) + 4 * hi;
+        if (c < a.d)
+            store4(po + c, o[j / 4][4 * (j % 4)] * inv, o[j / 4][4 * (j % 4) + 1] * inv,
+                   o[j / 4][4 * (j % 4) + 2] * inv, o[j / 4][4 * (j % 4) + 3] * inv);
+    }
+    if (a.stats && !hi && (WK == 1 || w == 0)) {
+        a.stats[row] = BIAS ? M : M * a.scale;
+        a.stats[a.batch * a.heads * a.nq + row] = Lt;
+    }
+}
+
+// The splits of one (entry, head, query) joined: out = sum_s exp(M_s - M) O_s / sum_s exp(M_s - M) L_s.
+template <typename T>
+__global__ __launch_bounds__(64) void k_cross_join(const CrossArgs a) {
+    __shared__ float wt[kCrossMaxSplits];
+    const int64_t rows = a.batch * a.heads * a.nq, row = blockIdx.x;
+    const int lane = threadIdx.x;
+    const float coef = a.bias.data ? kLog2e : a.scale * kLog2e;
+    const float* pm = a.part + (int64_t)a.splits * rows * a.d;
+    const float m = lane < a.splits ? pm[(int64_t)lane * rows + row] : -INFINITY;
+    float l = lane < a.splits ? pm[((int64_t)a.splits + lane) * rows + row] : 0.f;
+    float M = m;
+#pragma unroll
+    for (int i = 32; i; i >>= 1) M = fmaxf(M, __shfl_xor(M, i));
+    const float Ms = M == -INFINITY ? 0.f : M;
+    const float f = __builtin_amdgcn_exp2f((m - Ms) * coef);
+    wt[lane] = f;
+    l *= f;
+#pragma unroll
+    for (int i = 32; i; i >>= 1) l += __shfl_xor(l, i);
+    __syncthreads();
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int qi = (int)(row % a.nq);
+    const int64_t bh = row / a.nq, b = bh / a.heads;
+    const int h = (int)(bh - b * a.heads);
+    T* po = (T*)a.out.data + b * a.out.batch + (int64_t)qi * a.out.token + h * a.out.head;
+    for (int c = lane; c < a.d; c += 64) {
+        float x = 0.f;
+        for (int s = 0; s < a.splits; ++s) x += wt[s] * a.part[((int64_t)s * rows + row) * a.d + c];
+        Store<T>::st(po + c, x * inv);
+    }
+    if (a.stats && lane == 0) {
+        a.stats[row] = a.bias.data ? M : M * a.scale;
+        a.stats[rows + row] = l;
+    }
+}
+
+template <typename T, int DP, bool BIAS>
+hipError_t forward(const CrossArgs& a, const CrossPlan& p, hipStream_t s) {
+    constexpr int KC = sizeof(T) == 2 ? 64 : 32;
+    const int ctiles = (a.nq * a.group + p.cols - 1) / p.cols;
+    const dim3 grid((unsigned)(a.batch * a.kv_heads * ctiles * p.splits));
+    if (p.cols == 128)
+        hipLaunchKernelGGL((k_cross_forward<T, DP, KC, 1, BIAS>), grid, dim3(256), 0, s, a, ctiles);
+    else
+        hipLaunchKernelGGL((k_cross_forward<T, DP, 32, 4, BIAS>), grid, dim3(256), 0, s, a, ctiles);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    hipLaunchKernelGGL((k_cross_join<T>), dim3((unsigned)(a.batch * a.heads * a.nq)), dim3(64), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T, int DP>
+hipError_t forward(const CrossArgs& a, const CrossPlan& p, hipStream_t s) {
+    return a.bias.data ? forward<T, DP, true>(a, p, s) : forward<T, DP, false>(a, p, s);
+}
+
+template <typename T>
+hipError_t forward(const CrossArgs& a, const CrossPlan& p, hipStream_t s) {
+    return a.d <= 32 ? forward<T, 32>(a, p, s) : a.d <= 64 ? forward<T, 64>(a, p, s) : forward<T, 128>(a, p, s);
+}
+
+}  // namespace
+
+// Few columns: 32 to a work-group, its waves on different keys.  The keys are
+// split where the work-groups alone would not give each of the 256 compute
+// units two, as long as a split keeps 256 keys (two chunks a wave).
+CrossPlan cross_plan(int64_t batch, int kv_heads, int64_t cols, int64_t nk) {
+    CrossPlan p{cols <= 32 ? 32 : 128, 1, (int)((nk + 63) / 64 * 64)};
+    const int64_t groups = batch * kv_heads * ((cols + p.cols - 1) / p.cols);
+    if (groups > 0 && groups < 512) {
+        int64_t n = (512 + groups - 1) / groups;
+        if (n > nk / 256) n = nk / 256;
+        if (n > kCrossMaxSplits) n = kCrossMaxSplits;
+        if (n > 1) {
+            p.split_keys = (int)(((nk + n - 1) / n + 63) / 64 * 64);
+            p.splits = (int)((nk + p.split_keys - 1) / p.split_keys);
+        }
+    }
+    return p;
+}
+
+size_t cross_part_floats(const CrossPlan& p, int64_t batch, int64_t nq, int heads, int d) {
+    return p.splits > 1 ? (size_t)p.splits * (size_t)batch * (size_t)nq * (size_t)heads * (size_t)(d + 2) : 0;
+}
+
+hipError_t launch_cross_forward(int dtype, const CrossArgs& args, const CrossPlan& p, hipStream_t s) {
+    CrossArgs a = args;
+    a.splits = p.splits;
+    a.split_keys = p.split_keys;
+    return dtype == 1 ? forward<bf16_t>(a, p, s) : forward<float>(a, p, s);
+}
+
+}  // namespace trimul

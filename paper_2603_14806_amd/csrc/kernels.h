@@ -188,4 +188,45 @@ hipError_t launch_triattn(int out_dtype, const void* q, const void* k, const voi
                           const uint8_t* mask, int64_t rows, int64_t N, int H, int64_t ldb, int64_t k0, int64_t kend,
                           float* stA, float* stM, float* stL, int load_state, int finish, void* out, hipStream_t s);
 
+// Attention of queries over keys of another length (crossattn.hip,
+// crossattn_backward.hip).  The queries of one key head are taken together
+// as "columns": column c of key head hk is query c / group of head
+// hk * group + c % group, so that the heads that share K and V read them once.
+struct CrossTensor {
+    void* data;
+    int64_t batch, token, head;   // strides in elements
+};
+struct CrossBias {
+    void* data;                   // null: none
+    int64_t batch, head, row;     // strides in elements; 0 along a shared axis (batch, head)
+};
+struct CrossArgs {
+    CrossTensor q, k, v, out, dout, dq, dk, dv;
+    CrossBias bias, dbias;
+    const uint8_t* mask;
+    int64_t mask_batch;
+    float* stats;      // [2][batch][heads][nq]: maximum, sum
+    float* delta;      // [batch][heads][nq]: dout . out (written by the query pass, read by the other two)
+    float* part;       // partial results of split calls
+    int64_t batch;
+    int nq, nk, heads, kv_heads, group, d;
+    float scale;
+    int splits, split_keys;   // forward: key ranges [s * split_keys, ...); dbias: splits of the shared entries
+};
+// How a forward call is laid out: columns per work-group (32: the four waves
+// take different keys; 128: 32 columns a wave), and the split of the keys.
+constexpr int kCrossMaxSplits = 64;   // one lane of the join each
+struct CrossPlan {
+    int cols, splits, split_keys;
+};
+CrossPlan cross_plan(int64_t batch, int kv_heads, int64_t cols, int64_t nk);
+size_t cross_part_floats(const CrossPlan& p, int64_t batch, int64_t nq, int heads, int d);
+// Splits of the dbias pass over `shared` entries and heads per bias.
+int cross_dbias_splits(int dtype, int64_t slots, int64_t shared, int64_t nq, int64_t nk);
+size_t cross_dbias_part_floats(int dtype, int splits, int64_t slots, int64_t nq, int64_t nk);
+hipError_t launch_cross_forward(int dtype, const CrossArgs& a, const CrossPlan& p, hipStream_t s);
+hipError_t launch_cross_backward_q(int dtype, const CrossArgs& a, hipStream_t s);
+hipError_t launch_cross_backward_kv(int dtype, const CrossArgs& a, hipStream_t s);
+hipError_t launch_cross_backward_bias(int dtype, const CrossArgs& a, hipStream_t s);
+
 }  // namespace trimul
