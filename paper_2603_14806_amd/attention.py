@@ -5,13 +5,12 @@ tensors and allocate outputs and workspaces with torch.
 Every call runs on the device its tensors are on, on `stream` (a torch stream
 or a raw hipStream_t) or that device's current stream, and allocates there.
 """
-import contextlib
 import ctypes
 
 import torch
 
 from . import trimul as _t
-from .trimul import TRI_MUL_BF16, TRI_MUL_F32, _check, _i32, _i64, _ptr, _vp
+from .trimul import TRI_MUL_BF16, TRI_MUL_F32, _check, _i32, _i64, _ptr, _vp, on_stream
 
 _DTYPES = {torch.float32: TRI_MUL_F32, torch.bfloat16: TRI_MUL_BF16}
 
@@ -97,21 +96,6 @@ def tensor(t):
 def bias_tensor(t):
     """cross_attn_bias_t of a [batch or 1][heads or 1][nq][nk] tensor: an axis of length 1 is shared."""
     return CrossAttnBias(_ptr(t), 0 if t.shape[0] == 1 else t.stride(0), 0 if t.shape[1] == 1 else t.stride(1), t.stride(2))
-
-
-@contextlib.contextmanager
-def on_stream(device, stream):
-    """The device, and on it `stream` (None: the current one) as torch's current stream: what is allocated here
-    belongs to that stream, so that a workspace freed at the end is reused behind the kernels that use it."""
-    with torch.cuda.device(device):
-        if stream is None:
-            yield torch.cuda.current_stream(device).cuda_stream
-            return
-        s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device)
-        if s.device != device:
-            raise ValueError(f"stream of {s.device} for tensors on {device}")
-        with torch.cuda.stream(s):
-            yield s.cuda_stream
 
 
 def _heads_tensor(name, t, dtype, device, shape):

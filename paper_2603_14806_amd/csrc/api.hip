@@ -15,6 +15,7 @@
 #include "opm.h"
 #include "triattn.h"
 #include "cross_attn.h"
+#include "pair_dropout.h"
 #include "tri_mul_check.h"
 #include "common.h"
 #include "kernels.h"
@@ -1392,6 +1393,79 @@ int cross_attn_backward(const cross_attn_view_t* v, const cross_attn_tensor_t* q
     if (e == hipSuccess && dk && v->batch > 0 && v->nk > 0) e = trimul::launch_cross_backward_kv(v->dtype, a, s);
     if (e == hipSuccess && dbias && v->nq > 0 && v->nk > 0 && cross_slots(v) > 0) e = trimul::launch_cross_backward_bias(v->dtype, a, s);
     if (e != hipSuccess) return hip_fail(e, "attention backward kernel launch");
+    return ok();
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- residual addition with dropout
+
+namespace {
+
+bool aligned_to(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % esize(dtype) == 0; }
+
+int dropout_check(const pair_dropout_view_t* v) {
+    if (!v) return fail(TRI_MUL_EINVAL, "null view");
+    for (int t : {v->x_dtype, v->out_dtype})
+        if (t != TRI_MUL_F32 && t != TRI_MUL_BF16) return fail(TRI_MUL_EINVAL, "bad dtype %d", t);
+    if (v->share < PAIR_DROPOUT_EACH || v->share > PAIR_DROPOUT_COLUMNS) return fail(TRI_MUL_EINVAL, "bad sharing %d", v->share);
+    if (!(v->p >= 0.0 && v->p < 1.0)) return fail(TRI_MUL_EINVAL, "p = %g outside [0, 1)", v->p);
+    if (v->rows < 0 || v->cols < 0 || v->channels < 0 || v->row0 < 0 || v->col0 < 0) return fail(TRI_MUL_EINVAL, "negative size or place");
+    if (v->cols > v->n_cols || v->col0 > v->n_cols - v->cols) return fail(TRI_MUL_EINVAL, "columns [%lld, +%lld) outside the %lld of the whole tensor", (long long)v->col0, (long long)v->cols, (long long)v->n_cols);
+    const __int128 one = 1, last_row = (__int128)v->row0 + v->rows, row = (__int128)v->n_cols * v->channels;
+    if ((__int128)v->cols * v->channels >= one << 31) return fail(TRI_MUL_EUNSUPPORTED, "a row of 2^31 elements or more");
+    if (row >= one << 62 || last_row >= one << 62 || last_row * row >= one << 62) return fail(TRI_MUL_EUNSUPPORTED, "a tensor of 2^62 elements or more");
+    if (v->rows > 1 && (v->ld_x < v->cols * v->channels || v->ld_out < v->cols * v->channels)) return fail(TRI_MUL_EINVAL, "a row stride below cols * channels");
+    if (v->rows > (int64_t(1) << 40) || v->ld_x > (int64_t(1) << 40) || v->ld_out > (int64_t(1) << 40) || v->ld_x < 0 || v->ld_out < 0)
+        return fail(TRI_MUL_EINVAL, "rows or a row stride above 2^40, or negative");
+    return TRI_MUL_OK;
+}
+
+trimul::DropoutArgs dropout_args(const pair_dropout_view_t* v) {
+    trimul::DropoutArgs a{};
+    a.rows = v->rows;
+    a.cols = v->cols;
+    a.channels = v->channels;
+    a.row0 = v->row0;
+    a.col0 = v->col0;
+    a.n_cols = v->n_cols;
+    a.seed = v->seed;
+    a.offset = v->offset;
+    a.threshold = (uint32_t)std::min(std::nearbyint(v->p * 4294967296.0), 4294967295.0);
+    a.scale = (float)(1.0 / (1.0 - v->p));
+    return a;
+}
+
+bool dropout_empty(const pair_dropout_view_t* v) { return v->rows == 0 || v->cols == 0 || v->channels == 0; }
+
+}  // namespace
+
+extern "C" {
+
+int pair_dropout_add(const pair_dropout_view_t* v, const void* x, const void* res, void* out, void* stream) {
+    if (int rc = dropout_check(v)) return rc;
+    if (dropout_empty(v)) return ok();
+    if (!x || !out) return fail(TRI_MUL_EINVAL, "null x or out");
+    if (!aligned_to(x, v->x_dtype) || !aligned_to(res, v->out_dtype) || !aligned_to(out, v->out_dtype))
+        return fail(TRI_MUL_EINVAL, "x, res and out must be aligned to their type");
+    trimul::DropoutArgs a = dropout_args(v);
+    a.ld_in = v->ld_x;
+    a.ld_res = a.ld_res_out = v->ld_out;
+    const hipError_t e = trimul::launch_pair_dropout(v->x_dtype, v->out_dtype, v->share, a, x, res, out, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "dropout kernel launch");
+    return ok();
+}
+
+int pair_dropout_backward(const pair_dropout_view_t* v, const void* dout, void* dx, void* stream) {
+    if (int rc = dropout_check(v)) return rc;
+    if (dropout_empty(v)) return ok();
+    if (!dout || !dx) return fail(TRI_MUL_EINVAL, "null dout or dx");
+    if (!aligned_to(dout, v->out_dtype) || !aligned_to(dx, v->x_dtype)) return fail(TRI_MUL_EINVAL, "dout and dx must be aligned to their type");
+    trimul::DropoutArgs a = dropout_args(v);
+    a.ld_in = v->ld_out;
+    a.ld_res_out = v->ld_x;
+    const hipError_t e = trimul::launch_pair_dropout(v->out_dtype, v->x_dtype, v->share, a, dout, nullptr, dx, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "dropout backward kernel launch");
     return ok();
 }
 

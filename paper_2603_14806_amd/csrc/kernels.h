@@ -229,4 +229,18 @@ hipError_t launch_cross_backward_q(int dtype, const CrossArgs& a, hipStream_t s)
 hipError_t launch_cross_backward_kv(int dtype, const CrossArgs& a, hipStream_t s);
 hipError_t launch_cross_backward_bias(int dtype, const CrossArgs& a, hipStream_t s);
 
+// Residual addition with dropout (dropout.hip): out = res + kept x scale over
+// [rows][cols][channels], res null for 0; share 0: a mask value per element,
+// 1: all rows share one, 2: all columns do.
+struct DropoutArgs {
+    int64_t rows, cols, channels, row0, col0, n_cols, ld_in, ld_res, ld_res_out;   // row strides: x, res, out
+    uint64_t seed, offset;
+    uint32_t threshold;   // dropped below it
+    float scale;
+    int64_t loop;                    // filled in by the launcher, as are the next
+    int blocks, lanes, span;
+};
+hipError_t launch_pair_dropout(int in_dtype, int out_dtype, int share, const DropoutArgs& a, const void* x,
+                               const void* res, void* out, hipStream_t s);
+
 }  // namespace trimul

@@ -6,6 +6,7 @@ kernels.  PyTorch provides device memory and streams.  The functions keep the
 C names; TriMul and OuterProductMean are small convenience wrappers that own
 a handle.
 """
+import contextlib
 import ctypes
 import os
 
@@ -177,6 +178,21 @@ def _stream(stream):
     if stream is None:
         return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+
+
+@contextlib.contextmanager
+def on_stream(device, stream):
+    """The device, and on it `stream` (None: the current one) as torch's current stream: what is allocated here
+    belongs to that stream, so that a workspace freed at the end is reused behind the kernels that use it."""
+    with torch.cuda.device(device):
+        if stream is None:
+            yield torch.cuda.current_stream(device).cuda_stream
+            return
+        s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device)
+        if s.device != device:
+            raise ValueError(f"stream of {s.device} for tensors on {device}")
+        with torch.cuda.stream(s):
+            yield s.cuda_stream
 
 
 # ---------------------------------------------------------------- C names
@@ -449,6 +465,23 @@ class TriMul:
         else:
             tri_mul_layer_backward_saved(self.h, direction, z, mask, N, *saved, dout, dz, grads, ws, wsb, stream)
         return dz, grads
+
+    def residual(self, z, mask=None, direction="outgoing", p=0.25, seed=0, offset=0, share="rows", out=None,
+                 stream=None):
+        """z + dropout(update of z) in the storage dtype (include/pair_dropout.h; the pair stack shares the mask
+        along the rows); with p = 0 the plain residual addition.  out may be z itself."""
+        from . import dropout
+        with on_stream(z.device, stream) as s:
+            return dropout.dropout_add(self(z, mask, direction, stream=s), z, p, seed, offset, share, out=out, stream=s)
+
+    def residual_backward(self, z, dout, mask=None, direction="outgoing", p=0.25, seed=0, offset=0, share="rows",
+                          stream=None, saved=None):
+        """Gradients of sum(residual(z) * dout): (dz, grads), dout and dz in the storage dtype."""
+        from . import dropout
+        with on_stream(z.device, stream) as s:
+            du = dropout.dropout_backward(dout, p, seed, offset, share, dtype=self.out_dtype, stream=s)
+            dz, grads = self.backward(z, du, mask, direction, s, saved)
+            return dropout.dropout_add(dz, dout, 0.0, stream=s), grads
 
     def block_accumulate(self, view, a_panel, b_panel, acc, mask=None, z_tile=None, out_tile=None, stream=None,
                          ws=None):
