@@ -58,52 +58,50 @@ def lib():
 
 
 # ---------------------------------------------------------------- C names
-
-def _ref(t):
-    return None if t is None else ctypes.byref(t)
-
+#
+# Structures are passed as they are (ctypes takes their address), pointers as tensors or addresses.
 
 def cross_attn_workspace_size(view):
     n = ctypes.c_size_t()
-    _check(lib().cross_attn_workspace_size(_ref(view), ctypes.byref(n)))
+    _check(lib().cross_attn_workspace_size(view, n))
     return n.value
 
 
 def cross_attn_forward(view, q, k, v, out, stats, ws, ws_bytes, stream=None):
-    _check(lib().cross_attn_forward(_ref(view), _ref(q), _ref(k), _ref(v), _ref(out), _ptr(stats), _ptr(ws), ws_bytes,
-                                    _t._stream(stream)))
+    _check(lib().cross_attn_forward(view, q, k, v, out, _ptr(stats), _ptr(ws), ws_bytes, _t._stream(stream)))
 
 
 def cross_attn_backward_workspace_size(view):
     n = ctypes.c_size_t()
-    _check(lib().cross_attn_backward_workspace_size(_ref(view), ctypes.byref(n)))
+    _check(lib().cross_attn_backward_workspace_size(view, n))
     return n.value
 
 
 def cross_attn_backward(view, q, k, v, out, stats, dout, dq, dk, dv, dbias, ws, ws_bytes, stream=None):
-    _check(lib().cross_attn_backward(_ref(view), _ref(q), _ref(k), _ref(v), _ref(out), _ptr(stats), _ref(dout),
-                                     _ref(dq), _ref(dk), _ref(dv), _ref(dbias), _ptr(ws), ws_bytes,
+    _check(lib().cross_attn_backward(view, q, k, v, out, _ptr(stats), dout, dq, dk, dv, dbias, _ptr(ws), ws_bytes,
                                      _t._stream(stream)))
 
 
 # ---------------------------------------------------------------- torch tensors
 
 def tensor(t):
-    """cross_attn_tensor_t of a [batch][tokens][heads][d] tensor (kept alive by the caller)."""
-    return CrossAttnTensor(_ptr(t), t.stride(0), t.stride(1), t.stride(2))
+    """cross_attn_tensor_t of a [batch][tokens][heads][d] GPU tensor (kept alive by the caller)."""
+    s = t.stride()
+    return CrossAttnTensor(t.data_ptr(), s[0], s[1], s[2])
 
 
 def bias_tensor(t):
-    """cross_attn_bias_t of a [batch or 1][heads or 1][nq][nk] tensor: an axis of length 1 is shared."""
-    return CrossAttnBias(_ptr(t), 0 if t.shape[0] == 1 else t.stride(0), 0 if t.shape[1] == 1 else t.stride(1), t.stride(2))
+    """cross_attn_bias_t of a [batch or 1][heads or 1][nq][nk] GPU tensor: an axis of length 1 is shared."""
+    n, s = t.shape, t.stride()
+    return CrossAttnBias(t.data_ptr(), 0 if n[0] == 1 else s[0], 0 if n[1] == 1 else s[1], s[2])
 
 
 def _heads_tensor(name, t, dtype, device, shape):
     if t.dtype != dtype or t.device != device:
         raise ValueError(f"{name} must be a {dtype} tensor on {device}, not {t.dtype} on {t.device}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    if t.shape[3] > 1 and t.stride(3) != 1:
+    if t.stride(3) != 1 and t.shape[3] > 1:
         raise ValueError(f"{name} must have unit stride along its last axis")
 
 
@@ -116,14 +114,15 @@ def view(q, k, v, bias=None, mask=None, scale=None):
     if q.device.type != "cuda":
         raise ValueError("tensors passed to the library must live on the GPU")
     batch, nq, heads, d = q.shape
-    nk, kv_heads = k.shape[1], k.shape[2]
-    _heads_tensor("q", q, q.dtype, q.device, q.shape)
-    _heads_tensor("k", k, q.dtype, q.device, (batch, nk, kv_heads, d))
-    _heads_tensor("v", v, q.dtype, q.device, (batch, nk, kv_heads, d))
-    w = CrossAttnView(batch, nq, nk, heads, kv_heads, d, _DTYPES[q.dtype], d ** -0.5 if scale is None else scale)
+    _, nk, kv_heads, _ = k.shape
+    dtype, device, keys = q.dtype, q.device, (batch, nk, kv_heads, d)
+    _heads_tensor("q", q, dtype, device, q.shape)
+    _heads_tensor("k", k, dtype, device, keys)
+    _heads_tensor("v", v, dtype, device, keys)
+    w = CrossAttnView(batch, nq, nk, heads, kv_heads, d, _DTYPES[dtype], d ** -0.5 if scale is None else scale)
     if bias is not None:
-        if bias.dtype != q.dtype or bias.device != q.device:
-            raise ValueError(f"bias must be a {q.dtype} tensor on {q.device}")
+        if bias.dtype != dtype or bias.device != device:
+            raise ValueError(f"bias must be a {dtype} tensor on {device}")
         if bias.dim() == 3:
             bias = bias[None]
         if bias.dim() != 4 or bias.shape[0] not in (1, batch) or bias.shape[1] not in (1, heads) or tuple(bias.shape[2:]) != (nq, nk):
@@ -133,14 +132,14 @@ def view(q, k, v, bias=None, mask=None, scale=None):
                 raise ValueError("bias must have unit stride along its last axis")
             w.bias = bias_tensor(bias)
     if mask is not None:
-        if mask.dtype not in (torch.uint8, torch.bool) or mask.device != q.device:
-            raise ValueError(f"mask must be a uint8 or bool tensor on {q.device}")
+        if mask.dtype not in (torch.uint8, torch.bool) or mask.device != device:
+            raise ValueError(f"mask must be a uint8 or bool tensor on {device}")
         if mask.dim() == 1:
             mask = mask[None]
         if mask.dim() != 2 or mask.shape[0] not in (1, batch) or mask.shape[1] != nk or (nk > 1 and mask.stride(1) != 1):
             raise ValueError(f"mask must be [{batch} or 1][{nk}] with unit stride along the keys")
         if mask.numel():
-            w.mask = _ptr(mask)
+            w.mask = mask.data_ptr()
             w.mask_batch = 0 if mask.shape[0] == 1 else mask.stride(0)
     return w
 
@@ -155,7 +154,7 @@ def cross_attention(q, k, v, bias=None, mask=None, scale=None, return_stats=Fals
     [2][batch][heads][nq] float32 statistics that cross_attention_backward takes."""
     w = view(q, k, v, bias, mask, scale)
     with on_stream(q.device, stream) as s:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(q.shape)
         stats = torch.empty((2, w.batch, w.heads, w.nq), dtype=torch.float32, device=q.device) if return_stats else None
         n = cross_attn_workspace_size(w)
         ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
@@ -176,9 +175,8 @@ def cross_attention_backward(q, k, v, out, stats, dout, bias=None, mask=None, sc
     if stats.dtype != torch.float32 or stats.device != q.device or tuple(stats.shape) != (2, w.batch, w.heads, w.nq) or not stats.is_contiguous():
         raise ValueError("stats must be the contiguous [2][batch][heads][nq] float32 tensor of the forward")
     with on_stream(q.device, stream) as s:
-        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if need_kv else None
-        dv = torch.empty(v.shape, dtype=q.dtype, device=q.device) if need_kv else None
+        dq = q.new_empty(q.shape)
+        dk, dv = (k.new_empty(k.shape), v.new_empty(v.shape)) if need_kv else (None, None)
         dbias, grad = None, None
         if bias is not None and need_bias:
             dbias = torch.empty(tuple(bias.shape[:-1]) + (-(-w.nk // 8) * 8,), dtype=q.dtype, device=q.device)[..., :w.nk]

@@ -42,25 +42,27 @@ def lib():
 
 
 def pair_dropout_add(view, x, res, out, stream=None):
-    _check(lib().pair_dropout_add(ctypes.byref(view), _ptr(x), _ptr(res), _ptr(out), _t._stream(stream)))
+    _check(lib().pair_dropout_add(view, _ptr(x), _ptr(res), _ptr(out), _t._stream(stream)))
 
 
 def pair_dropout_backward(view, dout, dx, stream=None):
-    _check(lib().pair_dropout_backward(ctypes.byref(view), _ptr(dout), _ptr(dx), _t._stream(stream)))
+    _check(lib().pair_dropout_backward(view, _ptr(dout), _ptr(dx), _t._stream(stream)))
 
 
 def _rows(name, t, shape=None, device=None):
     """Row stride of a [rows][cols][channels] tensor whose rows are contiguous."""
-    if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ValueError(f"{name} must be [rows][cols][channels]" + (f" = {tuple(shape)}" if shape is not None else "") + f", not {list(t.shape)}")
+    n = t.shape
+    if len(n) != 3 or (shape is not None and n != shape):
+        raise ValueError(f"{name} must be [rows][cols][channels]" + (f" = {tuple(shape)}" if shape is not None else "") + f", not {list(n)}")
     if t.dtype not in _DTYPES:
         raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
-    if t.device.type != "cuda" or (device is not None and t.device != device):
+    if not t.is_cuda or (device is not None and t.device != device):
         raise ValueError(f"{name} must live on {'the GPU' if device is None else device}")
-    r, c, ch = t.shape
-    if t.numel() and ((ch > 1 and t.stride(2) != 1) or (c > 1 and t.stride(1) != ch)):
+    r, c, ch = n
+    sr, sc, sch = t.stride()
+    if ((ch > 1 and sch != 1) or (c > 1 and sc != ch)) and t.numel():
         raise ValueError(f"{name}'s columns and channels must be contiguous")
-    return t.stride(0) if r > 1 else c * ch
+    return sr if r > 1 else c * ch
 
 
 def _view(shape, ld_x, ld_out, x_dtype, out_dtype, p, seed, offset, share, row0, col0, n_cols):
@@ -82,10 +84,11 @@ def dropout_add(x, residual=None, p=0.25, seed=0, offset=0, share="none", row0=0
     dt = residual.dtype if residual is not None else x.dtype if out_dtype is None else _t.TORCH_DTYPE[DTYPE_CODE[out_dtype]]
     with on_stream(x.device, stream) as s:
         if out is None:
-            out = torch.empty(x.shape, dtype=dt, device=x.device)
-        ld = _rows("out", out, x.shape, x.device)
-        if out.dtype != dt:
-            raise ValueError(f"out must be {dt}, not {out.dtype}")
+            out, ld = x.new_empty(x.shape, dtype=dt), x.shape[1] * x.shape[2]
+        else:
+            ld = _rows("out", out, x.shape, x.device)
+            if out.dtype != dt:
+                raise ValueError(f"out must be {dt}, not {out.dtype}")
         if residual is not None and _rows("residual", residual, x.shape, x.device) != ld:
             raise ValueError("residual and out must have the same row stride")
         v = _view(x.shape, ld_x, ld, _DTYPES[x.dtype], _DTYPES[dt], p, seed, offset, share, row0, col0, n_cols)
@@ -100,7 +103,7 @@ def dropout_backward(dout, p=0.25, seed=0, offset=0, share="none", row0=0, col0=
     ld_out = _rows("dout", dout)
     dt = dout.dtype if dtype is None else _t.TORCH_DTYPE[DTYPE_CODE[dtype]]
     with on_stream(dout.device, stream) as s:
-        dx = torch.empty(dout.shape, dtype=dt, device=dout.device) if out is None else out
+        dx = dout.new_empty(dout.shape, dtype=dt) if out is None else out
         ld_x = _rows("out", dx, dout.shape, dout.device)
         if dx.dtype != dt:
             raise ValueError(f"out must be {dt}, not {dx.dtype}")

@@ -180,19 +180,36 @@ def _stream(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
 
-@contextlib.contextmanager
-def on_stream(device, stream):
-    """The device, and on it `stream` (None: the current one) as torch's current stream: what is allocated here
-    belongs to that stream, so that a workspace freed at the end is reused behind the kernels that use it."""
-    with torch.cuda.device(device):
-        if stream is None:
-            yield torch.cuda.current_stream(device).cuda_stream
-            return
-        s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device)
-        if s.device != device:
-            raise ValueError(f"stream of {s.device} for tensors on {device}")
-        with torch.cuda.stream(s):
-            yield s.cuda_stream
+class on_stream:
+    """with on_stream(device, stream) as handle: the device, and on it `stream` (None: its current one; a torch stream
+    or a raw hipStream_t) as torch's current stream.  What is allocated inside belongs to that stream, so that a
+    workspace freed at the end is reused behind the kernels that use it.  Calls on the current device and stream,
+    the usual ones, change nothing and cost next to nothing."""
+    __slots__ = ("device", "stream", "entered")
+
+    def __init__(self, device, stream):
+        self.device, self.stream, self.entered = device, stream, None
+
+    def __enter__(self):
+        index = self.device.index
+        if self.stream is None and torch.cuda.current_device() == index:
+            return torch._C._cuda_getCurrentRawStream(index)
+        with contextlib.ExitStack() as stack:
+            stack.enter_context(torch.cuda.device(index))
+            s = self.stream
+            if s is None:
+                s = torch.cuda.current_stream(index)
+            elif not isinstance(s, torch.cuda.Stream):
+                s = torch.cuda.ExternalStream(int(getattr(s, "cuda_stream", s)), index)
+            if s.device.index != index:
+                raise ValueError(f"stream of {s.device} for tensors on {self.device}")
+            stack.enter_context(torch.cuda.stream(s))
+            self.entered = stack.pop_all()
+        return s.cuda_stream
+
+    def __exit__(self, *exc):
+        if self.entered is not None:
+            self.entered.close()
 
 
 # ---------------------------------------------------------------- C names
