@@ -1242,7 +1242,15 @@ int cross_check(const cross_attn_view_t* v) {
     return TRI_MUL_OK;
 }
 
-int64_t cross_cols(const cross_attn_view_t* v) { return v->nq * (v->heads / v->kv_heads); }
+// Query heads taken together with their key head: all of a group, unless the rows of 32 columns of the bias
+// would not fit one buffer descriptor (2^31 bytes).
+int cross_group(const cross_attn_view_t* v) {
+    const int64_t group = v->heads / v->kv_heads;
+    const __int128 span = (__int128)31 * v->bias.row + (__int128)(group - 1) * v->bias.head + v->nk + 8;
+    return v->bias.data && span * (int64_t)esize(v->dtype) > ((int64_t)1 << 31) ? 1 : (int)group;
+}
+int64_t cross_cols(const cross_attn_view_t* v) { return v->nq * cross_group(v); }
+int cross_col_heads(const cross_attn_view_t* v) { return v->heads / cross_group(v); }
 // Biases of their own (the others share one) and how many entries and heads share each.
 int64_t cross_slots(const cross_attn_view_t* v) { return (v->bias.batch ? v->batch : 1) * (v->bias.head ? v->heads : 1); }
 int64_t cross_shared(const cross_attn_view_t* v) { return (v->bias.batch ? 1 : v->batch) * (v->bias.head ? 1 : v->heads); }
@@ -1281,8 +1289,9 @@ trimul::CrossArgs cross_args(const cross_attn_view_t* v, const cross_attn_tensor
     a.nq = (int)v->nq;
     a.nk = (int)v->nk;
     a.heads = v->heads;
-    a.kv_heads = v->kv_heads;
-    a.group = v->heads / v->kv_heads;
+    a.group = cross_group(v);
+    a.kv_heads = v->heads / a.group;
+    a.key_div = a.kv_heads / v->kv_heads;
     a.d = v->d;
     a.scale = v->scale;
     a.splits = 1;
@@ -1310,7 +1319,7 @@ extern "C" {
 int cross_attn_workspace_size(const cross_attn_view_t* v, size_t* bytes) {
     if (int rc = cross_check(v)) return rc;
     if (!bytes) return fail(TRI_MUL_EINVAL, "null bytes pointer");
-    const trimul::CrossPlan p = trimul::cross_plan(v->batch, v->kv_heads, cross_cols(v), v->nk);
+    const trimul::CrossPlan p = trimul::cross_plan(v->batch, cross_col_heads(v), cross_cols(v), v->nk);
     *bytes = trimul::cross_part_floats(p, v->batch, v->nq, v->heads, v->d) * 4;
     return ok();
 }
@@ -1323,8 +1332,9 @@ int cross_attn_forward(const cross_attn_view_t* v, const cross_attn_tensor_t* q,
     if (int rc = cross_tensor(v, k, "k", v->nk, v->kv_heads, false)) return rc;
     if (int rc = cross_tensor(v, vv, "v", v->nk, v->kv_heads, false)) return rc;
     if (int rc = cross_tensor(v, out, "out", v->nq, v->heads, true)) return rc;
-    const trimul::CrossPlan p = trimul::cross_plan(v->batch, v->kv_heads, cross_cols(v), v->nk);
-    if (v->batch * v->kv_heads > kMaxGroups || v->batch * v->kv_heads * ((cross_cols(v) + p.cols - 1) / p.cols) * p.splits > kMaxGroups)
+    const trimul::CrossPlan p = trimul::cross_plan(v->batch, cross_col_heads(v), cross_cols(v), v->nk);
+    const int64_t bh = v->batch * cross_col_heads(v);
+    if (bh > kMaxGroups || bh * ((cross_cols(v) + p.cols - 1) / p.cols) * p.splits > kMaxGroups)
         return fail(TRI_MUL_EUNSUPPORTED, "too many entries, heads and queries for one call");
     if (int rc = cross_workspace(ws, ws_bytes, trimul::cross_part_floats(p, v->batch, v->nq, v->heads, v->d) * 4)) return rc;
     if (v->batch == 0 || v->nq == 0) return ok();
@@ -1369,7 +1379,7 @@ int cross_attn_backward(const cross_attn_view_t* v, const cross_attn_tensor_t* q
     const bool queries = v->batch > 0 && v->nq > 0;
     if (queries && !stats) return fail(TRI_MUL_EINVAL, "null stats");
     const int splits = cross_bias_splits(v);
-    const int64_t bh = v->batch * v->kv_heads;
+    const int64_t bh = v->batch * cross_col_heads(v);
     if (bh > kMaxGroups || bh * ((cross_cols(v) + 127) / 128) > kMaxGroups || bh * ((v->nk + 127) / 128) > kMaxGroups ||
         (dbias && (cross_slots(v) > kMaxGroups || cross_slots(v) * splits * ((v->nq + 127) / 128) > kMaxGroups ||
                    cross_slots(v) * splits * ((v->nq + 127) / 128) * ((v->nk + 31) / 32) > kMaxGroups)))

@@ -111,75 +111,93 @@ struct Tile {
     // Byte offset of a piece.  Pieces are XOR-swizzled so that both kinds of
     // read are free of bank conflicts: the 16 rows (4 consecutive ones at four
     // distances) whose same piece a row read takes at a time, and the 64-byte
-    // spans of four consecutive rows of a transposing read.
-    static __device__ __forceinline__ uint32_t off(int row, int piece) {
-        const int g = ((row >> 2) & 1) | (row >= KC / 2 ? 2 : 0);
-        const int z = kPieces >= 16 ? (row & 3) << 2 : kPieces == 8 ? ((row >> 1) & 1) << 2 : 0;
-        return (uint32_t)(row * kRowBytes + ((piece ^ z ^ g) << 4));
+    // spans of four consecutive rows of a transposing read.  The swizzle looks
+    // at bits 0 to 2 of the row and at its half of the tile alone, so that a
+    // lane's offsets differ between products by constants added to the row and
+    // constants XORed to the piece.
+    static __host__ __device__ constexpr int twist(int row, int half) {
+        return (((row >> 2) & 1) | (half << 1)) ^
+               (kPieces >= 16 ? (row & 3) << 2 : kPieces == 8 ? ((row >> 1) & 1) << 2 : 0);
     }
-    // The row of this lane's product row (A operand) in the b-th product.
-    static __device__ __forceinline__ int row_of(int lane, int b) {
-        const int l = lane & 31;
-        return (KC / 2) * ((l >> 2) & 1) + 16 * b + 4 * (l >> 3) + (l & 3);
+    static __device__ __forceinline__ uint32_t off(int row, int piece) {
+        return (uint32_t)(row * kRowBytes + ((piece ^ twist(row, row >= KC / 2 ? 1 : 0)) << 4));
+    }
+
+    uint32_t ar, ac;   // this lane's first row read and transposing read
+    __device__ __forceinline__ void init(int lane) {
+        const int l = lane & 31, hi = lane >> 5;
+        // product row l of the b-th product: tile row (KC / 2) ((l / 4) % 2) + 16 b + 4 (l / 8) + l % 4
+        ar = off((KC / 2) * ((l >> 2) & 1) + 4 * (l >> 3) + (l & 3), (sizeof(T) == 2 ? 1 : 2) * hi);
+        if constexpr (sizeof(T) == 2)
+            ac = off((KC / 2) * hi + ((lane >> 2) & 3), 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) + (lane & 1) * 8;
+        else
+            ac = off((KC / 2) * hi, l >> 2) + (l & 3) * 4;
     }
     // A operand: rows of the b-th product, channels 16 s2 ..
-    static __device__ __forceinline__ void rows(const char* t, int lane, int b, int s2, Frag<bf16_t>& f) {
-        f.u = *reinterpret_cast<const uint4*>(t + off(row_of(lane, b), 2 * s2 + (lane >> 5)));
+    __device__ __forceinline__ void rows(const char* t, int b, int s2, Frag<bf16_t>& f) const {
+        f.u = *reinterpret_cast<const uint4*>(t + (ar ^ (s2 << 5)) + b * 16 * kRowBytes);
     }
-    static __device__ __forceinline__ void rows(const char* t, int lane, int b, int s2, Frag<float>& f) {
-        const int r = row_of(lane, b), p = 4 * s2 + 2 * (lane >> 5);
-        const float4 x = *reinterpret_cast<const float4*>(t + off(r, p));
-        const float4 y = *reinterpret_cast<const float4*>(t + off(r, p + 1));
+    __device__ __forceinline__ void rows(const char* t, int b, int s2, Frag<float>& f) const {
+        const float4 x = *reinterpret_cast<const float4*>(t + (ar ^ (s2 << 6)) + b * 16 * kRowBytes);
+        const float4 y = *reinterpret_cast<const float4*>(t + (ar ^ (s2 << 6) ^ 16) + b * 16 * kRowBytes);
         const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
         for (int e = 0; e < 8; ++e) f.v[e] = v[e];
     }
     // A operand, transposed: channels 32 db + lane % 32, reduction over the tile rows that
-    // registers 8 t .. of the b-th product stand for.
-    static __device__ __forceinline__ void cols(const char* t, int lane, int b, int tt, int db, Frag<bf16_t>& f) {
-        const int r = (KC / 2) * (lane >> 5) + 16 * b + 8 * tt + ((lane >> 2) & 3);
-        const int p = 4 * db + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1), s = (lane & 1) * 8;
-        const uint2 x = lds_tr4(t + off(r, p) + s), y = lds_tr4(t + off(r + 4, p) + s);
+    // registers 8 tt .. of the b-th product stand for.
+    __device__ __forceinline__ void cols(const char* t, int b, int tt, int db, Frag<bf16_t>& f) const {
+        const char* p = t + (16 * b + 8 * tt) * kRowBytes;
+        const uint2 x = lds_tr4(p + (ac ^ (db << 6))), y = lds_tr4(p + 4 * kRowBytes + (ac ^ (db << 6) ^ 16));
         f.u = make_uint4(x.x, x.y, y.x, y.y);
     }
-    static __device__ __forceinline__ void cols(const char* t, int lane, int b, int tt, int db, Frag<float>& f) {
-        const int r = (KC / 2) * (lane >> 5) + 16 * b + 8 * tt, c = 32 * db + (lane & 31);
+    __device__ __forceinline__ void cols(const char* t, int b, int tt, int db, Frag<float>& f) const {
+        const char* p = t + (16 * b + 8 * tt) * kRowBytes;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f.v[e] = *reinterpret_cast<const float*>(t + off(r + e, c >> 2) + (c & 3) * 4);
+        for (int e = 0; e < 8; ++e)
+            f.v[e] = *reinterpret_cast<const float*>(p + e * kRowBytes + (ac ^ (db << 7) ^ (twist(e, 0) << 4)));
     }
 };
 
-// The part of a tile that one of NT threads brings in: pieces t + NT i.  Rows
-// past the last one and pieces past d channels repeat valid ones (the first
-// are masked by the caller, the second meet zeros of the other operand or
-// give channels that are not written).
+// The part of a tile that one of NT threads brings in: pieces t + NT i of its
+// rows, through a buffer descriptor of the rows that exist (scalar registers:
+// the base moves from chunk to chunk, a thread's offsets stay).  Rows past the
+// last one and pieces past d channels read zero.
 template <typename T, int DP, int KC, int NT>
 struct Part {
     using TL = Tile<T, DP, KC>;
-    static constexpr int kN = KC * TL::kPieces / NT;
-    static_assert(KC * TL::kPieces % NT == 0, "whole pieces per thread");
+    static constexpr int kAll = KC * TL::kPieces, kN = (kAll + NT - 1) / NT;
+    static_assert(kAll % NT == 0 || kAll < NT, "whole pieces per thread");
+    uint32_t off[kN];
     uint4 p[kN];
 
     static __device__ __forceinline__ int row(int t, int i) { return (t + i * NT) / TL::kPieces; }
-    // rows r0 + row of a [n][stride] tensor, n > r0
-    __device__ __forceinline__ void load(const T* base, int64_t stride, int r0, int n, int d, int t) {
-        const T* first = base + (int64_t)r0 * stride;
-        const int last = n - 1 - r0;
+    static __device__ __forceinline__ int piece(int t, int i) { return (t + i * NT) % TL::kPieces; }
+    static __device__ __forceinline__ bool mine(int t) { return kAll >= NT || t < kAll; }
+    __device__ __forceinline__ void init(int64_t stride, int d, int t) {
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const int piece = (t + i * NT) % TL::kPieces;
-            const int r = min(row(t, i), last), c = piece * TL::kPer < d ? piece * TL::kPer : 0;
-            p[i] = *reinterpret_cast<const uint4*>(first + (uint32_t)(r * (int)stride + c));
-        }
+        for (int i = 0; i < kN; ++i)
+            off[i] = mine(t) && piece(t, i) * TL::kPer < d
+                         ? (uint32_t)row(t, i) * (uint32_t)(stride * (int)sizeof(T)) + 16 * piece(t, i)
+                         : 0xfffffff0u;
+    }
+    // rows r0 .. of n rows at base; no row left: nothing is read
+    __device__ __forceinline__ void load(const T* base, int64_t stride, int r0, int n, int d) {
+        const int rows = min(n - r0, KC);
+        const auto r = make_rsrc(base + (int64_t)r0 * stride,
+                                 rows > 0 ? (uint32_t)((rows - 1) * (uint32_t)stride + d) * (uint32_t)sizeof(T) : 0u);
+#pragma unroll
+        for (int i = 0; i < kN; ++i) p[i] = buf_load16(r, off[i]);
     }
     // present: bit r of the chunk's row r; rows without theirs become zero
     __device__ __forceinline__ void stage(char* tile, int t, bool some_absent, uint64_t present) const {
+        if (!mine(t)) return;
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
             const int r = row(t, i);
             uint4 x = p[i];
             if (some_absent && !((present >> r) & 1)) x = make_uint4(0, 0, 0, 0);
-            *reinterpret_cast<uint4*>(tile + TL::off(r, (t + i * NT) % TL::kPieces)) = x;
+            *reinterpret_cast<uint4*>(tile + TL::off(r, piece(t, i))) = x;
         }
     }
 };
@@ -187,11 +205,12 @@ struct Part {
 // Bits of the keys [k0, k0 + KC) that are in range and present, the same in every lane of the wave.
 struct KeyByte {
     uint32_t m;
+    // (loads without branches: the compiler then knows how many are in flight)
     __device__ __forceinline__ void load(const uint8_t* mask, int k0, int nk, int lane) {
-        m = mask ? mask[min(k0 + lane, nk - 1)] : 1u;
+        m = __builtin_amdgcn_raw_buffer_load_b8(make_rsrc(mask, mask ? (uint32_t)nk : 0u), k0 + lane, 0, 0);
     }
-    __device__ __forceinline__ uint64_t bits(int k0, int kend, int lane) const {
-        return __ballot(k0 + lane < kend && m != 0);
+    __device__ __forceinline__ uint64_t bits(const uint8_t* mask, int k0, int kend, int lane) const {
+        return __ballot(k0 + lane < kend && (m != 0 || mask == nullptr));
     }
 };
 
@@ -210,18 +229,33 @@ __device__ __forceinline__ float4 bf4(uint32_t lo, uint32_t hi) {
                        __uint_as_float(hi & 0xffff0000u));
 }
 
-// The bias of one lane's KC / 2 consecutive keys of its query.
+// The bias of one lane's KC / 2 consecutive keys of its query, through a
+// descriptor of the rows of its wave's 32 columns: from the first one's to the
+// end of the last one's keys (rounded up to 8: nothing behind that is read; a
+// piece past the keys of another row reads whatever follows it).
 template <typename T, int KC>
 struct BiasRow {
     static constexpr int kPer = 16 / (int)sizeof(T), kN = KC / 2 / kPer;
+    const T* first;      // uniform
+    uint32_t span, off;  // bytes; off: this lane's row, first key of its half
     uint4 p[kN];
-    // row: the query's bias; keys k .. ; pieces that start past the last key repeat the row's first
-    __device__ __forceinline__ void load(const T* row, int k, int nk) {
+    // columns c0 .. c1 (uniform) of key head hk, this lane's query and head
+    __device__ __forceinline__ void init(const CrossArgs& a, int64_t b, int hk, int c0, int c1, int qi, int h, int hi) {
+        const int q0 = c0 / a.group, q1 = c1 / a.group;
+        first = (const T*)a.bias.data + b * a.bias.batch + (int64_t)(hk * a.group) * a.bias.head + (int64_t)q0 * a.bias.row;
+        span = (uint32_t)((q1 - q0) * a.bias.row + (a.group - 1) * a.bias.head + ((a.nk + 7) & ~7)) * (uint32_t)sizeof(T);
+        off = (uint32_t)((qi - q0) * a.bias.row + (h - hk * a.group) * a.bias.head + (KC / 2) * hi) * (uint32_t)sizeof(T);
+    }
+    // queries q0 .. q1 (uniform) of one head, this lane's query
+    __device__ __forceinline__ void init(const CrossArgs& a, int64_t b, int h, int q0, int q1, int qi, int hi) {
+        first = (const T*)a.bias.data + b * a.bias.batch + (int64_t)h * a.bias.head + (int64_t)q0 * a.bias.row;
+        span = (uint32_t)((q1 - q0) * a.bias.row + ((a.nk + 7) & ~7)) * (uint32_t)sizeof(T);
+        off = (uint32_t)((qi - q0) * a.bias.row + (KC / 2) * hi) * (uint32_t)sizeof(T);
+    }
+    __device__ __forceinline__ void load(int k0, int nk) {
+        const auto r = make_rsrc(first + k0, k0 < nk ? span - (uint32_t)k0 * (uint32_t)sizeof(T) : 0u);
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const int c = k + i * kPer;
-            p[i] = *reinterpret_cast<const uint4*>(row + (c < nk ? c : 0));
-        }
+        for (int i = 0; i < kN; ++i) p[i] = buf_load16(r, off + 16 * i);
     }
     // values 16 b + 4 a .. + 3
     __device__ __forceinline__ float4 get(int b, int a) const {

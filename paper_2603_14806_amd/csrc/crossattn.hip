@@ -18,16 +18,23 @@ __device__ __forceinline__ void store4(T* p, float a, float b, float c, float d)
     else *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
 }
 
+// Waves per SIMD that the registers are limited for.
+template <typename T, int DP, int WK>
+constexpr int forward_waves() {
+    return DP == 32 ? (WK == 1 || sizeof(T) == 2 ? 4 : 3) : DP == 64 ? (WK == 1 ? 3 : 2) : (sizeof(T) == 4 && WK == 4 ? 1 : 2);
+}
+
 // WK = 1: a wave takes 32 columns and every chunk, the chunks staged by all
 // four waves (double-buffered).  WK = 4: 32 columns, wave w takes chunks w,
 // w + 4, ..., stages them for itself, and the four results are merged at the end.
 template <typename T, int DP, int KC, int WK, bool BIAS>
-__global__ __launch_bounds__(256) void k_cross_forward(const CrossArgs a, int ctiles) {
+__global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_forward(const CrossArgs a, int ctiles) {
     using TL = Tile<T, DP, KC>;
     constexpr int NT = 256 / WK, NB = KC / 32, ND = DP / 32, NS = DP / 16;
     __shared__ __align__(16) char mem[(WK == 1 ? 2 : 4) * 2 * TL::kBytes];
     __shared__ float red[WK == 1 ? 1 : 2][WK == 1 ? 1 : 4][32];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, ql = lane & 31, hi = lane >> 5;
+    const int lane = threadIdx.x & 63, ql = lane & 31, hi = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int t = WK == 1 ? threadIdx.x : lane;
 
     int64_t blk = blockIdx.x;
@@ -50,9 +57,8 @@ __global__ __launch_bounds__(256) void k_cross_forward(const CrossArgs a, int ct
 #pragma unroll
         for (int s = 0; s < NS; ++s) load_row(row, s, hi, a.d, qf[s]);
     }
-    const T* kb = (const T*)a.k.data + b * a.k.batch + hk * a.k.head;
-    const T* vb = (const T*)a.v.data + b * a.v.batch + hk * a.v.head;
-    const T* brow = BIAS ? (const T*)a.bias.data + b * a.bias.batch + h * a.bias.head + (int64_t)qi * a.bias.row : nullptr;
+    const T* kb = (const T*)a.k.data + b * a.k.batch + hk / a.key_div * a.k.head;
+    const T* vb = (const T*)a.v.data + b * a.v.batch + hk / a.key_div * a.v.head;
     const uint8_t* mask = a.mask ? a.mask + b * a.mask_batch : nullptr;
     const int ks = split * a.split_keys, ke = min(a.nk, ks + a.split_keys);
     const int nchunks = (ke - ks + KC - 1) / KC;
@@ -66,25 +72,30 @@ __global__ __launch_bounds__(256) void k_cross_forward(const CrossArgs a, int ct
         for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
     float M = -INFINITY, L = 0.f;
 
+    TL tl;
+    tl.init(lane);
     Part<T, DP, KC, NT> kp, vp;
     KeyByte kbyte;
     BiasRow<T, KC> bp;
+    kp.init(a.k.token, a.d, t);
+    vp.init(a.v.token, a.d, t);
     auto load = [&](int c) {
         const int k0 = ks + c * KC;
-        kp.load(kb, a.k.token, k0, a.nk, a.d, t);
-        vp.load(vb, a.v.token, k0, a.nk, a.d, t);
+        kp.load(kb, a.k.token, k0, a.nk, a.d);
+        vp.load(vb, a.v.token, k0, a.nk, a.d);
         kbyte.load(mask, k0, a.nk, lane);
     };
     const int c0 = WK == 1 ? 0 : w;
-    if (c0 < nchunks) {
-        load(c0);
-        if (BIAS) bp.load(brow, ks + c0 * KC + (KC / 2) * hi, a.nk);
+    load(c0);
+    if (BIAS) {
+        bp.init(a, b, hk, min(cw, ncols - 1), min(cw + 31, ncols - 1), qi, h, hi);
+        bp.load(ks + c0 * KC, a.nk);
     }
     for (int c = c0; c < nchunks; c += WK) {
         char* kt = mem + (WK == 1 ? (c & 1) : w) * 2 * TL::kBytes;
         char* vt = kt + TL::kBytes;
         const int k0 = ks + c * KC;
-        uint64_t bits = kbyte.bits(k0, ke, lane);
+        uint64_t bits = kbyte.bits(mask, k0, ke, lane);
         if (KC == 32) bits &= 0xffffffffull;
         const bool some = bits != (KC == 64 ? ~0ull : 0xffffffffull);
         if (WK > 1) {   // a wave's LDS operations run in order; only the compiler has to be kept from moving them
@@ -93,7 +104,7 @@ __global__ __launch_bounds__(256) void k_cross_forward(const CrossArgs a, int ct
         }
         kp.stage(kt, t, some, bits);
         vp.stage(vt, t, some, bits);
-        if (c + WK < nchunks) load(c + WK);
+        load(c + WK);
         if (WK == 1) {
             __syncthreads();
         } else {
@@ -109,33 +120,34 @@ __global__ __launch_bounds__(256) void k_cross_forward(const CrossArgs a, int ct
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
                     Frag<T> f;
-                    TL::rows(kt, lane, n, i, f);
+                    tl.rows(kt, n, i, f);
                     s[n] = mma(f, qf[i], s[n]);
                 }
             }
-            float cm = -INFINITY;
-            const uint32_t mine = (uint32_t)(bits >> ((KC / 2) * hi));
-            auto scores = [&](bool masked) {
+            if (BIAS) {
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        float4 bv;
-                        if (BIAS) bv = bp.get(n, g);
+                        const float4 bv = bp.get(n, g);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float x = s[n][4 * g + e];
-                            if (BIAS) x = __builtin_fmaf(x, a.scale, f4_get(bv, e));
-                            if (masked) x = (mine >> (16 * n + 4 * g + e)) & 1 ? x : -INFINITY;
-                            s[n][4 * g + e] = x;
-                        }
-                        cm = fmaxf(fmaxf(cm, s[n][4 * g]), s[n][4 * g + 1]);
-                        cm = fmaxf(fmaxf(cm, s[n][4 * g + 2]), s[n][4 * g + 3]);
+                        for (int e = 0; e < 4; ++e)
+                            s[n][4 * g + e] = __builtin_fmaf(s[n][4 * g + e], a.scale, f4_get(bv, e));
                     }
-            };
-            if (some) scores(true);
-            else scores(false);
-            if (BIAS && c + WK < nchunks) bp.load(brow, k0 + WK * KC + (KC / 2) * hi, a.nk);
+                bp.load(k0 + WK * KC, a.nk);
+            }
+            if (some) {
+                const uint32_t mine = (uint32_t)(bits >> ((KC / 2) * hi));
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[n][r] = (mine >> (16 * n + r)) & 1 ? s[n][r] : -INFINITY;
+            }
+            float cm = -INFINITY;
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; r += 2) cm = fmaxf(fmaxf(cm, s[n][r]), s[n][r + 1]);
             cm = fmaxf(cm, xor32(cm));
             const float Mn = fmaxf(M, cm);
             const float Ms = Mn == -INFINITY ? 0.f : Mn;      // no key yet: every x is -inf and every weight 0
@@ -146,25 +158,22 @@ __global__ __launch_bounds__(256) void k_cross_forward(const CrossArgs a, int ct
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
             M = Mn;
-            const float nsh = -Ms * coef;
-            float ps = 0.f;
-            if (__any(!(fabsf(nsh) <= kFmaMax))) {
+            float nsh = -Ms * coef;
+            if (__any(!(fabsf(nsh) <= kFmaMax))) {            // take the difference first
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        s[n][r] = __builtin_amdgcn_exp2f((s[n][r] - Ms) * coef);
-                        ps += s[n][r];
-                    }
-            } else {
-#pragma unroll
-                for (int n = 0; n < NB; ++n)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        s[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], coef, nsh));
-                        ps += s[n][r];
-                    }
+                    for (int r = 0; r < 16; ++r) s[n][r] -= Ms;
+                nsh = 0.f;
             }
+            float ps = 0.f;
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], coef, nsh));
+                    ps += s[n][r];
+                }
             L += ps;
 #pragma unroll
             for (int n = 0; n < NB; ++n)
@@ -175,18 +184,18 @@ __global__ __launch_bounds__(256) void k_cross_forward(const CrossArgs a, int ct
 #pragma unroll
                     for (int i = 0; i < ND; ++i) {
                         Frag<T> vf;
-                        TL::cols(vt, lane, n, tt, i, vf);
+                        tl.cols(vt, n, tt, i, vf);
                         o[i] = mma(vf, pf, o[i]);
                     }
                 }
-        } else if (BIAS && c + WK < nchunks) {
-            bp.load(brow, k0 + WK * KC + (KC / 2) * hi, a.nk);
+        } else if (BIAS) {
+            bp.load(k0 + WK * KC, a.nk);
         }
     }
 
     float Lt = L + xor32(L);
     constexpr int NG = ND * 4;              // groups of four channels a lane holds
-    int g0 = 0, g1 = NG;
+    int g0 = 0;
     if constexpr (WK > 1) {
         float* buf = reinterpret_cast<float*>(mem);
         if (!hi) {
@@ -207,8 +216,7 @@ __global__ __launch_bounds__(256) void k_cross_forward(const CrossArgs a, int ct
         __syncthreads();
         M = Mn;
         Lt = sum;
-        g0 = w * ND;
-        g1 = g0 + ND;                       // each wave adds and writes a quarter of the channels
+        g0 = w * ND;                        // each wave adds and writes a quarter of the channels
 #pragma unroll
         for (int j = 0; j < ND; ++j)
 #pragma unroll

@@ -33,26 +33,47 @@ struct RowStat {
     __device__ __forceinline__ bool far() const { return !(fabsf(M * kLog2e) <= kFmaMax); }
 };
 
-// P of one score: s = q . k, bv its bias.
-template <bool BIAS, bool FAR>
-__device__ __forceinline__ float weight(float s, float bv, float scale, float coef, float M, float n2, float sh) {
-    if (FAR) {
-        const float x = BIAS ? __builtin_fmaf(s, scale, bv) : s * scale;
-        return __builtin_amdgcn_exp2f(__builtin_fmaf(x - M, kLog2e, n2));
-    }
-    const float x = BIAS ? __builtin_fmaf(s, scale, bv) : s;
-    return __builtin_amdgcn_exp2f(__builtin_fmaf(x, coef, sh));
+// x = q . k scale + bias of a lane's keys.
+template <typename T, int KC>
+__device__ __forceinline__ void add_bias(f32x16_t (&s)[KC / 32], const BiasRow<T, KC>& bp, float scale) {
+#pragma unroll
+    for (int n = 0; n < KC / 32; ++n)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float4 bv = bp.get(n, g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[n][4 * g + e] = __builtin_fmaf(s[n][4 * g + e], scale, f4_get(bv, e));
+        }
+}
+// Absent keys (their bit of `mine` is 0): x = -inf.
+template <int NB>
+__device__ __forceinline__ void drop_absent(f32x16_t (&s)[NB], uint32_t mine) {
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[n][r] = (mine >> (16 * n + r)) & 1 ? s[n][r] : -INFINITY;
+}
+// x - M where M is large.
+template <int NB>
+__device__ __forceinline__ void take_from(f32x16_t (&s)[NB], float scale, float M) {
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[n][r] = __builtin_fmaf(s[n][r], scale, -M);
 }
 
 // ------------------------------------------------------------------ queries: dq, D
 //
 // The forward's layout (lane: one column, registers: keys), 32 columns a wave.
+template <typename T, int DP>
+constexpr int q_waves() { return DP == 32 ? 3 : DP == 64 || sizeof(T) == 2 ? 2 : 1; }
+
 template <typename T, int DP, int KC, bool BIAS>
-__global__ __launch_bounds__(256) void k_cross_backward_q(const CrossArgs a, int ctiles) {
+__global__ __launch_bounds__(256, (q_waves<T, DP>())) void k_cross_backward_q(const CrossArgs a, int ctiles) {
     using TL = Tile<T, DP, KC>;
     constexpr int NB = KC / 32, ND = DP / 32, NS = DP / 16;
     __shared__ __align__(16) char mem[2 * 2 * TL::kBytes];
-    const int t = threadIdx.x, lane = t & 63, w = t >> 6, ql = lane & 31, hi = lane >> 5;
+    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), ql = lane & 31, hi = lane >> 5;
 
     int64_t blk = blockIdx.x;
     const int ct = (int)(blk % ctiles);
@@ -86,9 +107,8 @@ __global__ __launch_bounds__(256) void k_cross_backward_q(const CrossArgs a, int
     st.set(a.stats[row], a.stats[a.batch * a.heads * a.nq + row]);
     const bool far = __any(st.far());
     const float coef = BIAS ? kLog2e : a.scale * kLog2e;
-    const T* kb = (const T*)a.k.data + b * a.k.batch + hk * a.k.head;
-    const T* vb = (const T*)a.v.data + b * a.v.batch + hk * a.v.head;
-    const T* brow = BIAS ? (const T*)a.bias.data + b * a.bias.batch + h * a.bias.head + (int64_t)qi * a.bias.row : nullptr;
+    const T* kb = (const T*)a.k.data + b * a.k.batch + hk / a.key_div * a.k.head;
+    const T* vb = (const T*)a.v.data + b * a.v.batch + hk / a.key_div * a.v.head;
     const uint8_t* mask = a.mask ? a.mask + b * a.mask_batch : nullptr;
     const int nchunks = (a.nk + KC - 1) / KC;
 
@@ -98,30 +118,34 @@ __global__ __launch_bounds__(256) void k_cross_backward_q(const CrossArgs a, int
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
 
+    TL tl;
+    tl.init(lane);
     Part<T, DP, KC, 256> kp, vp;
     KeyByte kbyte;
     BiasRow<T, KC> bp;
+    kp.init(a.k.token, a.d, t);
+    vp.init(a.v.token, a.d, t);
     auto load = [&](int c) {
-        kp.load(kb, a.k.token, c * KC, a.nk, a.d, t);
-        vp.load(vb, a.v.token, c * KC, a.nk, a.d, t);
+        kp.load(kb, a.k.token, c * KC, a.nk, a.d);
+        vp.load(vb, a.v.token, c * KC, a.nk, a.d);
         kbyte.load(mask, c * KC, a.nk, lane);
     };
-    if (nchunks) {
-        load(0);
-        if (BIAS) bp.load(brow, (KC / 2) * hi, a.nk);
+    load(0);
+    if (BIAS) {
+        bp.init(a, b, hk, min(cw, ncols - 1), min(cw + 31, ncols - 1), qi, h, hi);
+        bp.load(0, a.nk);
     }
     for (int c = 0; c < nchunks; ++c) {
         char* kt = mem + (c & 1) * 2 * TL::kBytes;
         char* vt = kt + TL::kBytes;
-        uint64_t bits = kbyte.bits(c * KC, a.nk, lane);
+        uint64_t bits = kbyte.bits(mask, c * KC, a.nk, lane);
         if (KC == 32) bits &= 0xffffffffull;
         const bool some = bits != (KC == 64 ? ~0ull : 0xffffffffull);
         kp.stage(kt, t, some, bits);
         vp.stage(vt, t, some, bits);
-        if (c + 1 < nchunks) load(c + 1);
+        load(c + 1);
         __syncthreads();
         if (bits != 0 && wave_live) {
-            const uint32_t mine = (uint32_t)(bits >> ((KC / 2) * hi));
             f32x16_t s[NB], dp[NB];
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
@@ -130,36 +154,32 @@ __global__ __launch_bounds__(256) void k_cross_backward_q(const CrossArgs a, int
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
                     Frag<T> f;
-                    TL::rows(kt, lane, n, i, f);
+                    tl.rows(kt, n, i, f);
                     s[n] = mma(f, qf[i], s[n]);
                 }
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
                     Frag<T> f;
-                    TL::rows(vt, lane, n, i, f);
+                    tl.rows(vt, n, i, f);
                     dp[n] = mma(f, gf[i], dp[n]);
                 }
             }
-            auto grads = [&](auto masked, auto isfar) {
+            if (BIAS) {
+                add_bias<T, KC>(s, bp, a.scale);
+                bp.load((c + 1) * KC, a.nk);
+            }
+            if (some) drop_absent<NB>(s, (uint32_t)(bits >> ((KC / 2) * hi)));
+            float cf = coef, sh = st.sh;
+            if (far) {
+                take_from<NB>(s, BIAS ? 1.f : a.scale, st.M);
+                cf = kLog2e;
+                sh = st.n2;
+            }
 #pragma unroll
-                for (int n = 0; n < NB; ++n)
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        float4 bv = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (BIAS) bv = bp.get(n, g);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int r = 4 * g + e;
-                            float p = weight<BIAS, decltype(isfar)::value>(s[n][r], f4_get(bv, e), a.scale, coef, st.M, st.n2, st.sh);
-                            if (decltype(masked)::value) p = (mine >> (16 * n + r)) & 1 ? p : 0.f;
-                            s[n][r] = p * (dp[n][r] - D);
-                        }
-                    }
-            };
-            if (far) grads(std::true_type{}, std::true_type{});
-            else if (some) grads(std::true_type{}, std::false_type{});
-            else grads(std::false_type{}, std::false_type{});
-            if (BIAS && c + 1 < nchunks) bp.load(brow, (c + 1) * KC + (KC / 2) * hi, a.nk);
+                for (int r = 0; r < 16; ++r)
+                    s[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], cf, sh)) * (dp[n][r] - D);
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -169,12 +189,12 @@ __global__ __launch_bounds__(256) void k_cross_backward_q(const CrossArgs a, int
 #pragma unroll
                     for (int i = 0; i < ND; ++i) {
                         Frag<T> kf;
-                        TL::cols(kt, lane, n, tt, i, kf);
+                        tl.cols(kt, n, tt, i, kf);
                         acc[i] = mma(kf, pf, acc[i]);
                     }
                 }
-        } else if (BIAS && c + 1 < nchunks) {
-            bp.load(brow, (c + 1) * KC + (KC / 2) * hi, a.nk);
+        } else if (BIAS) {
+            bp.load((c + 1) * KC, a.nk);
         }
     }
     if (!valid) return;
@@ -191,31 +211,36 @@ __global__ __launch_bounds__(256) void k_cross_backward_q(const CrossArgs a, int
 // ------------------------------------------------------------------ keys: dk, dv
 //
 // Lane: one key (K and V as B operands in registers), registers: the queries of
-// a chunk of QC columns, whose q and dout pass through LDS; 32 keys a wave.
+// a chunk of QC (of one head after the other), whose q and dout pass through
+// LDS; 32 keys a wave.
 // The bias tile of a chunk passes through LDS too and is read transposed
 // (four queries of one key at a time).
+template <typename T, int DP>
+constexpr int kv_waves() { return DP == 32 ? (sizeof(T) == 2 ? 3 : 2) : DP == 64 && sizeof(T) == 2 ? 2 : 1; }
+
 template <typename T, int DP, int QC, bool BIAS>
-__global__ __launch_bounds__(256) void k_cross_backward_kv(const CrossArgs a, int ktiles) {
+__global__ __launch_bounds__(256, (kv_waves<T, DP>())) void k_cross_backward_kv(const CrossArgs a, int ktiles) {
     using TL = Tile<T, DP, QC>;
-    constexpr int NB = QC / 32, ND = DP / 32, NS = DP / 16, kN = QC * TL::kPieces / 256;
+    constexpr int NB = QC / 32, ND = DP / 32, NS = DP / 16;
     constexpr int kBRow = 128 * (int)sizeof(T) + (sizeof(T) == 2 ? 64 : 16);   // spreads four rows over the banks
     constexpr int kBPieces = 128 * (int)sizeof(T) / 16, kBN = QC * kBPieces / 256;
     __shared__ __align__(16) char mem[2 * 2 * TL::kBytes];
     __shared__ __align__(16) char bmem[BIAS ? 2 * QC * kBRow : 16];
     __shared__ __align__(16) float stat[2][4][QC];             // M, n2, sh, D of a chunk's columns
-    const int t = threadIdx.x, lane = t & 63, w = t >> 6, kl = lane & 31, hi = lane >> 5;
+    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), kl = lane & 31, hi = lane >> 5;
 
     int64_t blk = blockIdx.x;
     const int kt_ = (int)(blk % ktiles);
     blk /= ktiles;
-    const int hk = (int)(blk % a.kv_heads);
-    const int64_t b = blk / a.kv_heads;
+    const int kv_heads = a.kv_heads / a.key_div, group = a.group * a.key_div;
+    const int hk = (int)(blk % kv_heads);
+    const int64_t b = blk / kv_heads;
     const int key0 = kt_ * 128, key = key0 + 32 * w + kl;
     const bool valid = key < a.nk, wave_live = key0 + 32 * w < a.nk;
     const int kc = min(key, a.nk - 1);
     const bool present = valid && (!a.mask || a.mask[b * a.mask_batch + kc] != 0);
     const bool all_present = __all(present);
-    const int ncols = a.nq * a.group, nchunks = (ncols + QC - 1) / QC;
+    const int per_head = (a.nq + QC - 1) / QC, nchunks = per_head * group;
     const float coef = BIAS ? kLog2e : a.scale * kLog2e;
 
     Frag<T> kf[NS], vf[NS];
@@ -226,6 +251,10 @@ __global__ __launch_bounds__(256) void k_cross_backward_kv(const CrossArgs a, in
         for (int s = 0; s < NS; ++s) {
             load_row(kr, s, hi, a.d, kf[s]);
             load_row(vr, s, hi, a.d, vf[s]);
+            if (!present) {                                    // may hold anything
+                kf[s].zero();
+                vf[s].zero();
+            }
         }
     }
     f32x16_t dk[ND], dv[ND];
@@ -234,53 +263,52 @@ __global__ __launch_bounds__(256) void k_cross_backward_kv(const CrossArgs a, in
 #pragma unroll
         for (int r = 0; r < 16; ++r) dk[i][r] = dv[i][r] = 0.f;
 
-    uint4 qp[kN], gp[kN], bp[BIAS ? kBN : 1];
-    float sm = 0.f, sl = 0.f, sd = 0.f;
-    const T* qb = (const T*)a.q.data + b * a.q.batch;
-    const T* gb = (const T*)a.dout.data + b * a.dout.batch;
-    const int64_t rows = a.batch * a.heads * a.nq;
-    auto split_col = [&](int c, int& qi, int& h) {
-        qi = a.group == 1 ? c : c / a.group;
-        h = hk * a.group + (c - qi * a.group);
-    };
-    auto load = [&](int c) {
-        int qi, h;
+    TL tl;
+    tl.init(lane);
+    Part<T, DP, QC, 256> qp, gp;
+    uint4 bp[BIAS ? kBN : 1];
+    uint32_t boff[BIAS ? kBN : 1];
+    qp.init(a.q.token, a.d, t);
+    gp.init(a.dout.token, a.d, t);
+    if (BIAS)
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const int u = t + 256 * i, piece = u % TL::kPieces;
-            split_col(min(c * QC + u / TL::kPieces, ncols - 1), qi, h);
-            const int ch = piece * TL::kPer < a.d ? piece * TL::kPer : 0;
-            qp[i] = *reinterpret_cast<const uint4*>(qb + (int64_t)qi * a.q.token + h * a.q.head + ch);
-            gp[i] = *reinterpret_cast<const uint4*>(gb + (int64_t)qi * a.dout.token + h * a.dout.head + ch);
+        for (int i = 0; i < kBN; ++i) {
+            const int u = t + 256 * i, k = key0 + (u % kBPieces) * TL::kPer;
+            boff[i] = k < a.nk ? (uint32_t)(u / kBPieces) * (uint32_t)(a.bias.row * (int)sizeof(T)) + 16 * (u % kBPieces) : 0xfffffff0u;
         }
-        if (BIAS)
+    float sm = 0.f, sl = 0.f, sd = 0.f;
+    const int64_t rows = a.batch * a.heads * a.nq;
+    int next_h = hk * group, next_q = 0;                      // the chunk that load() takes
+    auto load = [&]() {
+        const int left = next_h < (hk + 1) * group ? a.nq : 0;  // behind the last chunk nothing is read
+        const int h = min(next_h, (hk + 1) * group - 1);
+        qp.load((const T*)a.q.data + b * a.q.batch + h * a.q.head, a.q.token, next_q, left, a.d);
+        gp.load((const T*)a.dout.data + b * a.dout.batch + h * a.dout.head, a.dout.token, next_q, left, a.d);
+        if (BIAS) {
+            const auto r = make_rsrc((const T*)a.bias.data + b * a.bias.batch + h * a.bias.head + (int64_t)next_q * a.bias.row + key0,
+                                     left ? (uint32_t)((min(left - next_q, QC) - 1) * (uint32_t)a.bias.row + min(128, (a.nk - key0 + 7) & ~7)) * (uint32_t)sizeof(T) : 0u);
 #pragma unroll
-            for (int i = 0; i < kBN; ++i) {
-                const int u = t + 256 * i, k = key0 + (u % kBPieces) * TL::kPer;
-                split_col(min(c * QC + u / kBPieces, ncols - 1), qi, h);
-                bp[i] = *reinterpret_cast<const uint4*>((const T*)a.bias.data + b * a.bias.batch + h * a.bias.head +
-                                                        (int64_t)qi * a.bias.row + (k < a.nk ? k : 0));
-            }
-        const int cc = c * QC + (lane & (QC - 1));
-        split_col(min(cc, ncols - 1), qi, h);
-        const int64_t row = (b * a.heads + h) * a.nq + qi;
+            for (int i = 0; i < kBN; ++i) bp[i] = buf_load16(r, boff[i]);
+        }
+        const int qi = next_q + (lane & (QC - 1));
+        const int64_t row = (b * a.heads + h) * a.nq + min(qi, a.nq - 1);
         sm = a.stats[row];
-        sl = cc < ncols ? a.stats[rows + row] : 0.f;           // columns past the last have weight 0
+        sl = qi < a.nq ? a.stats[rows + row] : 0.f;             // rows past the last have weight 0
         sd = a.delta[row];
+        next_q += QC;
+        if (next_q >= a.nq) {
+            next_q = 0;
+            ++next_h;
+        }
     };
-    if (nchunks) load(0);
+    if (nchunks) load();
     for (int c = 0; c < nchunks; ++c) {
         const int buf = c & 1;
         char* qt = mem + buf * 2 * TL::kBytes;
         char* gt = qt + TL::kBytes;
         char* bt = bmem + (BIAS ? buf * QC * kBRow : 0);
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const int u = t + 256 * i;
-            const uint32_t off = TL::off(u / TL::kPieces, u % TL::kPieces);
-            *reinterpret_cast<uint4*>(qt + off) = qp[i];
-            *reinterpret_cast<uint4*>(gt + off) = gp[i];
-        }
+        qp.stage(qt, t, false, 0);
+        gp.stage(gt, t, false, 0);
         if (BIAS)
 #pragma unroll
             for (int i = 0; i < kBN; ++i) {
@@ -296,7 +324,7 @@ __global__ __launch_bounds__(256) void k_cross_backward_kv(const CrossArgs a, in
             stat[buf][2][lane] = st.sh;
             stat[buf][3][lane] = sd;
         }
-        if (c + 1 < nchunks) load(c + 1);
+        load();
         __syncthreads();
         if (!wave_live) continue;
         f32x16_t s[NB], dp[NB];
@@ -307,61 +335,71 @@ __global__ __launch_bounds__(256) void k_cross_backward_kv(const CrossArgs a, in
 #pragma unroll
             for (int i = 0; i < NS; ++i) {
                 Frag<T> f;
-                TL::rows(qt, lane, n, i, f);
+                tl.rows(qt, n, i, f);
                 s[n] = mma(f, kf[i], s[n]);
             }
 #pragma unroll
             for (int i = 0; i < NS; ++i) {
                 Frag<T> f;
-                TL::rows(gt, lane, n, i, f);
+                tl.rows(gt, n, i, f);
                 dp[n] = mma(f, vf[i], dp[n]);
             }
         }
-        auto grads = [&](auto masked, auto isfar) {
-            constexpr bool FAR = decltype(isfar)::value;
+        const int lr = (QC / 2) * hi;                          // the lane's first tile row
+        if constexpr (BIAS) {
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const int r0 = (QC / 2) * hi + 16 * n + 4 * g;      // the lane's four tile rows
-                    float4 bv = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if constexpr (BIAS) {
-                        if constexpr (sizeof(T) == 2) {
-                            const uint2 x = lds_tr4(bt + (r0 + ((lane >> 2) & 3)) * kBRow +
-                                                    (32 * w + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2);
-                            bv = bf4(x.x, x.y);
-                        } else {
-                            const char* p = bt + r0 * kBRow + (32 * w + kl) * 4;
-                            bv = make_float4(*(const float*)p, *(const float*)(p + kBRow), *(const float*)(p + 2 * kBRow),
-                                             *(const float*)(p + 3 * kBRow));
-                        }
-                    }
-                    const float4 d4 = *reinterpret_cast<const float4*>(&stat[buf][3][r0]);
-                    float4 m4, n4, h4;
-                    if (FAR) {
-                        m4 = *reinterpret_cast<const float4*>(&stat[buf][0][r0]);
-                        n4 = *reinterpret_cast<const float4*>(&stat[buf][1][r0]);
+                    const char* p = bt + (lr + 16 * n + 4 * g) * kBRow;
+                    float4 bv;
+                    if constexpr (sizeof(T) == 2) {
+                        const uint2 x = lds_tr4(p + ((lane >> 2) & 3) * kBRow + (32 * w + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2);
+                        bv = bf4(x.x, x.y);
                     } else {
-                        h4 = *reinterpret_cast<const float4*>(&stat[buf][2][r0]);
+                        p += (32 * w + kl) * 4;
+                        bv = make_float4(*(const float*)p, *(const float*)(p + kBRow), *(const float*)(p + 2 * kBRow),
+                                         *(const float*)(p + 3 * kBRow));
                     }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int r = 4 * g + e;
-                        float p = weight<BIAS, FAR>(s[n][r], f4_get(bv, e), a.scale, coef, FAR ? f4_get(m4, e) : 0.f,
-                                                    FAR ? f4_get(n4, e) : 0.f, FAR ? 0.f : f4_get(h4, e));
-                        float ds = p * (dp[n][r] - f4_get(d4, e));
-                        if (decltype(masked)::value) {          // an absent key's k and v may hold anything
-                            p = present ? p : 0.f;
-                            ds = present ? ds : 0.f;
-                        }
-                        s[n][r] = p;
-                        dp[n][r] = ds;
-                    }
+                    for (int e = 0; e < 4; ++e) s[n][4 * g + e] = __builtin_fmaf(s[n][4 * g + e], a.scale, f4_get(bv, e));
                 }
-        };
-        if (far) grads(std::true_type{}, std::true_type{});
-        else if (!all_present) grads(std::true_type{}, std::false_type{});
-        else grads(std::false_type{}, std::false_type{});
+        }
+        if (!all_present) {                                    // an absent key's bias may hold anything
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[n][r] = present ? s[n][r] : -INFINITY;
+        }
+        float cf = coef;
+        const float* shifts = stat[buf][2];
+        if (far) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 m4 = *reinterpret_cast<const float4*>(&stat[buf][0][lr + 16 * n + 4 * g]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        s[n][4 * g + e] = __builtin_fmaf(s[n][4 * g + e], BIAS ? 1.f : a.scale, -f4_get(m4, e));
+                }
+            cf = kLog2e;
+            shifts = stat[buf][1];
+        }
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4 h4 = *reinterpret_cast<const float4*>(&shifts[lr + 16 * n + 4 * g]);
+                const float4 d4 = *reinterpret_cast<const float4*>(&stat[buf][3][lr + 16 * n + 4 * g]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 4 * g + e;
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], cf, f4_get(h4, e)));
+                    s[n][r] = p;
+                    dp[n][r] = p * (dp[n][r] - f4_get(d4, e));
+                }
+            }
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -372,9 +410,9 @@ __global__ __launch_bounds__(256) void k_cross_backward_kv(const CrossArgs a, in
 #pragma unroll
                 for (int i = 0; i < ND; ++i) {
                     Frag<T> f;
-                    TL::cols(gt, lane, n, tt, i, f);
+                    tl.cols(gt, n, tt, i, f);
                     dv[i] = mma(f, pf, dv[i]);
-                    TL::cols(qt, lane, n, tt, i, f);
+                    tl.cols(qt, n, tt, i, f);
                     dk[i] = mma(f, df, dk[i]);
                 }
             }
@@ -400,12 +438,12 @@ __global__ __launch_bounds__(256) void k_cross_backward_kv(const CrossArgs a, in
 // entries and heads that share the bias (a split of them: the sums of the splits are added by
 // k_cross_dbias_sum).
 template <typename T, int DP, int KC>
-__global__ __launch_bounds__(256) void k_cross_dbias(const CrossArgs a, int slot_heads, int shared_heads, int shared,
+__global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const CrossArgs a, int slot_heads, int shared_heads, int shared,
                                                      int qtiles, int ktiles) {
     using TL = Tile<T, DP, KC>;
     constexpr int NB = KC / 32, NS = DP / 16, kPer = 16 / (int)sizeof(T);
     __shared__ __align__(16) char mem[2 * 2 * TL::kBytes];
-    const int t = threadIdx.x, lane = t & 63, w = t >> 6, ql = lane & 31, hi = lane >> 5;
+    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), ql = lane & 31, hi = lane >> 5;
 
     int64_t blk = blockIdx.x;
     const int kt_ = (int)(blk % ktiles);
@@ -422,25 +460,29 @@ __global__ __launch_bounds__(256) void k_cross_dbias(const CrossArgs a, int slot
     const int e0 = (int)((int64_t)shared * split / a.splits), e1 = (int)((int64_t)shared * (split + 1) / a.splits);
 
     BiasRow<T, KC> bias;
-    bias.load((const T*)a.bias.data + slot_b * a.bias.batch + slot_h * a.bias.head + (int64_t)qi * a.bias.row,
-              k0 + (KC / 2) * hi, a.nk);
+    bias.init(a, slot_b, slot_h, min(qw, a.nq - 1), min(qw + 31, a.nq - 1), qi, hi);
+    bias.load(k0, a.nk);
     f32x16_t acc[NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[n][r] = 0.f;
 
+    TL tl;
+    tl.init(lane);
     Part<T, DP, KC, 256> kp, vp;
     KeyByte kbyte;
+    kp.init(a.k.token, a.d, t);
+    vp.init(a.v.token, a.d, t);
     Frag<T> qf[NS], gf[NS];
-    float sm, sl, D;
+    float sm = 0.f, sl = 0.f, D = 0.f;
     const int64_t rows = a.batch * a.heads * a.nq;
     // entry and head of the e-th of those that share this bias: heads innermost
     auto load_keys = [&](int e) {
         const int64_t b = slot_b + e / shared_heads;
-        const int hk = (slot_h + e % shared_heads) / a.group;
-        kp.load((const T*)a.k.data + b * a.k.batch + hk * a.k.head, a.k.token, k0, a.nk, a.d, t);
-        vp.load((const T*)a.v.data + b * a.v.batch + hk * a.v.head, a.v.token, k0, a.nk, a.d, t);
+        const int hk = (slot_h + e % shared_heads) / (a.group * a.key_div);
+        kp.load((const T*)a.k.data + b * a.k.batch + hk * a.k.head, a.k.token, k0, a.nk, a.d);
+        vp.load((const T*)a.v.data + b * a.v.batch + hk * a.v.head, a.v.token, k0, a.nk, a.d);
         kbyte.load(a.mask ? a.mask + b * a.mask_batch : nullptr, k0, a.nk, lane);
     };
     auto load_queries = [&](int e) {
@@ -465,15 +507,14 @@ __global__ __launch_bounds__(256) void k_cross_dbias(const CrossArgs a, int slot
     for (int e = e0; e < e1; ++e) {
         char* kt = mem + ((e - e0) & 1) * 2 * TL::kBytes;
         char* vt = kt + TL::kBytes;
-        uint64_t bits = kbyte.bits(k0, a.nk, lane);
+        uint64_t bits = kbyte.bits(a.mask, k0, a.nk, lane);
         if (KC == 32) bits &= 0xffffffffull;
         const bool some = bits != (KC == 64 ? ~0ull : 0xffffffffull);
         kp.stage(kt, t, some, bits);
         vp.stage(vt, t, some, bits);
-        if (e + 1 < e1) load_keys(e + 1);
+        load_keys(min(e + 1, e1 - 1));
         __syncthreads();
         if (bits != 0 && wave_live) {
-            const uint32_t mine = (uint32_t)(bits >> ((KC / 2) * hi));
             RowStat st;
             st.set(sm, sl);
             const bool far = __any(st.far());
@@ -486,38 +527,31 @@ __global__ __launch_bounds__(256) void k_cross_dbias(const CrossArgs a, int slot
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
                     Frag<T> f;
-                    TL::rows(kt, lane, n, i, f);
+                    tl.rows(kt, n, i, f);
                     s[n] = mma(f, qf[i], s[n]);
                 }
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
                     Frag<T> f;
-                    TL::rows(vt, lane, n, i, f);
+                    tl.rows(vt, n, i, f);
                     dp[n] = mma(f, gf[i], dp[n]);
                 }
             }
-            if (e + 1 < e1) load_queries(e + 1);
-            auto grads = [&](auto masked, auto isfar) {
+            load_queries(min(e + 1, e1 - 1));
+            add_bias<T, KC>(s, bias, a.scale);
+            if (some) drop_absent<NB>(s, (uint32_t)(bits >> ((KC / 2) * hi)));
+            float sh = st.sh;
+            if (far) {
+                take_from<NB>(s, 1.f, st.M);
+                sh = st.n2;
+            }
 #pragma unroll
-                for (int n = 0; n < NB; ++n)
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const float4 bv = bias.get(n, g);
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const int r = 4 * g + x;
-                            float p = weight<true, decltype(isfar)::value>(s[n][r], f4_get(bv, x), a.scale, kLog2e, st.M, st.n2, st.sh);
-                            float ds = p * (dp[n][r] - Dn);
-                            if (decltype(masked)::value) ds = (mine >> (16 * n + r)) & 1 ? ds : 0.f;
-                            acc[n][r] += ds;
-                        }
-                    }
-            };
-            if (far) grads(std::true_type{}, std::true_type{});
-            else if (some) grads(std::true_type{}, std::false_type{});
-            else grads(std::false_type{}, std::false_type{});
-        } else if (e + 1 < e1) {
-            load_queries(e + 1);
+                for (int r = 0; r < 16; ++r)
+                    acc[n][r] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], kLog2e, sh)), dp[n][r] - Dn, acc[n][r]);
+        } else {
+            load_queries(min(e + 1, e1 - 1));
         }
     }
     if (!valid) return;
@@ -576,16 +610,16 @@ template <typename T, int DP, bool BIAS>
 hipError_t backward_q(const CrossArgs& a, hipStream_t s) {
     const int ctiles = (a.nq * a.group + 127) / 128;
     const dim3 grid((unsigned)(a.batch * a.kv_heads * ctiles));
-    hipLaunchKernelGGL((k_cross_backward_q<T, DP, kKeyChunk<T>, BIAS>), grid, dim3(256), 0, s, a, ctiles);
+    constexpr int KC = DP == 128 ? 32 : kKeyChunk<T>;
+    hipLaunchKernelGGL((k_cross_backward_q<T, DP, KC, BIAS>), grid, dim3(256), 0, s, a, ctiles);
     return hipGetLastError();
 }
 
 template <typename T, int DP, bool BIAS>
 hipError_t backward_kv(const CrossArgs& a, hipStream_t s) {
     const int ktiles = (a.nk + 127) / 128;
-    const dim3 grid((unsigned)(a.batch * a.kv_heads * ktiles));
-    constexpr int QC = sizeof(T) == 2 && DP == 32 ? 64 : 32;
-    hipLaunchKernelGGL((k_cross_backward_kv<T, DP, QC, BIAS>), grid, dim3(256), 0, s, a, ktiles);
+    const dim3 grid((unsigned)(a.batch * (a.kv_heads / a.key_div) * ktiles));
+    hipLaunchKernelGGL((k_cross_backward_kv<T, DP, 32, BIAS>), grid, dim3(256), 0, s, a, ktiles);
     return hipGetLastError();
 }
 

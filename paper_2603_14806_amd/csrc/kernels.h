@@ -210,6 +210,7 @@ struct CrossArgs {
     float* part;       // partial results of split calls
     int64_t batch;
     int nq, nk, heads, kv_heads, group, d;
+    int key_div;       // key head of kv_heads' hk: hk / key_div (1, unless query heads that share one are taken singly)
     float scale;
     int splits, split_keys;   // forward: key ranges [s * split_keys, ...); dbias: splits of the shared entries
 };
