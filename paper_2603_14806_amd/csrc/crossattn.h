@@ -202,6 +202,39 @@ struct Part {
     }
 };
 
+// Work-groups go to the eight XCDs in turn; this order gives each XCD consecutive
+// ones, which read the same keys (or queries), so that its L2 serves the repeats.
+__device__ __forceinline__ int64_t xcd_block() {
+    const uint32_t n = gridDim.x, x = blockIdx.x & 7, i = blockIdx.x >> 3;
+    return (int64_t)x * (n >> 3) + min(x, n & 7) + i;
+}
+
+// Wave-private LDS: a wave's LDS operations run in order, only the compiler has to be kept from moving them.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// The four waves' results of the same 32 columns added up: wave w gets channels 8 ND w .. + 8 ND - 1 (as registers
+// 4 j + e, j < ND: channel 8 (ND w + j) + 4 hi + e).  buf: 4 * ND * 16 * 64 floats that no wave uses any more.
+template <int ND>
+__device__ __forceinline__ void add_waves(f32x16_t (&o)[ND], float* buf, int w, int lane) {
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) buf[(w * ND * 16 + 16 * i + r) * 64 + lane] = o[i][r];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < ND; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float x = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x += buf[(i * ND * 16 + 4 * (w * ND + j) + e) * 64 + lane];
+            o[j / 4][4 * (j % 4) + e] = x;
+        }
+}
+
 // Bits of the keys [k0, k0 + KC) that are in range and present, the same in every lane of the wave.
 struct KeyByte {
     uint32_t m;
@@ -227,6 +260,24 @@ constexpr float kFmaMax = 1024.f;
 __device__ __forceinline__ float4 bf4(uint32_t lo, uint32_t hi) {
     return make_float4(__uint_as_float(lo << 16), __uint_as_float(lo & 0xffff0000u), __uint_as_float(hi << 16),
                        __uint_as_float(hi & 0xffff0000u));
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+    else *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
+}
+
+// Channel groups g0 .. of a result (registers 4 j + e: channel 8 (g0 + j) + 4 hi + e), scaled, to a row of d channels.
+template <int ND, typename T>
+__device__ __forceinline__ void store_row(T* row, const f32x16_t (&o)[ND], int groups, int g0, int hi, int d, float scale) {
+#pragma unroll
+    for (int j = 0; j < 4 * ND; ++j) {
+        const int c = 8 * (g0 + j) + 4 * hi;
+        if (j < groups && c < d)
+            store4(row + c, o[j / 4][4 * (j % 4)] * scale, o[j / 4][4 * (j % 4) + 1] * scale,
+                   o[j / 4][4 * (j % 4) + 2] * scale, o[j / 4][4 * (j % 4) + 3] * scale);
+    }
 }
 
 // The bias of one lane's KC / 2 consecutive keys of its query, through a

@@ -12,12 +12,6 @@
 namespace trimul {
 namespace {
 
-template <typename T>
-__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d) {
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
-    else *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
-}
-
 // Waves per SIMD that the registers are limited for.
 template <typename T, int DP, int WK>
 constexpr int forward_waves() {
@@ -37,7 +31,7 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int t = WK == 1 ? threadIdx.x : lane;
 
-    int64_t blk = blockIdx.x;
+    int64_t blk = xcd_block();
     const int split = (int)(blk % a.splits);
     blk /= a.splits;
     const int ct = (int)(blk % ctiles);
@@ -98,19 +92,12 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
         uint64_t bits = kbyte.bits(mask, k0, ke, lane);
         if (KC == 32) bits &= 0xffffffffull;
         const bool some = bits != (KC == 64 ? ~0ull : 0xffffffffull);
-        if (WK > 1) {   // a wave's LDS operations run in order; only the compiler has to be kept from moving them
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-        }
+        if (WK > 1) wave_sync();
         kp.stage(kt, t, some, bits);
         vp.stage(vt, t, some, bits);
         load(c + WK);
-        if (WK == 1) {
-            __syncthreads();
-        } else {
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-        }
+        if (WK == 1) __syncthreads();
+        else wave_sync();
         if (bits != 0 && wave_live) {
             f32x16_t s[NB];
 #pragma unroll
@@ -194,10 +181,9 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
     }
 
     float Lt = L + xor32(L);
-    constexpr int NG = ND * 4;              // groups of four channels a lane holds
+    constexpr int groups = WK == 1 ? ND * 4 : ND;   // groups of four channels that this lane writes, from g0 on
     int g0 = 0;
-    if constexpr (WK > 1) {
-        float* buf = reinterpret_cast<float*>(mem);
+    if constexpr (WK > 1) {                 // each wave ends up with a quarter of the channels
         if (!hi) {
             red[0][w][ql] = M;
             red[1][w][ql] = Lt;
@@ -212,33 +198,17 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
 #pragma unroll
         for (int i = 0; i < ND; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) buf[(w * ND * 16 + 16 * i + r) * 64 + lane] = o[i][r] * f;
-        __syncthreads();
+            for (int r = 0; r < 16; ++r) o[i][r] *= f;
+        add_waves<ND>(o, reinterpret_cast<float*>(mem), w, lane);
         M = Mn;
         Lt = sum;
-        g0 = w * ND;                        // each wave adds and writes a quarter of the channels
-#pragma unroll
-        for (int j = 0; j < ND; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float x = 0.f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x += buf[(i * ND * 16 + 4 * (g0 + j) + e) * 64 + lane];
-                o[j / 4][4 * (j % 4) + e] = x;
-            }
+        g0 = w * ND;
     }
     if (!valid) return;
     const int64_t row = (b * a.heads + h) * a.nq + qi;
     if (a.splits > 1) {
         const int64_t rows = a.batch * a.heads * a.nq, at = (int64_t)split * rows + row;
-        float* po = a.part + at * a.d;
-#pragma unroll
-        for (int j = 0; j < (WK > 1 ? ND : NG); ++j) {
-            const int c = 8 * (g0 + j) + 4 * hi;
-            if (c < a.d)
-                *reinterpret_cast<float4*>(po + c) = make_float4(o[j / 4][4 * (j % 4)], o[j / 4][4 * (j % 4) + 1],
-                                                                 o[j / 4][4 * (j % 4) + 2], o[j / 4][4 * (j % 4) + 3]);
-        }
+        store_row<ND>(a.part + at * a.d, o, groups, g0, hi, a.d, 1.f);
         if (!hi && (WK == 1 || w == 0)) {
             float* pm = a.part + (int64_t)a.splits * rows * a.d;
             pm[at] = M;
@@ -247,14 +217,7 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
         return;
     }
     const float inv = Lt == 0.f ? 0.f : 1.f / Lt;
-    T* po = (T*)a.out.data + b * a.out.batch + (int64_t)qi * a.out.token + h * a.out.head;
-#pragma unroll
-    for (int j = 0; j < (WK > 1 ? ND : NG); ++j) {
-        const int c = 8 * (g0 + j) + 4 * hi;
-        if (c < a.d)
-            store4(po + c, o[j / 4][4 * (j % 4)] * inv, o[j / 4][4 * (j % 4) + 1] * inv,
-                   o[j / 4][4 * (j % 4) + 2] * inv, o[j / 4][4 * (j % 4) + 3] * inv);
-    }
+    store_row<ND>((T*)a.out.data + b * a.out.batch + (int64_t)qi * a.out.token + h * a.out.head, o, groups, g0, hi, a.d, inv);
     if (a.stats && !hi && (WK == 1 || w == 0)) {
         a.stats[row] = BIAS ? M : M * a.scale;
         a.stats[a.batch * a.heads * a.nq + row] = Lt;
@@ -324,11 +287,12 @@ hipError_t forward(const CrossArgs& a, const CrossPlan& p, hipStream_t s) {
 
 }  // namespace
 
-// Few columns: 32 to a work-group, its waves on different keys.  The keys are
-// split where the work-groups alone would not give each of the 256 compute
-// units two, as long as a split keeps 256 keys (two chunks a wave).
+// 128 columns to a work-group where that makes two work-groups for each of the
+// 256 compute units; else 32, its waves on different keys.  Where even that
+// leaves compute units without two, the keys are split, as long as a
+// split keeps 256 keys (two chunks a wave).
 CrossPlan cross_plan(int64_t batch, int kv_heads, int64_t cols, int64_t nk) {
-    CrossPlan p{cols <= 32 ? 32 : 128, 1, (int)((nk + 63) / 64 * 64)};
+    CrossPlan p{cross_few(batch * kv_heads, cols) ? 32 : 128, 1, (int)((nk + 63) / 64 * 64)};
     const int64_t groups = batch * kv_heads * ((cols + p.cols - 1) / p.cols);
     if (groups > 0 && groups < 512) {
         int64_t n = (512 + groups - 1) / groups;

@@ -15,12 +15,6 @@
 namespace trimul {
 namespace {
 
-template <typename T>
-__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d) {
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
-    else *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
-}
-
 // A query's statistics as the weights use them: P = exp2((x - M) log2 e + n2) = exp2(x log2 e + sh).
 // A query with no key: M = 0, n2 = -inf, P = 0.
 struct RowStat {
@@ -64,23 +58,28 @@ __device__ __forceinline__ void take_from(f32x16_t (&s)[NB], float scale, float 
 
 // ------------------------------------------------------------------ queries: dq, D
 //
-// The forward's layout (lane: one column, registers: keys), 32 columns a wave.
-template <typename T, int DP>
-constexpr int q_waves() { return DP == 32 ? 3 : DP == 64 || sizeof(T) == 2 ? 2 : 1; }
+// The forward's layout (lane: one column, registers: keys): WK = 1, 32 columns
+// a wave, or WK = 4, 32 columns a work-group and its waves on different keys.
+template <typename T, int DP, int WK>
+constexpr int q_waves() {
+    if (WK > 1) return sizeof(T) == 2 ? (DP == 32 ? 3 : DP == 64 ? 2 : 1) : (DP == 32 ? 2 : 1);
+    return DP == 32 ? 3 : DP == 64 || sizeof(T) == 2 ? 2 : 1;
+}
 
-template <typename T, int DP, int KC, bool BIAS>
-__global__ __launch_bounds__(256, (q_waves<T, DP>())) void k_cross_backward_q(const CrossArgs a, int ctiles) {
+template <typename T, int DP, int KC, int WK, bool BIAS>
+__global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_q(const CrossArgs a, int ctiles) {
     using TL = Tile<T, DP, KC>;
-    constexpr int NB = KC / 32, ND = DP / 32, NS = DP / 16;
-    __shared__ __align__(16) char mem[2 * 2 * TL::kBytes];
-    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), ql = lane & 31, hi = lane >> 5;
+    constexpr int NT = 256 / WK, NB = KC / 32, ND = DP / 32, NS = DP / 16;
+    __shared__ __align__(16) char mem[(WK == 1 ? 2 : 4) * 2 * TL::kBytes];
+    const int lane = threadIdx.x & 63, ql = lane & 31, hi = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = WK == 1 ? threadIdx.x : lane;
 
-    int64_t blk = blockIdx.x;
+    int64_t blk = xcd_block();
     const int ct = (int)(blk % ctiles);
     blk /= ctiles;
     const int hk = (int)(blk % a.kv_heads);
     const int64_t b = blk / a.kv_heads;
-    const int ncols = a.nq * a.group, cw = ct * 128 + 32 * w;
+    const int ncols = a.nq * a.group, cw = ct * (128 / WK) + (WK == 1 ? 32 * w : 0);
     const bool wave_live = cw < ncols, valid = cw + ql < ncols;
     const int col = min(cw + ql, ncols - 1);
     const int qi = col / a.group, h = hk * a.group + (col - qi * a.group);
@@ -101,7 +100,7 @@ __global__ __launch_bounds__(256, (q_waves<T, DP>())) void k_cross_backward_q(co
             D += Frag<T>::dot(gf[s], of);
         }
         D += xor32(D);
-        if (valid && !hi) a.delta[row] = D;
+        if (valid && !hi && (WK == 1 || w == 0)) a.delta[row] = D;
     }
     RowStat st;
     st.set(a.stats[row], a.stats[a.batch * a.heads * a.nq + row]);
@@ -120,7 +119,7 @@ __global__ __launch_bounds__(256, (q_waves<T, DP>())) void k_cross_backward_q(co
 
     TL tl;
     tl.init(lane);
-    Part<T, DP, KC, 256> kp, vp;
+    Part<T, DP, KC, NT> kp, vp;
     KeyByte kbyte;
     BiasRow<T, KC> bp;
     kp.init(a.k.token, a.d, t);
@@ -130,21 +129,24 @@ __global__ __launch_bounds__(256, (q_waves<T, DP>())) void k_cross_backward_q(co
         vp.load(vb, a.v.token, c * KC, a.nk, a.d);
         kbyte.load(mask, c * KC, a.nk, lane);
     };
-    load(0);
+    const int c0 = WK == 1 ? 0 : w;
+    load(c0);
     if (BIAS) {
         bp.init(a, b, hk, min(cw, ncols - 1), min(cw + 31, ncols - 1), qi, h, hi);
-        bp.load(0, a.nk);
+        bp.load(c0 * KC, a.nk);
     }
-    for (int c = 0; c < nchunks; ++c) {
-        char* kt = mem + (c & 1) * 2 * TL::kBytes;
+    for (int c = c0; c < nchunks; c += WK) {
+        char* kt = mem + (WK == 1 ? (c & 1) : w) * 2 * TL::kBytes;
         char* vt = kt + TL::kBytes;
         uint64_t bits = kbyte.bits(mask, c * KC, a.nk, lane);
         if (KC == 32) bits &= 0xffffffffull;
         const bool some = bits != (KC == 64 ? ~0ull : 0xffffffffull);
+        if (WK > 1) wave_sync();
         kp.stage(kt, t, some, bits);
         vp.stage(vt, t, some, bits);
-        load(c + 1);
-        __syncthreads();
+        load(c + WK);
+        if (WK == 1) __syncthreads();
+        else wave_sync();
         if (bits != 0 && wave_live) {
             f32x16_t s[NB], dp[NB];
 #pragma unroll
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(256, (q_waves<T, DP>())) void k_cross_backward_q(co
             }
             if (BIAS) {
                 add_bias<T, KC>(s, bp, a.scale);
-                bp.load((c + 1) * KC, a.nk);
+                bp.load((c + WK) * KC, a.nk);
             }
             if (some) drop_absent<NB>(s, (uint32_t)(bits >> ((KC / 2) * hi)));
             float cf = coef, sh = st.sh;
@@ -194,49 +196,51 @@ __global__ __launch_bounds__(256, (q_waves<T, DP>())) void k_cross_backward_q(co
                     }
                 }
         } else if (BIAS) {
-            bp.load((c + 1) * KC, a.nk);
+            bp.load((c + WK) * KC, a.nk);
         }
     }
-    if (!valid) return;
-    T* po = (T*)a.dq.data + b * a.dq.batch + (int64_t)qi * a.dq.token + h * a.dq.head;
-#pragma unroll
-    for (int j = 0; j < 4 * ND; ++j) {
-        const int c = 8 * j + 4 * hi;
-        if (c < a.d)
-            store4(po + c, acc[j / 4][4 * (j % 4)] * a.scale, acc[j / 4][4 * (j % 4) + 1] * a.scale,
-                   acc[j / 4][4 * (j % 4) + 2] * a.scale, acc[j / 4][4 * (j % 4) + 3] * a.scale);
+    if constexpr (WK > 1) {
+        __syncthreads();
+        add_waves<ND>(acc, reinterpret_cast<float*>(mem), w, lane);
     }
+    if (!valid) return;
+    store_row<ND>((T*)a.dq.data + b * a.dq.batch + (int64_t)qi * a.dq.token + h * a.dq.head, acc, WK == 1 ? 4 * ND : ND,
+                  WK == 1 ? 0 : w * ND, hi, a.d, a.scale);
 }
 
 // ------------------------------------------------------------------ keys: dk, dv
 //
 // Lane: one key (K and V as B operands in registers), registers: the queries of
 // a chunk of QC (of one head after the other), whose q and dout pass through
-// LDS; 32 keys a wave.
+// LDS: WK = 1, 32 keys a wave, or WK = 4, 32 keys a work-group and its waves on
+// different chunks.
 // The bias tile of a chunk passes through LDS too and is read transposed
 // (four queries of one key at a time).
-template <typename T, int DP>
+template <typename T, int DP, int WK>
 constexpr int kv_waves() { return DP == 32 ? (sizeof(T) == 2 ? 3 : 2) : DP == 64 && sizeof(T) == 2 ? 2 : 1; }
 
-template <typename T, int DP, int QC, bool BIAS>
-__global__ __launch_bounds__(256, (kv_waves<T, DP>())) void k_cross_backward_kv(const CrossArgs a, int ktiles) {
+template <typename T, int DP, int QC, int WK, bool BIAS>
+__global__ __launch_bounds__(256, (kv_waves<T, DP, WK>())) void k_cross_backward_kv(const CrossArgs a, int ktiles) {
     using TL = Tile<T, DP, QC>;
     constexpr int NB = QC / 32, ND = DP / 32, NS = DP / 16;
-    constexpr int kBRow = 128 * (int)sizeof(T) + (sizeof(T) == 2 ? 64 : 16);   // spreads four rows over the banks
-    constexpr int kBPieces = 128 * (int)sizeof(T) / 16, kBN = QC * kBPieces / 256;
-    __shared__ __align__(16) char mem[2 * 2 * TL::kBytes];
-    __shared__ __align__(16) char bmem[BIAS ? 2 * QC * kBRow : 16];
-    __shared__ __align__(16) float stat[2][4][QC];             // M, n2, sh, D of a chunk's columns
-    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), kl = lane & 31, hi = lane >> 5;
+    constexpr int NT = 256 / WK, KT = 128 / WK, BUF = WK == 1 ? 2 : 4;   // threads of a chunk, keys, buffers
+    // bias rows in LDS: four of them spread over the banks
+    constexpr int kBRow = KT * (int)sizeof(T) + (sizeof(T) == 4 ? 16 : KT == 128 ? 64 : 0);
+    constexpr int kBPieces = KT * (int)sizeof(T) / 16, kBN = QC * kBPieces / NT;
+    __shared__ __align__(16) char mem[BUF * 2 * TL::kBytes];
+    __shared__ __align__(16) char bmem[BIAS ? BUF * QC * kBRow : 16];
+    __shared__ __align__(16) float stat[BUF][4][QC];           // M, n2, sh, D of a chunk's columns
+    const int lane = threadIdx.x & 63, kl = lane & 31, hi = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = WK == 1 ? threadIdx.x : lane;
 
-    int64_t blk = blockIdx.x;
+    int64_t blk = xcd_block();
     const int kt_ = (int)(blk % ktiles);
     blk /= ktiles;
     const int kv_heads = a.kv_heads / a.key_div, group = a.group * a.key_div;
     const int hk = (int)(blk % kv_heads);
     const int64_t b = blk / kv_heads;
-    const int key0 = kt_ * 128, key = key0 + 32 * w + kl;
-    const bool valid = key < a.nk, wave_live = key0 + 32 * w < a.nk;
+    const int key0 = kt_ * KT, kw = WK == 1 ? 32 * w : 0, key = key0 + kw + kl;
+    const bool valid = key < a.nk, wave_live = key0 + kw < a.nk;
     const int kc = min(key, a.nk - 1);
     const bool present = valid && (!a.mask || a.mask[b * a.mask_batch + kc] != 0);
     const bool all_present = __all(present);
@@ -265,7 +269,7 @@ __global__ __launch_bounds__(256, (kv_waves<T, DP>())) void k_cross_backward_kv(
 
     TL tl;
     tl.init(lane);
-    Part<T, DP, QC, 256> qp, gp;
+    Part<T, DP, QC, NT> qp, gp;
     uint4 bp[BIAS ? kBN : 1];
     uint32_t boff[BIAS ? kBN : 1];
     qp.init(a.q.token, a.d, t);
@@ -273,12 +277,18 @@ __global__ __launch_bounds__(256, (kv_waves<T, DP>())) void k_cross_backward_kv(
     if (BIAS)
 #pragma unroll
         for (int i = 0; i < kBN; ++i) {
-            const int u = t + 256 * i, k = key0 + (u % kBPieces) * TL::kPer;
+            const int u = t + NT * i, k = key0 + (u % kBPieces) * TL::kPer;
             boff[i] = k < a.nk ? (uint32_t)(u / kBPieces) * (uint32_t)(a.bias.row * (int)sizeof(T)) + 16 * (u % kBPieces) : 0xfffffff0u;
         }
     float sm = 0.f, sl = 0.f, sd = 0.f;
     const int64_t rows = a.batch * a.heads * a.nq;
-    int next_h = hk * group, next_q = 0;                      // the chunk that load() takes
+    int next_h = hk * group, next_q = WK == 1 ? 0 : w * QC;   // the chunk that load() takes
+    auto wrap = [&]() {
+        while (next_q >= per_head * QC) {
+            next_q -= per_head * QC;
+            ++next_h;
+        }
+    };
     auto load = [&]() {
         const int left = next_h < (hk + 1) * group ? a.nq : 0;  // behind the last chunk nothing is read
         const int h = min(next_h, (hk + 1) * group - 1);
@@ -286,7 +296,7 @@ __global__ __launch_bounds__(256, (kv_waves<T, DP>())) void k_cross_backward_kv(
         gp.load((const T*)a.dout.data + b * a.dout.batch + h * a.dout.head, a.dout.token, next_q, left, a.d);
         if (BIAS) {
             const auto r = make_rsrc((const T*)a.bias.data + b * a.bias.batch + h * a.bias.head + (int64_t)next_q * a.bias.row + key0,
-                                     left ? (uint32_t)((min(left - next_q, QC) - 1) * (uint32_t)a.bias.row + min(128, (a.nk - key0 + 7) & ~7)) * (uint32_t)sizeof(T) : 0u);
+                                     left ? (uint32_t)((min(left - next_q, QC) - 1) * (uint32_t)a.bias.row + min(KT, (a.nk - key0 + 7) & ~7)) * (uint32_t)sizeof(T) : 0u);
 #pragma unroll
             for (int i = 0; i < kBN; ++i) bp[i] = buf_load16(r, boff[i]);
         }
@@ -295,37 +305,39 @@ __global__ __launch_bounds__(256, (kv_waves<T, DP>())) void k_cross_backward_kv(
         sm = a.stats[row];
         sl = qi < a.nq ? a.stats[rows + row] : 0.f;             // rows past the last have weight 0
         sd = a.delta[row];
-        next_q += QC;
-        if (next_q >= a.nq) {
-            next_q = 0;
-            ++next_h;
-        }
+        next_q += WK * QC;
+        wrap();
     };
-    if (nchunks) load();
-    for (int c = 0; c < nchunks; ++c) {
-        const int buf = c & 1;
+    if (nchunks) {                          // (wrap() ends only where a head has chunks)
+        wrap();
+        load();
+    }
+    for (int c = WK == 1 ? 0 : w; c < nchunks; c += WK) {
+        const int buf = WK == 1 ? c & 1 : w;
         char* qt = mem + buf * 2 * TL::kBytes;
         char* gt = qt + TL::kBytes;
         char* bt = bmem + (BIAS ? buf * QC * kBRow : 0);
+        if (WK > 1) wave_sync();
         qp.stage(qt, t, false, 0);
         gp.stage(gt, t, false, 0);
         if (BIAS)
 #pragma unroll
             for (int i = 0; i < kBN; ++i) {
-                const int u = t + 256 * i;
+                const int u = t + NT * i;
                 *reinterpret_cast<uint4*>(bt + (u / kBPieces) * kBRow + (u % kBPieces) * 16) = bp[i];
             }
         RowStat st;
         st.set(sm, sl);
         const bool far = __any(st.far());
-        if (w == 0 && lane < QC) {
+        if ((WK > 1 || w == 0) && lane < QC) {
             stat[buf][0][lane] = st.M;
             stat[buf][1][lane] = st.n2;
             stat[buf][2][lane] = st.sh;
             stat[buf][3][lane] = sd;
         }
         load();
-        __syncthreads();
+        if (WK == 1) __syncthreads();
+        else wave_sync();
         if (!wave_live) continue;
         f32x16_t s[NB], dp[NB];
 #pragma unroll
@@ -354,10 +366,10 @@ __global__ __launch_bounds__(256, (kv_waves<T, DP>())) void k_cross_backward_kv(
                     const char* p = bt + (lr + 16 * n + 4 * g) * kBRow;
                     float4 bv;
                     if constexpr (sizeof(T) == 2) {
-                        const uint2 x = lds_tr4(p + ((lane >> 2) & 3) * kBRow + (32 * w + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2);
+                        const uint2 x = lds_tr4(p + ((lane >> 2) & 3) * kBRow + (kw + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2);
                         bv = bf4(x.x, x.y);
                     } else {
-                        p += (32 * w + kl) * 4;
+                        p += (kw + kl) * 4;
                         bv = make_float4(*(const float*)p, *(const float*)(p + kBRow), *(const float*)(p + 2 * kBRow),
                                          *(const float*)(p + 3 * kBRow));
                     }
@@ -417,19 +429,17 @@ __global__ __launch_bounds__(256, (kv_waves<T, DP>())) void k_cross_backward_kv(
                 }
             }
     }
-    if (!valid) return;
-    T* pk = (T*)a.dk.data + b * a.dk.batch + (int64_t)key * a.dk.token + hk * a.dk.head;
-    T* pv = (T*)a.dv.data + b * a.dv.batch + (int64_t)key * a.dv.token + hk * a.dv.head;
-#pragma unroll
-    for (int j = 0; j < 4 * ND; ++j) {
-        const int c = 8 * j + 4 * hi;
-        if (c < a.d) {
-            store4(pk + c, dk[j / 4][4 * (j % 4)] * a.scale, dk[j / 4][4 * (j % 4) + 1] * a.scale,
-                   dk[j / 4][4 * (j % 4) + 2] * a.scale, dk[j / 4][4 * (j % 4) + 3] * a.scale);
-            store4(pv + c, dv[j / 4][4 * (j % 4)], dv[j / 4][4 * (j % 4) + 1], dv[j / 4][4 * (j % 4) + 2],
-                   dv[j / 4][4 * (j % 4) + 3]);
-        }
+    if constexpr (WK > 1) {
+        __syncthreads();
+        add_waves<ND>(dk, reinterpret_cast<float*>(mem), w, lane);
+        __syncthreads();
+        add_waves<ND>(dv, reinterpret_cast<float*>(mem), w, lane);
     }
+    if (!valid) return;
+    constexpr int groups = WK == 1 ? 4 * ND : ND;
+    const int g0 = WK == 1 ? 0 : w * ND;
+    store_row<ND>((T*)a.dk.data + b * a.dk.batch + (int64_t)key * a.dk.token + hk * a.dk.head, dk, groups, g0, hi, a.d, a.scale);
+    store_row<ND>((T*)a.dv.data + b * a.dv.batch + (int64_t)key * a.dv.token + hk * a.dv.head, dv, groups, g0, hi, a.d, 1.f);
 }
 
 // ------------------------------------------------------------------ dbias
@@ -445,7 +455,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const Cro
     __shared__ __align__(16) char mem[2 * 2 * TL::kBytes];
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), ql = lane & 31, hi = lane >> 5;
 
-    int64_t blk = blockIdx.x;
+    int64_t blk = xcd_block();
     const int kt_ = (int)(blk % ktiles);
     blk /= ktiles;
     const int qt_ = (int)(blk % qtiles);
@@ -608,18 +618,30 @@ int key_chunk(int dtype) { return dtype == 1 ? 64 : 32; }
 
 template <typename T, int DP, bool BIAS>
 hipError_t backward_q(const CrossArgs& a, hipStream_t s) {
-    const int ctiles = (a.nq * a.group + 127) / 128;
+    const int cols = a.nq * a.group;
+    const bool few = cross_few(a.batch * a.kv_heads, cols);
+    const int ctiles = few ? (cols + 31) / 32 : (cols + 127) / 128;
     const dim3 grid((unsigned)(a.batch * a.kv_heads * ctiles));
     constexpr int KC = DP == 128 ? 32 : kKeyChunk<T>;
-    hipLaunchKernelGGL((k_cross_backward_q<T, DP, KC, BIAS>), grid, dim3(256), 0, s, a, ctiles);
+    if (few) hipLaunchKernelGGL((k_cross_backward_q<T, DP, 32, 4, BIAS>), grid, dim3(256), 0, s, a, ctiles);
+    else hipLaunchKernelGGL((k_cross_backward_q<T, DP, KC, 1, BIAS>), grid, dim3(256), 0, s, a, ctiles);
     return hipGetLastError();
 }
 
 template <typename T, int DP, bool BIAS>
 hipError_t backward_kv(const CrossArgs& a, hipStream_t s) {
-    const int ktiles = (a.nk + 127) / 128;
-    const dim3 grid((unsigned)(a.batch * (a.kv_heads / a.key_div) * ktiles));
-    hipLaunchKernelGGL((k_cross_backward_kv<T, DP, 32, BIAS>), grid, dim3(256), 0, s, a, ktiles);
+    const int64_t heads = a.batch * (a.kv_heads / a.key_div);
+    // (at d > 64 in fp32 a wave cannot hold a chunk of its own)
+    constexpr bool kSplit = sizeof(T) == 2 || DP < 128;
+    const bool few = kSplit && cross_few(heads, a.nk);
+    const int ktiles = few ? (a.nk + 31) / 32 : (a.nk + 127) / 128;
+    const dim3 grid((unsigned)(heads * ktiles));
+    if constexpr (kSplit)
+        if (few) {
+            hipLaunchKernelGGL((k_cross_backward_kv<T, DP, 32, 4, BIAS>), grid, dim3(256), 0, s, a, ktiles);
+            return hipGetLastError();
+        }
+    hipLaunchKernelGGL((k_cross_backward_kv<T, DP, 32, 1, BIAS>), grid, dim3(256), 0, s, a, ktiles);
     return hipGetLastError();
 }
 

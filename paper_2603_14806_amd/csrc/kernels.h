@@ -220,6 +220,8 @@ constexpr int kCrossMaxSplits = 64;   // one lane of the join each
 struct CrossPlan {
     int cols, splits, split_keys;
 };
+// Whether tiles of 128 columns (or keys) are too few: below two for each of the 256 compute units.
+inline bool cross_few(int64_t heads, int64_t n) { return heads * ((n + 127) / 128) < 512; }
 CrossPlan cross_plan(int64_t batch, int kv_heads, int64_t cols, int64_t nk);
 size_t cross_part_floats(const CrossPlan& p, int64_t batch, int64_t nq, int heads, int d);
 // Splits of the dbias pass over `shared` entries and heads per bias.
