@@ -140,6 +140,7 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
             const float Ms = Mn == -INFINITY ? 0.f : Mn;      // no key yet: every x is -inf and every weight 0
             const float alpha = __builtin_amdgcn_exp2f((M - Ms) * coef);
             L *= alpha;
+            if (__any(alpha != 1.f))                          // (for a wave deep in the keys the maxima stand most of the time)
 #pragma unroll
             for (int i = 0; i < ND; ++i)
 #pragma unroll

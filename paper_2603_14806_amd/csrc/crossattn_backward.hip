@@ -213,17 +213,21 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
 // Lane: one key (K and V as B operands in registers), registers: the queries of
 // a chunk of QC (of one head after the other), whose q and dout pass through
 // LDS: WK = 1, 32 keys a wave, or WK = 4, 32 keys a work-group and its waves on
-// different chunks.
+// different chunks.  TWO (WK = 1): eight waves, each 32 keys taken by two of
+// them, one for dv (S and P^T dout), one for dk (S, dP and dS^T Q).  S twice
+// is a quarter more products, but at d = 128 the two sums and the fragments of
+// K and V leave no room for a second wave on a SIMD, and a single one waits
+// for each of its LDS reads and products in turn.
 // The bias tile of a chunk passes through LDS too and is read transposed
 // (four queries of one key at a time).
-template <typename T, int DP, int WK>
-constexpr int kv_waves() { return DP == 32 ? (sizeof(T) == 2 ? 3 : 2) : DP == 64 && sizeof(T) == 2 ? 2 : 1; }
+template <typename T, int DP, int WK, bool TWO>
+constexpr int kv_waves() { return TWO ? 2 : DP == 32 ? (sizeof(T) == 2 ? 3 : 2) : DP == 64 && sizeof(T) == 2 ? 2 : 1; }
 
-template <typename T, int DP, int QC, int WK, bool BIAS>
-__global__ __launch_bounds__(256, (kv_waves<T, DP, WK>())) void k_cross_backward_kv(const CrossArgs a, int ktiles) {
+template <typename T, int DP, int QC, int WK, bool TWO, bool BIAS>
+__global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void k_cross_backward_kv(const CrossArgs a, int ktiles) {
     using TL = Tile<T, DP, QC>;
     constexpr int NB = QC / 32, ND = DP / 32, NS = DP / 16;
-    constexpr int NT = 256 / WK, KT = 128 / WK, BUF = WK == 1 ? 2 : 4;   // threads of a chunk, keys, buffers
+    constexpr int NT = (TWO ? 512 : 256) / WK, KT = 128 / WK, BUF = WK == 1 ? 2 : 4;   // threads of a chunk, keys, buffers
     // bias rows in LDS: four of them spread over the banks
     constexpr int kBRow = KT * (int)sizeof(T) + (sizeof(T) == 4 ? 16 : KT == 128 ? 64 : 0);
     constexpr int kBPieces = KT * (int)sizeof(T) / 16, kBN = QC * kBPieces / NT;
@@ -231,7 +235,9 @@ __global__ __launch_bounds__(256, (kv_waves<T, DP, WK>())) void k_cross_backward
     __shared__ __align__(16) char bmem[BIAS ? BUF * QC * kBRow : 16];
     __shared__ __align__(16) float stat[BUF][4][QC];           // M, n2, sh, D of a chunk's columns
     const int lane = threadIdx.x & 63, kl = lane & 31, hi = lane >> 5;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = WK == 1 ? threadIdx.x : lane;
+    const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = WK == 1 ? threadIdx.x : lane;
+    const int w = TWO ? wid & 3 : wid;
+    const bool for_k = TWO && wid >= 4;                        // TWO: this wave's half
 
     int64_t blk = xcd_block();
     const int kt_ = (int)(blk % ktiles);
@@ -261,11 +267,11 @@ __global__ __launch_bounds__(256, (kv_waves<T, DP, WK>())) void k_cross_backward
             }
         }
     }
-    f32x16_t dk[ND], dv[ND];
+    f32x16_t dk[TWO ? 1 : ND], dv[ND];                         // TWO: dv is the wave's one sum, dv's or dk's
 #pragma unroll
     for (int i = 0; i < ND; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dk[i][r] = dv[i][r] = 0.f;
+        for (int r = 0; r < 16; ++r) dk[TWO ? 0 : i][r] = dv[i][r] = 0.f;
 
     TL tl;
     tl.init(lane);
@@ -329,7 +335,7 @@ __global__ __launch_bounds__(256, (kv_waves<T, DP, WK>())) void k_cross_backward
         RowStat st;
         st.set(sm, sl);
         const bool far = __any(st.far());
-        if ((WK > 1 || w == 0) && lane < QC) {
+        if ((WK > 1 || wid == 0) && lane < QC) {
             stat[buf][0][lane] = st.M;
             stat[buf][1][lane] = st.n2;
             stat[buf][2][lane] = st.sh;
@@ -350,12 +356,13 @@ __global__ __launch_bounds__(256, (kv_waves<T, DP, WK>())) void k_cross_backward
                 tl.rows(qt, n, i, f);
                 s[n] = mma(f, kf[i], s[n]);
             }
+            if (!TWO || for_k)
 #pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                Frag<T> f;
-                tl.rows(gt, n, i, f);
-                dp[n] = mma(f, vf[i], dp[n]);
-            }
+                for (int i = 0; i < NS; ++i) {
+                    Frag<T> f;
+                    tl.rows(gt, n, i, f);
+                    dp[n] = mma(f, vf[i], dp[n]);
+                }
         }
         const int lr = (QC / 2) * hi;                          // the lane's first tile row
         if constexpr (BIAS) {
@@ -403,43 +410,60 @@ __global__ __launch_bounds__(256, (kv_waves<T, DP, WK>())) void k_cross_backward
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const float4 h4 = *reinterpret_cast<const float4*>(&shifts[lr + 16 * n + 4 * g]);
-                const float4 d4 = *reinterpret_cast<const float4*>(&stat[buf][3][lr + 16 * n + 4 * g]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = 4 * g + e;
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], cf, f4_get(h4, e)));
-                    s[n][r] = p;
-                    dp[n][r] = p * (dp[n][r] - f4_get(d4, e));
-                }
+                for (int e = 0; e < 4; ++e)
+                    s[n][4 * g + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][4 * g + e], cf, f4_get(h4, e)));
             }
+        if (!TWO || for_k)
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 d4 = *reinterpret_cast<const float4*>(&stat[buf][3][lr + 16 * n + 4 * g]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float ds = s[n][4 * g + e] * (dp[n][4 * g + e] - f4_get(d4, e));
+                        if (TWO) s[n][4 * g + e] = ds;
+                        else dp[n][4 * g + e] = ds;
+                    }
+                }
+        const char* vt = TWO && for_k ? qt : gt;
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {
                 Frag<T> pf, df;
                 take8(s[n], tt, pf);
-                take8(dp[n], tt, df);
+                if (!TWO) take8(dp[n], tt, df);
 #pragma unroll
                 for (int i = 0; i < ND; ++i) {
                     Frag<T> f;
-                    tl.cols(gt, n, tt, i, f);
+                    tl.cols(vt, n, tt, i, f);
                     dv[i] = mma(f, pf, dv[i]);
-                    tl.cols(qt, n, tt, i, f);
-                    dk[i] = mma(f, df, dk[i]);
+                    if (!TWO) {
+                        tl.cols(qt, n, tt, i, f);
+                        dk[TWO ? 0 : i] = mma(f, df, dk[TWO ? 0 : i]);
+                    }
                 }
             }
     }
-    if constexpr (WK > 1) {
-        __syncthreads();
-        add_waves<ND>(dk, reinterpret_cast<float*>(mem), w, lane);
-        __syncthreads();
-        add_waves<ND>(dv, reinterpret_cast<float*>(mem), w, lane);
+    T* const to_k = (T*)a.dk.data + b * a.dk.batch + (int64_t)key * a.dk.token + hk * a.dk.head;
+    T* const to_v = (T*)a.dv.data + b * a.dv.batch + (int64_t)key * a.dv.token + hk * a.dv.head;
+    if constexpr (TWO) {
+        if (valid) store_row<ND>(for_k ? to_k : to_v, dv, 4 * ND, 0, hi, a.d, for_k ? a.scale : 1.f);
+    } else {
+        if constexpr (WK > 1) {
+            __syncthreads();
+            add_waves<ND>(dk, reinterpret_cast<float*>(mem), w, lane);
+            __syncthreads();
+            add_waves<ND>(dv, reinterpret_cast<float*>(mem), w, lane);
+        }
+        if (!valid) return;
+        constexpr int groups = WK == 1 ? 4 * ND : ND;
+        const int g0 = WK == 1 ? 0 : w * ND;
+        store_row<ND>(to_k, dk, groups, g0, hi, a.d, a.scale);
+        store_row<ND>(to_v, dv, groups, g0, hi, a.d, 1.f);
     }
-    if (!valid) return;
-    constexpr int groups = WK == 1 ? 4 * ND : ND;
-    const int g0 = WK == 1 ? 0 : w * ND;
-    store_row<ND>((T*)a.dk.data + b * a.dk.batch + (int64_t)key * a.dk.token + hk * a.dk.head, dk, groups, g0, hi, a.d, a.scale);
-    store_row<ND>((T*)a.dv.data + b * a.dv.batch + (int64_t)key * a.dv.token + hk * a.dv.head, dv, groups, g0, hi, a.d, 1.f);
 }
 
 // ------------------------------------------------------------------ dbias
@@ -631,17 +655,18 @@ hipError_t backward_q(const CrossArgs& a, hipStream_t s) {
 template <typename T, int DP, bool BIAS>
 hipError_t backward_kv(const CrossArgs& a, hipStream_t s) {
     const int64_t heads = a.batch * (a.kv_heads / a.key_div);
-    // (at d > 64 in fp32 a wave cannot hold a chunk of its own)
-    constexpr bool kSplit = sizeof(T) == 2 || DP < 128;
-    const bool few = kSplit && cross_few(heads, a.nk);
+    constexpr bool kTwo = DP == 128 && sizeof(T) == 2, kSplit = DP < 128 || sizeof(T) == 2;
+    // (d > 64: in bf16 half a tile per compute unit is enough for the eight waves, in fp32 a wave's registers do not hold
+    // a chunk of its own)
+    const bool few = kSplit && cross_few(heads, a.nk) && (!kTwo || heads * ((a.nk + 127) / 128) < 128);
     const int ktiles = few ? (a.nk + 31) / 32 : (a.nk + 127) / 128;
     const dim3 grid((unsigned)(heads * ktiles));
     if constexpr (kSplit)
         if (few) {
-            hipLaunchKernelGGL((k_cross_backward_kv<T, DP, 32, 4, BIAS>), grid, dim3(256), 0, s, a, ktiles);
+            hipLaunchKernelGGL((k_cross_backward_kv<T, DP, 32, 4, false, BIAS>), grid, dim3(256), 0, s, a, ktiles);
             return hipGetLastError();
         }
-    hipLaunchKernelGGL((k_cross_backward_kv<T, DP, 32, 1, BIAS>), grid, dim3(256), 0, s, a, ktiles);
+    hipLaunchKernelGGL((k_cross_backward_kv<T, DP, 32, 1, kTwo, BIAS>), grid, dim3(kTwo ? 512 : 256), 0, s, a, ktiles);
     return hipGetLastError();
 }
 
