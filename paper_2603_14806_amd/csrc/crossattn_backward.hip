@@ -490,63 +490,79 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const Cro
     const int slot_h = (int)(slot - slot_b * slot_heads);
     const int k0 = kt_ * KC, qw = qt_ * 128 + 32 * w;
     const bool wave_live = qw < a.nq, valid = qw + ql < a.nq;
-    const int qi = min(qw + ql, a.nq - 1);
+    const int qi = qw + ql;
     const int e0 = (int)((int64_t)shared * split / a.splits), e1 = (int)((int64_t)shared * (split + 1) / a.splits);
 
-    BiasRow<T, KC> bias;
-    bias.init(a, slot_b, slot_h, min(qw, a.nq - 1), min(qw + 31, a.nq - 1), qi, hi);
-    bias.load(k0, a.nk);
-    f32x16_t acc[NB];
+    f32x16_t bv[NB], acc[NB];               // the lane's bias, the same for all entries and heads here, and its gradient
+    {
+        BiasRow<T, KC> bias;
+        bias.init(a, slot_b, slot_h, min(qw, a.nq - 1), min(qw + 31, a.nq - 1), min(qw + ql, a.nq - 1), hi);
+        bias.load(k0, a.nk);
 #pragma unroll
-    for (int n = 0; n < NB; ++n)
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[n][r] = 0.f;
+            for (int g = 0; g < 4; ++g) {
+                const float4 x = bias.get(n, g);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    bv[n][4 * g + e] = f4_get(x, e);
+                    acc[n][4 * g + e] = 0.f;
+                }
+            }
+    }
 
     TL tl;
     tl.init(lane);
     Part<T, DP, KC, 256> kp, vp;
     KeyByte kbyte;
+    RowFrags<T, DP> qf, gf;
     kp.init(a.k.token, a.d, t);
     vp.init(a.v.token, a.d, t);
-    Frag<T> qf[NS], gf[NS];
+    qf.init(a.q.token, lane);
+    gf.init(a.dout.token, lane);
     float sm = 0.f, sl = 0.f, D = 0.f;
     const int64_t rows = a.batch * a.heads * a.nq;
-    // entry and head of the e-th of those that share this bias: heads innermost
-    auto load_keys = [&](int e) {
-        const int64_t b = slot_b + e / shared_heads;
-        const int hk = (slot_h + e % shared_heads) / (a.group * a.key_div);
-        kp.load((const T*)a.k.data + b * a.k.batch + hk * a.k.head, a.k.token, k0, a.nk, a.d);
-        vp.load((const T*)a.v.data + b * a.v.batch + hk * a.v.head, a.v.token, k0, a.nk, a.d);
-        kbyte.load(a.mask ? a.mask + b * a.mask_batch : nullptr, k0, a.nk, lane);
+    const int rows_left = max(a.nq - qw, 0), per_key = a.group * a.key_div;
+    // the e-th entry and head of those that share this bias, heads innermost
+    struct At {
+        int64_t b;
+        int h;
     };
-    auto load_queries = [&](int e) {
-        const int64_t b = slot_b + e / shared_heads;
-        const int h = slot_h + e % shared_heads;
-        const T* qr = (const T*)a.q.data + b * a.q.batch + (int64_t)qi * a.q.token + h * a.q.head;
-        const T* gr = (const T*)a.dout.data + b * a.dout.batch + (int64_t)qi * a.dout.token + h * a.dout.head;
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            load_row(qr, s, hi, a.d, qf[s]);
-            load_row(gr, s, hi, a.d, gf[s]);
+    auto next = [&](At& at) {
+        if (++at.h == slot_h + shared_heads) {
+            at.h = slot_h;
+            ++at.b;
         }
-        const int64_t row = (b * a.heads + h) * a.nq + qi;
-        sm = a.stats[row];
-        sl = a.stats[rows + row];
-        D = a.delta[row];
     };
-    if (e0 < e1) {
-        load_keys(e0);
-        load_queries(e0);
-    }
+    auto load_keys = [&](const At& at, bool any) {
+        const int hk = at.h / per_key, n = any ? a.nk : 0;
+        kp.load((const T*)a.k.data + at.b * a.k.batch + hk * a.k.head, a.k.token, k0, n, a.d);
+        vp.load((const T*)a.v.data + at.b * a.v.batch + hk * a.v.head, a.v.token, k0, n, a.d);
+        kbyte.load(a.mask && any ? a.mask + at.b * a.mask_batch : nullptr, k0, n, lane);
+    };
+    auto load_queries = [&](const At& at, bool any) {
+        const int n = any ? rows_left : 0;
+        qf.load((const T*)a.q.data + at.b * a.q.batch + (int64_t)qw * a.q.token + at.h * a.q.head, a.q.token, n, a.d, hi);
+        gf.load((const T*)a.dout.data + at.b * a.dout.batch + (int64_t)qw * a.dout.token + at.h * a.dout.head, a.dout.token, n, a.d, hi);
+        const int64_t row = (at.b * a.heads + at.h) * a.nq + qw;      // rows past the last read zero: a weight of 0
+        const uint32_t bytes = 4u * (uint32_t)min(n, 32);
+        sm = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(make_rsrc(a.stats + row, bytes), 4 * ql, 0, 0));
+        sl = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(make_rsrc(a.stats + rows + row, bytes), 4 * ql, 0, 0));
+        D = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(make_rsrc(a.delta + row, bytes), 4 * ql, 0, 0));
+    };
+    At at{slot_b + e0 / shared_heads, slot_h + e0 % shared_heads};
+    load_keys(at, e0 < e1);
+    load_queries(at, e0 < e1);
     for (int e = e0; e < e1; ++e) {
         char* kt = mem + ((e - e0) & 1) * 2 * TL::kBytes;
         char* vt = kt + TL::kBytes;
         uint64_t bits = kbyte.bits(a.mask, k0, a.nk, lane);
         if (KC == 32) bits &= 0xffffffffull;
-        const bool some = bits != (KC == 64 ? ~0ull : 0xffffffffull);
+        const bool some = bits != (KC == 64 ? ~0ull : 0xffffffffull), more = e + 1 < e1;
         kp.stage(kt, t, some, bits);
         vp.stage(vt, t, some, bits);
-        load_keys(min(e + 1, e1 - 1));
+        next(at);
+        load_keys(at, more);
         __syncthreads();
         if (bits != 0 && wave_live) {
             RowStat st;
@@ -562,17 +578,20 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const Cro
                 for (int i = 0; i < NS; ++i) {
                     Frag<T> f;
                     tl.rows(kt, n, i, f);
-                    s[n] = mma(f, qf[i], s[n]);
+                    s[n] = mma(f, qf.f[i], s[n]);
                 }
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
                     Frag<T> f;
                     tl.rows(vt, n, i, f);
-                    dp[n] = mma(f, gf[i], dp[n]);
+                    dp[n] = mma(f, gf.f[i], dp[n]);
                 }
             }
-            load_queries(min(e + 1, e1 - 1));
-            add_bias<T, KC>(s, bias, a.scale);
+            load_queries(at, more);
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[n][r] = __builtin_fmaf(s[n][r], a.scale, bv[n][r]);
             if (some) drop_absent<NB>(s, (uint32_t)(bits >> ((KC / 2) * hi)));
             float sh = st.sh;
             if (far) {
@@ -585,7 +604,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const Cro
                 for (int r = 0; r < 16; ++r)
                     acc[n][r] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], kLog2e, sh)), dp[n][r] - Dn, acc[n][r]);
         } else {
-            load_queries(min(e + 1, e1 - 1));
+            load_queries(at, more);
         }
     }
     if (!valid) return;
