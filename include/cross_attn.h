@@ -86,7 +86,7 @@ int cross_attn_forward(const cross_attn_view_t* v, const cross_attn_tensor_t* q,
                        const cross_attn_tensor_t* vv, const cross_attn_tensor_t* out, float* stats, void* ws,
                        size_t ws_bytes, void* stream);
 
-/* Bytes of the workspace of cross_attn_backward (one fp32 value per query and
+/* Bytes of the workspace of cross_attn_backward (four fp32 values per query and
  * head, and the partial sums of dbias where few tiles of a bias are shared by
  * many entries or heads). */
 int cross_attn_backward_workspace_size(const cross_attn_view_t* v, size_t* bytes);

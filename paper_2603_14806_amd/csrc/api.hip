@@ -1306,8 +1306,8 @@ int cross_workspace(const void* ws, size_t ws_bytes, size_t need) {
     return TRI_MUL_OK;
 }
 
-// The backward's workspace: D of every query and head, then the partial sums of dbias.
-size_t cross_delta_bytes(const cross_attn_view_t* v) { return round256((size_t)v->batch * v->heads * v->nq * 4); }
+// The backward's workspace: four values of every query and head, then the partial sums of dbias.
+size_t cross_rows_bytes(const cross_attn_view_t* v) { return round256((size_t)v->batch * v->heads * v->nq * 16); }
 int cross_bias_splits(const cross_attn_view_t* v) {
     return v->bias.data ? trimul::cross_dbias_splits(v->dtype, cross_slots(v), cross_shared(v), v->nq, v->nk) : 1;
 }
@@ -1349,7 +1349,7 @@ int cross_attn_forward(const cross_attn_view_t* v, const cross_attn_tensor_t* q,
 int cross_attn_backward_workspace_size(const cross_attn_view_t* v, size_t* bytes) {
     if (int rc = cross_check(v)) return rc;
     if (!bytes) return fail(TRI_MUL_EINVAL, "null bytes pointer");
-    *bytes = cross_delta_bytes(v) + trimul::cross_dbias_part_floats(v->dtype, cross_bias_splits(v), cross_slots(v), v->nq, v->nk) * 4;
+    *bytes = cross_rows_bytes(v) + trimul::cross_dbias_part_floats(v->dtype, cross_bias_splits(v), cross_slots(v), v->nq, v->nk) * 4;
     return ok();
 }
 
@@ -1394,8 +1394,8 @@ int cross_attn_backward(const cross_attn_view_t* v, const cross_attn_tensor_t* q
     a.dv = cross_arg(dv);
     if (dbias) a.dbias = {dbias->data, dbias->batch, dbias->head, dbias->row};
     a.stats = const_cast<float*>(stats);
-    a.delta = static_cast<float*>(ws);
-    a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + cross_delta_bytes(v));
+    a.rows = static_cast<float*>(ws);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + cross_rows_bytes(v));
     a.splits = splits;
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = hipSuccess;

@@ -16,13 +16,15 @@ namespace trimul {
 namespace {
 
 // A query's statistics as the weights use them: P = exp2((x - M) log2 e + n2) = exp2(x log2 e + sh).
-// A query with no key: M = 0, n2 = -inf, P = 0.
+// A query with no key: M = 0, n2 = -inf, P = 0.  The query pass leaves them, and D, in the workspace
+// for the other two.
 struct RowStat {
-    float M, n2, sh;
-    __device__ __forceinline__ void set(float m, float l) {
+    float M, n2, sh, D;
+    __device__ __forceinline__ void set(float m, float l, float d) {
         M = l == 0.f ? 0.f : m;
         n2 = l == 0.f ? -INFINITY : -__builtin_amdgcn_logf(l);
         sh = __builtin_fmaf(-M, kLog2e, n2);
+        D = d;
     }
     __device__ __forceinline__ bool far() const { return !(fabsf(M * kLog2e) <= kFmaMax); }
 };
@@ -100,10 +102,10 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
             D += Frag<T>::dot(gf[s], of);
         }
         D += xor32(D);
-        if (valid && !hi && (WK == 1 || w == 0)) a.delta[row] = D;
     }
     RowStat st;
-    st.set(a.stats[row], a.stats[a.batch * a.heads * a.nq + row]);
+    st.set(a.stats[row], a.stats[a.batch * a.heads * a.nq + row], D);
+    if (valid && !hi && (WK == 1 || w == 0)) reinterpret_cast<float4*>(a.rows)[row] = make_float4(st.M, st.n2, st.sh, D);
     const bool far = __any(st.far());
     const float coef = BIAS ? kLog2e : a.scale * kLog2e;
     const T* kb = (const T*)a.k.data + b * a.k.batch + hk / a.key_div * a.k.head;
@@ -286,8 +288,7 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
             const int u = t + NT * i, k = key0 + (u % kBPieces) * TL::kPer;
             boff[i] = k < a.nk ? (uint32_t)(u / kBPieces) * (uint32_t)(a.bias.row * (int)sizeof(T)) + 16 * (u % kBPieces) : 0xfffffff0u;
         }
-    float sm = 0.f, sl = 0.f, sd = 0.f;
-    const int64_t rows = a.batch * a.heads * a.nq;
+    float4 row4 = make_float4(0.f, 0.f, 0.f, 0.f);              // the statistics of row lane % QC of the chunk
     int next_h = hk * group, next_q = WK == 1 ? 0 : w * QC;   // the chunk that load() takes
     auto wrap = [&]() {
         while (next_q >= per_head * QC) {
@@ -307,10 +308,8 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
             for (int i = 0; i < kBN; ++i) bp[i] = buf_load16(r, boff[i]);
         }
         const int qi = next_q + (lane & (QC - 1));
-        const int64_t row = (b * a.heads + h) * a.nq + min(qi, a.nq - 1);
-        sm = a.stats[row];
-        sl = qi < a.nq ? a.stats[rows + row] : 0.f;             // rows past the last have weight 0
-        sd = a.delta[row];
+        row4 = reinterpret_cast<const float4*>(a.rows)[(b * a.heads + h) * a.nq + min(qi, a.nq - 1)];
+        if (qi >= a.nq) row4.y = row4.z = -INFINITY;           // rows past the last have weight 0
         next_q += WK * QC;
         wrap();
     };
@@ -332,14 +331,12 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
                 const int u = t + NT * i;
                 *reinterpret_cast<uint4*>(bt + (u / kBPieces) * kBRow + (u % kBPieces) * 16) = bp[i];
             }
-        RowStat st;
-        st.set(sm, sl);
-        const bool far = __any(st.far());
+        const bool far = __any(!(fabsf(row4.x * kLog2e) <= kFmaMax));
         if ((WK > 1 || wid == 0) && lane < QC) {
-            stat[buf][0][lane] = st.M;
-            stat[buf][1][lane] = st.n2;
-            stat[buf][2][lane] = st.sh;
-            stat[buf][3][lane] = sd;
+            stat[buf][0][lane] = row4.x;
+            stat[buf][1][lane] = row4.y;
+            stat[buf][2][lane] = row4.z;
+            stat[buf][3][lane] = row4.w;
         }
         load();
         if (WK == 1) __syncthreads();
@@ -515,13 +512,13 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const Cro
     tl.init(lane);
     Part<T, DP, KC, 256> kp, vp;
     KeyByte kbyte;
-    RowFrags<T, DP> qf, gf;
+    RowFrags<T, DP> qn, gn;                 // the next entry's; this one's are copied out
+    Frag<T> qf[NS], gf[NS];
     kp.init(a.k.token, a.d, t);
     vp.init(a.v.token, a.d, t);
-    qf.init(a.q.token, lane);
-    gf.init(a.dout.token, lane);
-    float sm = 0.f, sl = 0.f, D = 0.f;
-    const int64_t rows = a.batch * a.heads * a.nq;
+    qn.init(a.q.token, lane);
+    gn.init(a.dout.token, lane);
+    float4 row4;
     const int rows_left = max(a.nq - qw, 0), per_key = a.group * a.key_div;
     // the e-th entry and head of those that share this bias, heads innermost
     struct At {
@@ -542,13 +539,10 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const Cro
     };
     auto load_queries = [&](const At& at, bool any) {
         const int n = any ? rows_left : 0;
-        qf.load((const T*)a.q.data + at.b * a.q.batch + (int64_t)qw * a.q.token + at.h * a.q.head, a.q.token, n, a.d, hi);
-        gf.load((const T*)a.dout.data + at.b * a.dout.batch + (int64_t)qw * a.dout.token + at.h * a.dout.head, a.dout.token, n, a.d, hi);
-        const int64_t row = (at.b * a.heads + at.h) * a.nq + qw;      // rows past the last read zero: a weight of 0
-        const uint32_t bytes = 4u * (uint32_t)min(n, 32);
-        sm = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(make_rsrc(a.stats + row, bytes), 4 * ql, 0, 0));
-        sl = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(make_rsrc(a.stats + rows + row, bytes), 4 * ql, 0, 0));
-        D = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(make_rsrc(a.delta + row, bytes), 4 * ql, 0, 0));
+        qn.load((const T*)a.q.data + at.b * a.q.batch + (int64_t)qw * a.q.token + at.h * a.q.head, a.q.token, n, a.d, hi);
+        gn.load((const T*)a.dout.data + at.b * a.dout.batch + (int64_t)qw * a.dout.token + at.h * a.dout.head, a.dout.token, n, a.d, hi);
+        row4 = __builtin_bit_cast(float4, buf_load16(make_rsrc(reinterpret_cast<const float4*>(a.rows) + (at.b * a.heads + at.h) * a.nq + qw,
+                                                               16u * (uint32_t)min(n, 32)), 16 * ql));
     };
     At at{slot_b + e0 / shared_heads, slot_h + e0 % shared_heads};
     load_keys(at, e0 < e1);
@@ -563,12 +557,16 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const Cro
         vp.stage(vt, t, some, bits);
         next(at);
         load_keys(at, more);
+        const RowStat st{row4.x, row4.y, row4.z, row4.w};
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            qf[i] = qn.f[i];
+            gf[i] = gn.f[i];
+        }
+        load_queries(at, more);
         __syncthreads();
         if (bits != 0 && wave_live) {
-            RowStat st;
-            st.set(sm, sl);
             const bool far = __any(st.far());
-            const float Dn = D;
             f32x16_t s[NB], dp[NB];
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
@@ -578,16 +576,15 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const Cro
                 for (int i = 0; i < NS; ++i) {
                     Frag<T> f;
                     tl.rows(kt, n, i, f);
-                    s[n] = mma(f, qf.f[i], s[n]);
+                    s[n] = mma(f, qf[i], s[n]);
                 }
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
                     Frag<T> f;
                     tl.rows(vt, n, i, f);
-                    dp[n] = mma(f, gf.f[i], dp[n]);
+                    dp[n] = mma(f, gf[i], dp[n]);
                 }
             }
-            load_queries(at, more);
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -602,9 +599,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const Cro
             for (int n = 0; n < NB; ++n)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    acc[n][r] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], kLog2e, sh)), dp[n][r] - Dn, acc[n][r]);
-        } else {
-            load_queries(at, more);
+                    acc[n][r] = __builtin_fmaf(__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], kLog2e, sh)), dp[n][r] - st.D, acc[n][r]);
         }
     }
     if (!valid) return;
