@@ -1381,7 +1381,7 @@ int cross_attn_backward(const cross_attn_view_t* v, const cross_attn_tensor_t* q
     const int splits = cross_bias_splits(v);
     const int64_t bh = v->batch * cross_col_heads(v);
     if (bh > kMaxGroups || bh * ((cross_cols(v) + 127) / 128) > kMaxGroups || bh * ((v->nk + 127) / 128) > kMaxGroups ||
-        (dbias && (cross_slots(v) > kMaxGroups || cross_slots(v) * splits * ((v->nq + 127) / 128) > kMaxGroups ||
+        (dbias && cross_shared(v) != 1 && (cross_slots(v) > kMaxGroups || cross_slots(v) * splits * ((v->nq + 127) / 128) > kMaxGroups ||
                    cross_slots(v) * splits * ((v->nq + 127) / 128) * ((v->nk + 31) / 32) > kMaxGroups)))
         return fail(TRI_MUL_EUNSUPPORTED, "too many entries, heads, queries and keys for one call");
     size_t need = 0;
@@ -1393,6 +1393,7 @@ int cross_attn_backward(const cross_attn_view_t* v, const cross_attn_tensor_t* q
     a.dk = cross_arg(dk);
     a.dv = cross_arg(dv);
     if (dbias) a.dbias = {dbias->data, dbias->batch, dbias->head, dbias->row};
+    a.direct_bias = dbias && cross_shared(v) == 1;
     a.stats = const_cast<float*>(stats);
     a.rows = static_cast<float*>(ws);
     a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + cross_rows_bytes(v));
@@ -1401,7 +1402,8 @@ int cross_attn_backward(const cross_attn_view_t* v, const cross_attn_tensor_t* q
     hipError_t e = hipSuccess;
     if (queries) e = trimul::launch_cross_backward_q(v->dtype, a, s);
     if (e == hipSuccess && dk && v->batch > 0 && v->nk > 0) e = trimul::launch_cross_backward_kv(v->dtype, a, s);
-    if (e == hipSuccess && dbias && v->nq > 0 && v->nk > 0 && cross_slots(v) > 0) e = trimul::launch_cross_backward_bias(v->dtype, a, s);
+    if (e == hipSuccess && dbias && !a.direct_bias && v->nq > 0 && v->nk > 0 && cross_slots(v) > 0)
+        e = trimul::launch_cross_backward_bias(v->dtype, a, s);
     if (e != hipSuccess) return hip_fail(e, "attention backward kernel launch");
     return ok();
 }

@@ -85,6 +85,28 @@ __device__ __forceinline__ void take8(const f32x16_t& s, int t, Frag<float>& f) 
     for (int e = 0; e < 8; ++e) f.v[e] = s[8 * t + e];
 }
 
+// The values of a fragment to memory (16-byte aligned), the first n of them.
+__device__ __forceinline__ void store8(bf16_t* p, const Frag<bf16_t>& f, int n) {
+    if (n >= 8) {
+        *reinterpret_cast<uint4*>(p) = f.u;
+    } else {
+        const uint32_t w[4] = {f.u.x, f.u.y, f.u.z, f.u.w};
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < n) p[e] = (bf16_t)(w[e >> 1] >> (16 * (e & 1)));
+    }
+}
+__device__ __forceinline__ void store8(float* p, const Frag<float>& f, int n) {
+    if (n >= 8) {
+        reinterpret_cast<float4*>(p)[0] = make_float4(f.v[0], f.v[1], f.v[2], f.v[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(f.v[4], f.v[5], f.v[6], f.v[7]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < n) p[e] = f.v[e];
+    }
+}
+
 // A fragment of one token's channels straight from memory: values 16 s2 + 8 hi
 // .. + 7 of a row of d channels (zero past d).
 __device__ __forceinline__ void load_row(const bf16_t* row, int s2, int hi, int d, Frag<bf16_t>& f) {

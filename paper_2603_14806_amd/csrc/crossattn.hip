@@ -288,14 +288,15 @@ hipError_t forward(const CrossArgs& a, const CrossPlan& p, hipStream_t s) {
 
 }  // namespace
 
-// 128 columns to a work-group where that makes two work-groups for each of the
-// 256 compute units; else 32, its waves on different keys.  Where even that
-// leaves compute units without two, the keys are split, as long as a
-// split keeps 256 keys (two chunks a wave).
+// 128 columns to a work-group where that makes one for each compute unit; else
+// 32, its waves on different keys.  Where even that leaves compute units
+// without one, the keys are split, for two on each, as long as a split
+// keeps 256 keys (two chunks a wave).  (Joining the splits of many rows costs
+// more than they bring: 13 us for 20800 rows of d = 24.)
 CrossPlan cross_plan(int64_t batch, int kv_heads, int64_t cols, int64_t nk) {
     CrossPlan p{cross_few(batch * kv_heads, cols) ? 32 : 128, 1, (int)((nk + 63) / 64 * 64)};
     const int64_t groups = batch * kv_heads * ((cols + p.cols - 1) / p.cols);
-    if (groups > 0 && groups < 512) {
+    if (groups > 0 && groups < 256) {
         int64_t n = (512 + groups - 1) / groups;
         if (n > nk / 256) n = nk / 256;
         if (n > kCrossMaxSplits) n = kCrossMaxSplits;

@@ -62,6 +62,7 @@ __device__ __forceinline__ void take_from(f32x16_t (&s)[NB], float scale, float 
 //
 // The forward's layout (lane: one column, registers: keys): WK = 1, 32 columns
 // a wave, or WK = 4, 32 columns a work-group and its waves on different keys.
+// A bias that no other entry or head shares gets its gradient, dS, from here.
 template <typename T, int DP, int WK>
 constexpr int q_waves() {
     if (WK > 1) return sizeof(T) == 2 ? (DP == 32 ? 3 : DP == 64 ? 2 : 1) : (DP == 32 ? 2 : 1);
@@ -112,6 +113,7 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
     const T* vb = (const T*)a.v.data + b * a.v.batch + hk / a.key_div * a.v.head;
     const uint8_t* mask = a.mask ? a.mask + b * a.mask_batch : nullptr;
     const int nchunks = (a.nk + KC - 1) / KC;
+    T* const drow = BIAS && a.direct_bias ? (T*)a.dbias.data + b * a.dbias.batch + h * a.dbias.head + (int64_t)qi * a.dbias.row : nullptr;
 
     f32x16_t acc[ND];
 #pragma unroll
@@ -190,6 +192,10 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
                 for (int tt = 0; tt < 2; ++tt) {
                     Frag<T> pf;
                     take8(s[n], tt, pf);
+                    if (BIAS && a.direct_bias) {
+                        const int k = c * KC + (KC / 2) * hi + 16 * n + 8 * tt;
+                        if (valid) store8(drow + k, pf, a.nk - k);
+                    }
 #pragma unroll
                     for (int i = 0; i < ND; ++i) {
                         Frag<T> kf;
@@ -199,6 +205,15 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
                 }
         } else if (BIAS) {
             bp.load((c + WK) * KC, a.nk);
+            if (a.direct_bias && valid) {                      // no key here: dS is 0
+                Frag<T> z;
+                z.zero();
+#pragma unroll
+                for (int i = 0; i < KC / 16; ++i) {
+                    const int k = c * KC + (KC / 2) * hi + 8 * i;
+                    store8(drow + k, z, a.nk - k);
+                }
+            }
         }
     }
     if constexpr (WK > 1) {
@@ -465,8 +480,8 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
 
 // ------------------------------------------------------------------ dbias
 //
-// One work-group: 128 queries x KC keys of one bias (the query pass's layout), its loop over the
-// entries and heads that share the bias (a split of them: the sums of the splits are added by
+// A bias that several entries or heads share.  One work-group: 128 queries x KC keys of it (the query
+// pass's layout), its loop over the entries and heads that share it (a split of them: the sums of the splits are added by
 // k_cross_dbias_sum).
 template <typename T, int DP, int KC>
 __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const CrossArgs a, int slot_heads, int shared_heads, int shared,

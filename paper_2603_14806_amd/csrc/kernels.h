@@ -212,6 +212,7 @@ struct CrossArgs {
     int nq, nk, heads, kv_heads, group, d;
     int key_div;       // key head of kv_heads' hk: hk / key_div (1, unless query heads that share one are taken singly)
     float scale;
+    int direct_bias;          // the query pass writes dbias: no other entry or head shares it
     int splits, split_keys;   // forward: key ranges [s * split_keys, ...); dbias: splits of the shared entries
 };
 // How a forward call is laid out: columns per work-group (32: the four waves
@@ -220,8 +221,10 @@ constexpr int kCrossMaxSplits = 64;   // one lane of the join each
 struct CrossPlan {
     int cols, splits, split_keys;
 };
-// Whether tiles of 128 columns (or keys) are too few: below two for each of the 256 compute units.
-inline bool cross_few(int64_t heads, int64_t n) { return heads * ((n + 127) / 128) < 512; }
+// Whether tiles of 128 columns (or keys) are too few: below one for each of the
+// 256 compute units.  (16 heads of d = 24 with bias: 2600 columns, 336 tiles, 31 us
+// in tiles of 128 and 47 in tiles of 32; 1300, 176 tiles, 28 and 27.)
+inline bool cross_few(int64_t heads, int64_t n) { return heads * ((n + 127) / 128) < 256; }
 CrossPlan cross_plan(int64_t batch, int kv_heads, int64_t cols, int64_t nk);
 size_t cross_part_floats(const CrossPlan& p, int64_t batch, int64_t nq, int heads, int d);
 // Splits of the dbias pass over `shared` entries and heads per bias.
