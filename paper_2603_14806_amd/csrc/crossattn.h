@@ -123,35 +123,6 @@ __device__ __forceinline__ void load_row(const float* row, int s2, int hi, int d
     for (int e = 0; e < 8; ++e) f.v[e] = c < d ? v[e] : 0.f;
 }
 
-// The fragments of 32 consecutive tokens' rows (lane l: row l % 32) as a B
-// operand, through a descriptor of the rows that exist; rows past them and
-// channels past d are zero.
-template <typename T, int DP>
-struct RowFrags {
-    static constexpr int NS = DP / 16;
-    uint32_t off;        // of the lane's row and half
-    Frag<T> f[NS];
-    __device__ __forceinline__ void init(int64_t stride, int lane) {
-        off = (uint32_t)(lane & 31) * (uint32_t)(stride * (int)sizeof(T)) + (lane >> 5) * 8 * (int)sizeof(T);
-    }
-    // n rows at base (uniform)
-    __device__ __forceinline__ void load(const T* base, int64_t stride, int n, int d, int hi) {
-        const auto r = make_rsrc(base, n > 0 ? (uint32_t)((min(n, 32) - 1) * (uint32_t)stride + d) * (uint32_t)sizeof(T) : 0u);
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            const uint32_t o = 16 * s + 8 * hi < d ? off + 16 * s * (int)sizeof(T) : 0xffffffe0u;
-            if constexpr (sizeof(T) == 2) {
-                f[s].u = buf_load16(r, o);
-            } else {
-                const float4 x = __builtin_bit_cast(float4, buf_load16(r, o)), y = __builtin_bit_cast(float4, buf_load16(r, o + 16));
-                const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[s].v[e] = v[e];
-            }
-        }
-    }
-};
-
 template <typename T, int DP, int KC>
 struct Tile {
     static constexpr int kRowBytes = DP * (int)sizeof(T);
@@ -191,6 +162,17 @@ struct Tile {
     __device__ __forceinline__ void rows(const char* t, int b, int s2, Frag<float>& f) const {
         const float4 x = *reinterpret_cast<const float4*>(t + (ar ^ (s2 << 6)) + b * 16 * kRowBytes);
         const float4 y = *reinterpret_cast<const float4*>(t + (ar ^ (s2 << 6) ^ 16) + b * 16 * kRowBytes);
+        const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f.v[e] = v[e];
+    }
+    // One row's channels 16 s2 + 8 hi .. (rows in their own order)
+    static __device__ __forceinline__ void row(const char* t, int r, int hi, int s2, Frag<bf16_t>& f) {
+        f.u = *reinterpret_cast<const uint4*>(t + off(r, 2 * s2 + hi));
+    }
+    static __device__ __forceinline__ void row(const char* t, int r, int hi, int s2, Frag<float>& f) {
+        const float4 x = *reinterpret_cast<const float4*>(t + off(r, 4 * s2 + 2 * hi));
+        const float4 y = *reinterpret_cast<const float4*>(t + off(r, 4 * s2 + 2 * hi + 1));
         const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
         for (int e = 0; e < 8; ++e) f.v[e] = v[e];

@@ -250,7 +250,7 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
     constexpr int kBPieces = KT * (int)sizeof(T) / 16, kBN = QC * kBPieces / NT;
     __shared__ __align__(16) char mem[BUF * 2 * TL::kBytes];
     __shared__ __align__(16) char bmem[BIAS ? BUF * QC * kBRow : 16];
-    __shared__ __align__(16) float stat[BUF][4][QC];           // M, n2, sh, D of a chunk's columns
+    __shared__ __align__(16) float stat[BUF][4][QC];           // M, n2, sh, -D of a chunk's columns
     const int lane = threadIdx.x & 63, kl = lane & 31, hi = lane >> 5;
     const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = WK == 1 ? threadIdx.x : lane;
     const int w = TWO ? wid & 3 : wid;
@@ -351,12 +351,13 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
             stat[buf][0][lane] = row4.x;
             stat[buf][1][lane] = row4.y;
             stat[buf][2][lane] = row4.z;
-            stat[buf][3][lane] = row4.w;
+            stat[buf][3][lane] = -row4.w;
         }
         load();
         if (WK == 1) __syncthreads();
         else wave_sync();
         if (!wave_live) continue;
+        const int lr = (QC / 2) * hi;                          // the lane's first tile row
         f32x16_t s[NB], dp[NB];
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
@@ -368,15 +369,21 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
                 tl.rows(qt, n, i, f);
                 s[n] = mma(f, kf[i], s[n]);
             }
-            if (!TWO || for_k)
+            if (!TWO || for_k) {                               // dP - D: the sum starts at -D
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 d4 = *reinterpret_cast<const float4*>(&stat[buf][3][lr + 16 * n + 4 * g]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) dp[n][4 * g + e] = f4_get(d4, e);
+                }
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
                     Frag<T> f;
                     tl.rows(gt, n, i, f);
                     dp[n] = mma(f, vf[i], dp[n]);
                 }
+            }
         }
-        const int lr = (QC / 2) * hi;                          // the lane's first tile row
         if constexpr (BIAS) {
 #pragma unroll
             for (int n = 0; n < NB; ++n)
@@ -430,14 +437,9 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const float4 d4 = *reinterpret_cast<const float4*>(&stat[buf][3][lr + 16 * n + 4 * g]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float ds = s[n][4 * g + e] * (dp[n][4 * g + e] - f4_get(d4, e));
-                        if (TWO) s[n][4 * g + e] = ds;
-                        else dp[n][4 * g + e] = ds;
-                    }
+                for (int r = 0; r < 16; ++r) {
+                    if (TWO) s[n][r] *= dp[n][r];
+                    else dp[n][r] *= s[n][r];
                 }
         const char* vt = TWO && for_k ? qt : gt;
 #pragma unroll
@@ -484,11 +486,14 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
 // pass's layout), its loop over the entries and heads that share it (a split of them: the sums of the splits are added by
 // k_cross_dbias_sum).
 template <typename T, int DP, int KC>
-__global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const CrossArgs a, int slot_heads, int shared_heads, int shared,
+__global__ __launch_bounds__(256, DP == 32 || (DP == 64 && sizeof(T) == 2) ? 2 : 1) void k_cross_dbias(const CrossArgs a, int slot_heads, int shared_heads, int shared,
                                                      int qtiles, int ktiles) {
     using TL = Tile<T, DP, KC>;
     constexpr int NB = KC / 32, NS = DP / 16, kPer = 16 / (int)sizeof(T);
-    __shared__ __align__(16) char mem[2 * 2 * TL::kBytes];
+    using QL = Tile<T, DP, 32>;
+    constexpr int BUF = sizeof(T) == 4 && DP == 128 ? 1 : 2;   // buffers of keys (a second does not fit 160 KB there)
+    __shared__ __align__(16) char mem[BUF * 2 * TL::kBytes];
+    __shared__ __align__(16) char qmem[4][2 * QL::kBytes];     // a wave's 32 queries: q and dout
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), ql = lane & 31, hi = lane >> 5;
 
     int64_t blk = xcd_block();
@@ -527,12 +532,13 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const Cro
     tl.init(lane);
     Part<T, DP, KC, 256> kp, vp;
     KeyByte kbyte;
-    RowFrags<T, DP> qn, gn;                 // the next entry's; this one's are copied out
-    Frag<T> qf[NS], gf[NS];
+    // q and dout as whole rows, and the fragments through LDS: loaded as fragments, each load would touch 32 rows for
+    // 32 bytes of each
+    Part<T, DP, 32, 64> qn, gn;
     kp.init(a.k.token, a.d, t);
     vp.init(a.v.token, a.d, t);
-    qn.init(a.q.token, lane);
-    gn.init(a.dout.token, lane);
+    qn.init(a.q.token, a.d, lane);
+    gn.init(a.dout.token, a.d, lane);
     float4 row4;
     const int rows_left = max(a.nq - qw, 0), per_key = a.group * a.key_div;
     // the e-th entry and head of those that share this bias, heads innermost
@@ -554,8 +560,8 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const Cro
     };
     auto load_queries = [&](const At& at, bool any) {
         const int n = any ? rows_left : 0;
-        qn.load((const T*)a.q.data + at.b * a.q.batch + (int64_t)qw * a.q.token + at.h * a.q.head, a.q.token, n, a.d, hi);
-        gn.load((const T*)a.dout.data + at.b * a.dout.batch + (int64_t)qw * a.dout.token + at.h * a.dout.head, a.dout.token, n, a.d, hi);
+        qn.load((const T*)a.q.data + at.b * a.q.batch + (int64_t)qw * a.q.token + at.h * a.q.head, a.q.token, 0, n, a.d);
+        gn.load((const T*)a.dout.data + at.b * a.dout.batch + (int64_t)qw * a.dout.token + at.h * a.dout.head, a.dout.token, 0, n, a.d);
         row4 = __builtin_bit_cast(float4, buf_load16(make_rsrc(reinterpret_cast<const float4*>(a.rows) + (at.b * a.heads + at.h) * a.nq + qw,
                                                                16u * (uint32_t)min(n, 32)), 16 * ql));
     };
@@ -563,41 +569,47 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void k_cross_dbias(const Cro
     load_keys(at, e0 < e1);
     load_queries(at, e0 < e1);
     for (int e = e0; e < e1; ++e) {
-        char* kt = mem + ((e - e0) & 1) * 2 * TL::kBytes;
+        char* kt = mem + (BUF == 2 ? (e - e0) & 1 : 0) * 2 * TL::kBytes;
         char* vt = kt + TL::kBytes;
         uint64_t bits = kbyte.bits(a.mask, k0, a.nk, lane);
         if (KC == 32) bits &= 0xffffffffull;
         const bool some = bits != (KC == 64 ? ~0ull : 0xffffffffull), more = e + 1 < e1;
+        if (BUF == 1) __syncthreads();
         kp.stage(kt, t, some, bits);
         vp.stage(vt, t, some, bits);
         next(at);
         load_keys(at, more);
         const RowStat st{row4.x, row4.y, row4.z, row4.w};
-#pragma unroll
-        for (int i = 0; i < NS; ++i) {
-            qf[i] = qn.f[i];
-            gf[i] = gn.f[i];
-        }
+        wave_sync();
+        qn.stage(qmem[w], lane, false, 0);
+        gn.stage(qmem[w] + QL::kBytes, lane, false, 0);
         load_queries(at, more);
         __syncthreads();
         if (bits != 0 && wave_live) {
             const bool far = __any(st.far());
             f32x16_t s[NB], dp[NB];
 #pragma unroll
-            for (int n = 0; n < NB; ++n) {
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[n][r] = dp[n][r] = 0.f;
 #pragma unroll
-                for (int i = 0; i < NS; ++i) {
-                    Frag<T> f;
-                    tl.rows(kt, n, i, f);
-                    s[n] = mma(f, qf[i], s[n]);
-                }
+            for (int i = 0; i < NS; ++i) {
+                Frag<T> q, f;
+                QL::row(qmem[w], ql, hi, i, q);
 #pragma unroll
-                for (int i = 0; i < NS; ++i) {
-                    Frag<T> f;
+                for (int n = 0; n < NB; ++n) {
+                    tl.rows(kt, n, i, f);
+                    s[n] = mma(f, q, s[n]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                Frag<T> g, f;
+                QL::row(qmem[w] + QL::kBytes, ql, hi, i, g);
+#pragma unroll
+                for (int n = 0; n < NB; ++n) {
                     tl.rows(vt, n, i, f);
-                    dp[n] = mma(f, gf[i], dp[n]);
+                    dp[n] = mma(f, g, dp[n]);
                 }
             }
 #pragma unroll
