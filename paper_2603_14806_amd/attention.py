@@ -116,7 +116,8 @@ def view(q, k, v, bias=None, mask=None, scale=None):
     batch, nq, heads, d = q.shape
     _, nk, kv_heads, _ = k.shape
     dtype, device, keys = q.dtype, q.device, (batch, nk, kv_heads, d)
-    _heads_tensor("q", q, dtype, device, q.shape)
+    if q.stride(3) != 1 and d > 1:
+        raise ValueError("q must have unit stride along its last axis")
     _heads_tensor("k", k, dtype, device, keys)
     _heads_tensor("v", v, dtype, device, keys)
     w = CrossAttnView(batch, nq, nk, heads, kv_heads, d, _DTYPES[dtype], d ** -0.5 if scale is None else scale)

@@ -1312,6 +1312,10 @@ int cross_bias_splits(const cross_attn_view_t* v) {
     return v->bias.data ? trimul::cross_dbias_splits(v->dtype, cross_slots(v), cross_shared(v), v->nq, v->nk) : 1;
 }
 
+trimul::CrossKvPlan cross_kv(const cross_attn_view_t* v) {
+    return trimul::cross_kv_plan(v->dtype, v->d, v->batch * v->kv_heads, v->nk, v->nq, v->heads / v->kv_heads);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1349,7 +1353,10 @@ int cross_attn_forward(const cross_attn_view_t* v, const cross_attn_tensor_t* q,
 int cross_attn_backward_workspace_size(const cross_attn_view_t* v, size_t* bytes) {
     if (int rc = cross_check(v)) return rc;
     if (!bytes) return fail(TRI_MUL_EINVAL, "null bytes pointer");
-    *bytes = cross_rows_bytes(v) + trimul::cross_dbias_part_floats(v->dtype, cross_bias_splits(v), cross_slots(v), v->nq, v->nk) * 4;
+    // the partial sums of dk and dv are done with before those of dbias begin
+    *bytes = cross_rows_bytes(v) +
+             4 * std::max(trimul::cross_dbias_part_floats(v->dtype, cross_bias_splits(v), cross_slots(v), v->nq, v->nk),
+                          trimul::cross_kv_part_floats(cross_kv(v), v->batch * v->kv_heads, v->nk, v->d));
     return ok();
 }
 
@@ -1380,7 +1387,7 @@ int cross_attn_backward(const cross_attn_view_t* v, const cross_attn_tensor_t* q
     if (queries && !stats) return fail(TRI_MUL_EINVAL, "null stats");
     const int splits = cross_bias_splits(v);
     const int64_t bh = v->batch * cross_col_heads(v);
-    if (bh > kMaxGroups || bh * ((cross_cols(v) + 127) / 128) > kMaxGroups || bh * ((v->nk + 127) / 128) > kMaxGroups ||
+    if (bh > kMaxGroups || bh * ((cross_cols(v) + 127) / 128) > kMaxGroups || bh * ((v->nk + 127) / 128) > kMaxGroups / 2 ||
         (dbias && cross_shared(v) != 1 && (cross_slots(v) > kMaxGroups || cross_slots(v) * splits * ((v->nq + 127) / 128) > kMaxGroups ||
                    cross_slots(v) * splits * ((v->nq + 127) / 128) * ((v->nk + 31) / 32) > kMaxGroups)))
         return fail(TRI_MUL_EUNSUPPORTED, "too many entries, heads, queries and keys for one call");
@@ -1401,7 +1408,7 @@ int cross_attn_backward(const cross_attn_view_t* v, const cross_attn_tensor_t* q
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = hipSuccess;
     if (queries) e = trimul::launch_cross_backward_q(v->dtype, a, s);
-    if (e == hipSuccess && dk && v->batch > 0 && v->nk > 0) e = trimul::launch_cross_backward_kv(v->dtype, a, s);
+    if (e == hipSuccess && dk && v->batch > 0 && v->nk > 0) e = trimul::launch_cross_backward_kv(v->dtype, a, cross_kv(v), s);
     if (e == hipSuccess && dbias && !a.direct_bias && v->nq > 0 && v->nk > 0 && cross_slots(v) > 0)
         e = trimul::launch_cross_backward_bias(v->dtype, a, s);
     if (e != hipSuccess) return hip_fail(e, "attention backward kernel launch");

@@ -291,14 +291,14 @@ hipError_t forward(const CrossArgs& a, const CrossPlan& p, hipStream_t s) {
 // 128 columns to a work-group where that makes one for each compute unit; else
 // 32, its waves on different keys.  Where even that leaves compute units
 // without one, the keys are split, for two on each, as long as a split
-// keeps 256 keys (two chunks a wave).  (Joining the splits of many rows costs
-// more than they bring: 13 us for 20800 rows of d = 24.)
+// keeps 512 keys (four chunks a wave): the join is a launch of 4 us, 13 for 20800
+// rows of d = 24.  (fp32, 2 entries x 4 heads, 500 x 777: 16.4 us whole, 14.9 + 4.3 us in three splits.)
 CrossPlan cross_plan(int64_t batch, int kv_heads, int64_t cols, int64_t nk) {
     CrossPlan p{cross_few(batch * kv_heads, cols) ? 32 : 128, 1, (int)((nk + 63) / 64 * 64)};
     const int64_t groups = batch * kv_heads * ((cols + p.cols - 1) / p.cols);
     if (groups > 0 && groups < 256) {
         int64_t n = (512 + groups - 1) / groups;
-        if (n > nk / 256) n = nk / 256;
+        if (n > nk / 512) n = nk / 512;
         if (n > kCrossMaxSplits) n = kCrossMaxSplits;
         if (n > 1) {
             p.split_keys = (int)(((nk + n - 1) / n + 63) / 64 * 64);

@@ -12,6 +12,9 @@
 // entries and heads that share it).  Each recomputes S and dP.
 #include "crossattn.h"
 
+#include <algorithm>
+#include <cmath>
+
 namespace trimul {
 namespace {
 
@@ -259,6 +262,8 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
     int64_t blk = xcd_block();
     const int kt_ = (int)(blk % ktiles);
     blk /= ktiles;
+    const int split = (int)(blk % a.splits);
+    blk /= a.splits;
     const int kv_heads = a.kv_heads / a.key_div, group = a.group * a.key_div;
     const int hk = (int)(blk % kv_heads);
     const int64_t b = blk / kv_heads;
@@ -267,7 +272,8 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
     const int kc = min(key, a.nk - 1);
     const bool present = valid && (!a.mask || a.mask[b * a.mask_batch + kc] != 0);
     const bool all_present = __all(present);
-    const int per_head = (a.nq + QC - 1) / QC, nchunks = per_head * group;
+    const int per_head = (a.nq + QC - 1) / QC, all = per_head * group;
+    const int c0 = (int)((int64_t)all * split / a.splits), nchunks = (int)((int64_t)all * (split + 1) / a.splits);
     const float coef = BIAS ? kLog2e : a.scale * kLog2e;
 
     Frag<T> kf[NS], vf[NS];
@@ -304,7 +310,8 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
             boff[i] = k < a.nk ? (uint32_t)(u / kBPieces) * (uint32_t)(a.bias.row * (int)sizeof(T)) + 16 * (u % kBPieces) : 0xfffffff0u;
         }
     float4 row4 = make_float4(0.f, 0.f, 0.f, 0.f);              // the statistics of row lane % QC of the chunk
-    int next_h = hk * group, next_q = WK == 1 ? 0 : w * QC;   // the chunk that load() takes
+    const int first = c0 + (WK == 1 ? 0 : w);                  // this wave's first chunk
+    int next_h = hk * group, next_q = 0;                       // the chunk that load() takes
     auto wrap = [&]() {
         while (next_q >= per_head * QC) {
             next_q -= per_head * QC;
@@ -328,11 +335,12 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
         next_q += WK * QC;
         wrap();
     };
-    if (nchunks) {                          // (wrap() ends only where a head has chunks)
-        wrap();
+    if (c0 < nchunks) {                     // (a head has chunks then: wrap() ends)
+        next_h += first / per_head;
+        next_q = first % per_head * QC;
         load();
     }
-    for (int c = WK == 1 ? 0 : w; c < nchunks; c += WK) {
+    for (int c = first; c < nchunks; c += WK) {
         const int buf = WK == 1 ? c & 1 : w;
         char* qt = mem + buf * 2 * TL::kBytes;
         char* gt = qt + TL::kBytes;
@@ -461,23 +469,51 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
                 }
             }
     }
+    if constexpr (WK > 1) {
+        __syncthreads();
+        add_waves<ND>(dk, reinterpret_cast<float*>(mem), w, lane);
+        __syncthreads();
+        add_waves<ND>(dv, reinterpret_cast<float*>(mem), w, lane);
+    }
+    if (!valid) return;
+    constexpr int groups = WK == 1 ? 4 * ND : ND;
+    const int g0 = WK == 1 ? 0 : w * ND;
+    if (a.splits > 1) {                     // [split][dk, dv][entry][key head][key][d]
+        const int64_t one = a.batch * kv_heads * a.nk * a.d;
+        float* po = a.part + (int64_t)split * 2 * one + ((b * kv_heads + hk) * a.nk + key) * a.d;
+        if (TWO) {
+            store_row<ND>(for_k ? po : po + one, dv, groups, g0, hi, a.d, for_k ? a.scale : 1.f);
+        } else {
+            store_row<TWO ? 1 : ND>(po, dk, groups, g0, hi, a.d, a.scale);
+            store_row<ND>(po + one, dv, groups, g0, hi, a.d, 1.f);
+        }
+        return;
+    }
     T* const to_k = (T*)a.dk.data + b * a.dk.batch + (int64_t)key * a.dk.token + hk * a.dk.head;
     T* const to_v = (T*)a.dv.data + b * a.dv.batch + (int64_t)key * a.dv.token + hk * a.dv.head;
-    if constexpr (TWO) {
-        if (valid) store_row<ND>(for_k ? to_k : to_v, dv, 4 * ND, 0, hi, a.d, for_k ? a.scale : 1.f);
+    if (TWO) {
+        store_row<ND>(for_k ? to_k : to_v, dv, groups, g0, hi, a.d, for_k ? a.scale : 1.f);
     } else {
-        if constexpr (WK > 1) {
-            __syncthreads();
-            add_waves<ND>(dk, reinterpret_cast<float*>(mem), w, lane);
-            __syncthreads();
-            add_waves<ND>(dv, reinterpret_cast<float*>(mem), w, lane);
-        }
-        if (!valid) return;
-        constexpr int groups = WK == 1 ? 4 * ND : ND;
-        const int g0 = WK == 1 ? 0 : w * ND;
-        store_row<ND>(to_k, dk, groups, g0, hi, a.d, a.scale);
+        store_row<TWO ? 1 : ND>(to_k, dk, groups, g0, hi, a.d, a.scale);
         store_row<ND>(to_v, dv, groups, g0, hi, a.d, 1.f);
     }
+}
+
+// The splits' sums of dk and dv, four channels a thread, in the order of the splits.
+template <typename T>
+__global__ __launch_bounds__(256) void k_cross_kv_sum(const CrossArgs a, int kv_heads) {
+    const int64_t one = a.batch * kv_heads * a.nk * a.d, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= 2 * one) return;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < a.splits; ++s) {
+        const float4 y = *reinterpret_cast<const float4*>(a.part + (int64_t)s * 2 * one + i);
+        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+    }
+    const bool is_v = i >= one;
+    const int64_t r = (is_v ? i - one : i) / a.d, bh = r / a.nk, b = bh / kv_heads;
+    const int c = (int)(i % a.d), key = (int)(r - bh * a.nk), hk = (int)(bh - b * kv_heads);
+    const CrossTensor& to = is_v ? a.dv : a.dk;
+    store4((T*)to.data + b * to.batch + (int64_t)key * to.token + hk * to.head + c, x.x, x.y, x.z, x.w);
 }
 
 // ------------------------------------------------------------------ dbias
@@ -693,21 +729,28 @@ hipError_t backward_q(const CrossArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+// d > 64: in bf16 eight waves to 128 keys; in fp32 a wave's registers do not hold a chunk of its own.
+constexpr bool kv_two(int dtype, int d) { return dtype == 1 && d > 64; }
+constexpr bool kv_may_be_few(int dtype, int d) { return dtype == 1 || d <= 64; }
+
 template <typename T, int DP, bool BIAS>
-hipError_t backward_kv(const CrossArgs& a, hipStream_t s) {
-    const int64_t heads = a.batch * (a.kv_heads / a.key_div);
-    constexpr bool kTwo = DP == 128 && sizeof(T) == 2, kSplit = DP < 128 || sizeof(T) == 2;
-    // (d > 64: in bf16 half a tile per compute unit is enough for the eight waves, in fp32 a wave's registers do not hold
-    // a chunk of its own)
-    const bool few = kSplit && cross_few(heads, a.nk) && (!kTwo || heads * ((a.nk + 127) / 128) < 128);
-    const int ktiles = few ? (a.nk + 31) / 32 : (a.nk + 127) / 128;
-    const dim3 grid((unsigned)(heads * ktiles));
-    if constexpr (kSplit)
-        if (few) {
-            hipLaunchKernelGGL((k_cross_backward_kv<T, DP, 32, 4, false, BIAS>), grid, dim3(256), 0, s, a, ktiles);
-            return hipGetLastError();
-        }
-    hipLaunchKernelGGL((k_cross_backward_kv<T, DP, 32, 1, kTwo, BIAS>), grid, dim3(kTwo ? 512 : 256), 0, s, a, ktiles);
+hipError_t backward_kv(const CrossArgs& args, const CrossKvPlan& p, hipStream_t s) {
+    CrossArgs a = args;
+    a.splits = p.splits;
+    constexpr int dt = sizeof(T) == 2 ? 1 : 0;
+    constexpr bool kTwo = kv_two(dt, DP);
+    const int kv_heads = a.kv_heads / a.key_div;
+    const dim3 grid((unsigned)(a.batch * kv_heads * p.ktiles * p.splits));
+    if constexpr (kv_may_be_few(dt, DP)) {
+        if (p.few) hipLaunchKernelGGL((k_cross_backward_kv<T, DP, 32, 4, false, BIAS>), grid, dim3(256), 0, s, a, p.ktiles);
+        else hipLaunchKernelGGL((k_cross_backward_kv<T, DP, 32, 1, kTwo, BIAS>), grid, dim3(kTwo ? 512 : 256), 0, s, a, p.ktiles);
+    } else {
+        hipLaunchKernelGGL((k_cross_backward_kv<T, DP, 32, 1, kTwo, BIAS>), grid, dim3(kTwo ? 512 : 256), 0, s, a, p.ktiles);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    const int64_t n = 2 * a.batch * kv_heads * a.nk * a.d / 4;
+    hipLaunchKernelGGL((k_cross_kv_sum<T>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a, kv_heads);
     return hipGetLastError();
 }
 
@@ -730,6 +773,39 @@ hipError_t backward_bias(const CrossArgs& a, hipStream_t s) {
 
 }  // namespace
 
+// Tiles of 128 keys from one for each compute unit on (half a one where eight
+// waves share a tile), else of 32.  The queries are split where that fills the
+// compute units better: an estimate of the time, the ten operations a score and
+// channel at the rate that the pass reaches on a full chip over the share of it
+// that the work-groups keep busy, plus the sums' launch and their bytes.  A split
+// keeps 16 chunks of 32 queries.  (2 entries x 4 key heads of 3000 keys, d = 128:
+// 192 work-groups, one to a compute unit, 367 us; 768 in four splits.)
+CrossKvPlan cross_kv_plan(int dtype, int d, int64_t heads, int64_t nk, int64_t per_head, int64_t group) {
+    CrossKvPlan p{false, 0, 1};
+    const bool two = kv_two(dtype, d);
+    const int64_t wide = (nk + 127) / 128;
+    p.few = kv_may_be_few(dtype, d) && heads * wide < (two ? 128 : 256);
+    p.ktiles = (int)(p.few ? (nk + 31) / 32 : wide);
+    const int64_t groups = heads * p.ktiles, chunks = (per_head + 31) / 32 * group;
+    if (groups < 1 || chunks < 1) return p;
+    const double places = 256.0 * (two && !p.few ? 1 : d <= 32 && dtype == 1 ? 3 : d <= 64 ? 2 : 1);
+    const double work = 10.0 * (double)heads * (double)nk * (double)per_head * (double)group * d / (dtype == 1 ? 500e6 : 60e6);   // us
+    const double bytes = 2.0 * (double)heads * (double)nk * d * 4;
+    double best = 0;
+    for (int n = 1; n <= 16 && n * 16 <= std::max<int64_t>(chunks, 16); ++n) {
+        const double busy = (double)groups * n / places, t = work * std::ceil(busy) / busy + (n > 1 ? 8 + 2 * n * bytes / 4e6 : 0);
+        if (n == 1 || t < 0.95 * best) {
+            best = t;
+            p.splits = n;
+        }
+    }
+    return p;
+}
+
+size_t cross_kv_part_floats(const CrossKvPlan& p, int64_t heads, int64_t nk, int d) {
+    return p.splits > 1 ? (size_t)p.splits * 2 * (size_t)heads * (size_t)nk * (size_t)d : 0;
+}
+
 // The work-groups of the tiles alone leave compute units idle below about
 // 1024; a split keeps four entries or heads.
 int cross_dbias_splits(int dtype, int64_t slots, int64_t shared, int64_t nq, int64_t nk) {
@@ -750,11 +826,11 @@ size_t cross_dbias_part_floats(int dtype, int splits, int64_t slots, int64_t nq,
     (dtype == 1 ? (a.d <= 32 ? F(bf16_t, 32) : a.d <= 64 ? F(bf16_t, 64) : F(bf16_t, 128))                        \
                 : (a.d <= 32 ? F(float, 32) : a.d <= 64 ? F(float, 64) : F(float, 128)))
 #define CROSS_Q(T, DP) (a.bias.data ? backward_q<T, DP, true>(a, s) : backward_q<T, DP, false>(a, s))
-#define CROSS_KV(T, DP) (a.bias.data ? backward_kv<T, DP, true>(a, s) : backward_kv<T, DP, false>(a, s))
+#define CROSS_KV(T, DP) (a.bias.data ? backward_kv<T, DP, true>(a, p, s) : backward_kv<T, DP, false>(a, p, s))
 #define CROSS_BIAS(T, DP) (backward_bias<T, DP>(a, s))
 
 hipError_t launch_cross_backward_q(int dtype, const CrossArgs& a, hipStream_t s) { return CROSS_BY_TYPE(CROSS_Q); }
-hipError_t launch_cross_backward_kv(int dtype, const CrossArgs& a, hipStream_t s) { return CROSS_BY_TYPE(CROSS_KV); }
+hipError_t launch_cross_backward_kv(int dtype, const CrossArgs& a, const CrossKvPlan& p, hipStream_t s) { return CROSS_BY_TYPE(CROSS_KV); }
 hipError_t launch_cross_backward_bias(int dtype, const CrossArgs& a, hipStream_t s) { return CROSS_BY_TYPE(CROSS_BIAS); }
 
 }  // namespace trimul

@@ -227,12 +227,20 @@ struct CrossPlan {
 inline bool cross_few(int64_t heads, int64_t n) { return heads * ((n + 127) / 128) < 256; }
 CrossPlan cross_plan(int64_t batch, int kv_heads, int64_t cols, int64_t nk);
 size_t cross_part_floats(const CrossPlan& p, int64_t batch, int64_t nq, int heads, int d);
+// How the key pass of a backward is laid out: 32 keys to a work-group (its waves on different queries) or 128, and
+// the split of the queries.
+struct CrossKvPlan {
+    bool few;
+    int ktiles, splits;
+};
+CrossKvPlan cross_kv_plan(int dtype, int d, int64_t heads, int64_t nk, int64_t per_head, int64_t group);
+size_t cross_kv_part_floats(const CrossKvPlan& p, int64_t heads, int64_t nk, int d);
 // Splits of the dbias pass over `shared` entries and heads per bias.
 int cross_dbias_splits(int dtype, int64_t slots, int64_t shared, int64_t nq, int64_t nk);
 size_t cross_dbias_part_floats(int dtype, int splits, int64_t slots, int64_t nq, int64_t nk);
 hipError_t launch_cross_forward(int dtype, const CrossArgs& a, const CrossPlan& p, hipStream_t s);
 hipError_t launch_cross_backward_q(int dtype, const CrossArgs& a, hipStream_t s);
-hipError_t launch_cross_backward_kv(int dtype, const CrossArgs& a, hipStream_t s);
+hipError_t launch_cross_backward_kv(int dtype, const CrossArgs& a, const CrossKvPlan& p, hipStream_t s);
 hipError_t launch_cross_backward_bias(int dtype, const CrossArgs& a, hipStream_t s);
 
 // Residual addition with dropout (dropout.hip): out = res + kept x scale over

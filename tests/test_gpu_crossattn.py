@@ -124,7 +124,7 @@ def check(got, x, what, dtype, scale=None, rounded=False):
 # key heads; every padded width of d
 SHAPES = [(1, 1, 1, 1, 1, 8), (2, 1, 257, 4, 4, 32), (1, 1, 5000, 8, 2, 64), (3, 5, 7, 8, 8, 16), (2, 33, 65, 4, 2, 24),
           (1, 130, 64, 2, 2, 40), (2, 129, 100, 3, 1, 128), (1, 31, 513, 4, 4, 96), (2, 200, 300, 2, 2, 64),
-          (1, 3, 2049, 6, 1, 128), (1, 40, 1500, 4, 2, 32)]
+          (1, 3, 2049, 6, 1, 128), (1, 40, 1500, 4, 2, 32), (1, 1100, 40, 4, 2, 64), (1, 1030, 77, 2, 1, 24)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -340,6 +340,53 @@ def test_offsets_past_32_bits():
     w = torch.softmax(s, 0)
     ref = sum((w[i:i + 200000, None] * vv[1, i:i + 200000, 3].double()).sum(0) for i in range(0, nk // 2, 200000))
     assert float((out2[1, 0, 3].double() - ref).norm() / ref.norm()) < 2.0 ** -7
+
+
+def on_gpu(q, k, v, dout, scale):
+    """float64 reference of one (entry, head) on the device: out, dq, dk, dv."""
+    q, k, v, g = (t.double() for t in (q, k, v, dout))
+    P = torch.softmax(q @ k.T * scale, -1)
+    out = P @ v
+    dS = P * (g @ v.T - (g * out).sum(-1, keepdim=True))
+    return out, dS @ k * scale, dS.T @ q * scale, P.T @ g
+
+
+def test_split_gradients_of_wide_heads():
+    """2 x 4 key heads of 3000 keys and d = 128: eight waves to 128 keys, and the queries in four splits.  The rounding
+    of bf16 results, weights and dS: three errors of RMS 2^-8 / sqrt(3) at most."""
+    x = cuda(make(2, 1024, 3000, 16, 4, 128, "bf16"))
+    w = A.view(x["q"], x["k"], x["v"])
+    rows = 2 * 16 * 1024 * 16                                  # workspace without splits
+    assert A.cross_attn_backward_workspace_size(w) > rows + 2 * 2 * 4 * 3000 * 128 * 4
+    got, _ = call(x)
+    for b, hk in ((0, 0), (1, 3)):
+        dk = dv = 0
+        for h in range(4 * hk, 4 * hk + 4):
+            ref = on_gpu(x["q"][b, :, h], x["k"][b, :, hk], x["v"][b, :, hk], x["dout"][b, :, h], 128 ** -0.5)
+            for n, r in (("out", ref[0]), ("dq", ref[1])):
+                rel = float((got[n][b, :, h].double() - r).norm() / r.norm())
+                say(f"  wide heads {n} b={b} h={h}: {rel:.2e}")
+                assert rel <= 2.0 ** -8, (n, rel)
+            dk, dv = dk + ref[2], dv + ref[3]
+        for n, r in (("dk", dk), ("dv", dv)):
+            rel = float((got[n][b, :, hk].double() - r).norm() / r.norm())
+            say(f"  wide heads {n} b={b} hk={hk}: {rel:.2e}")
+            assert rel <= 2.0 ** -8, (n, rel)
+
+
+def test_bias_further_apart_than_a_descriptor():
+    """The biases of two query heads that share a key head, 2^30 + 64 values apart: the heads are taken singly then,
+    with the results of the same biases side by side (each within half a step of bf16)."""
+    far = (1 << 30) + 64
+    x = cuda(make(1, 50, 60, 2, 1, 32, "bf16", (1, 2), "random"))
+    room = torch.empty(far + 50 * 64, dtype=torch.bfloat16, device="cuda")
+    bias = room.as_strided((1, 2, 50, 60), (8, far, 64, 1))
+    bias.copy_(x["bias"])
+    y = dict(x, bias=bias)
+    want, got = call(x)[0], call(y)[0]
+    for n in ("out", "dq", "dk", "dv", "dbias"):
+        assert float((got[n].float() - want[n].float()).norm()) <= 2.0 ** -8 * float(want[n].float().norm()), n
+    check(got, x, "far biases", "bf16")
 
 
 def test_scale_and_python_refusals():
