@@ -33,7 +33,9 @@
  *
  * Precision: fp32 sums, softmax statistics and gradients throughout; with bf16
  * storage the softmax weights (and dS in the backward) enter their products
- * as bf16, an error of the size of the results' own rounding.
+ * as bf16, an error of the size of the results' own rounding.  dout . out,
+ * which the backward subtracts, is taken from out before its rounding (kept
+ * beside the statistics): with few keys it is as large as what is left.
  */
 #ifndef CROSS_ATTN_H
 #define CROSS_ATTN_H
@@ -75,9 +77,14 @@ typedef struct {
  * that split the keys because there are few queries; 0 for the others. */
 int cross_attn_workspace_size(const cross_attn_view_t* v, size_t* bytes);
 
+/* Bytes of the stats that a forward leaves for its backward. */
+int cross_attn_stats_size(const cross_attn_view_t* v, size_t* bytes);
+
 /* out from q, k, vv (strides of each as given).  stats: NULL, or
- * [2][batch][heads][nq] fp32 for the backward (each query's maximum of x, and
- * its sum of exp(x - maximum); -inf and 0 for a query with no key).  ws:
+ * cross_attn_stats_size bytes (16-byte aligned) for the backward: [2][batch][heads][nq]
+ * fp32, each query's maximum of x, and its sum of exp(x - maximum) (-inf and 0 for
+ * a query with no key); with bf16 storage also, from the next multiple of 256
+ * bytes on, [batch][heads][nq][d] bf16, what the rounding took from out.  ws:
  * cross_attn_workspace_size bytes, 256-byte aligned (NULL if 0).  Errors:
  * EINVAL for null or misaligned pointers, bad sizes or strides; EUNSUPPORTED
  * for d, heads or sizes beyond the ones above; ENOMEM for a small workspace;

@@ -36,6 +36,7 @@ _view, _tensor, _size = ctypes.POINTER(CrossAttnView), ctypes.POINTER(CrossAttnT
 # name -> (restype, argtypes); the same order and meaning as include/cross_attn.h
 SIGNATURES = {
     "cross_attn_workspace_size": (ctypes.c_int, [_view, _size]),
+    "cross_attn_stats_size": (ctypes.c_int, [_view, _size]),
     "cross_attn_forward": (ctypes.c_int, [_view, _tensor, _tensor, _tensor, _tensor, _vp, _vp, ctypes.c_size_t, _vp]),
     "cross_attn_backward_workspace_size": (ctypes.c_int, [_view, _size]),
     "cross_attn_backward": (ctypes.c_int, [_view] + [_tensor] * 4 + [_vp] + [_tensor] * 4 +
@@ -64,6 +65,12 @@ def lib():
 def cross_attn_workspace_size(view):
     n = ctypes.c_size_t()
     _check(lib().cross_attn_workspace_size(view, n))
+    return n.value
+
+
+def cross_attn_stats_size(view):
+    n = ctypes.c_size_t()
+    _check(lib().cross_attn_stats_size(view, n))
     return n.value
 
 
@@ -151,12 +158,13 @@ def cross_attention(q, k, v, bias=None, mask=None, scale=None, return_stats=Fals
 
     bias: [batch or 1][heads or 1][nq][nk] (or without the first axis) of q's type whose rows are a multiple of 8
     values apart (a view of a padded tensor is fine); an axis of length 1 is shared.  mask: [batch or 1][nk] or [nk],
-    uint8 or bool, nonzero where the key is present.  scale: default 1 / sqrt(d).  With return_stats also the
-    [2][batch][heads][nq] float32 statistics that cross_attention_backward takes."""
+    uint8 or bool, nonzero where the key is present.  scale: default 1 / sqrt(d).  With return_stats also what
+    cross_attention_backward takes: a flat float32 tensor of the library's own layout (first the maxima and the sums,
+    [2][batch][heads][nq])."""
     w = view(q, k, v, bias, mask, scale)
     with on_stream(q.device, stream) as s:
         out = q.new_empty(q.shape)
-        stats = torch.empty((2, w.batch, w.heads, w.nq), dtype=torch.float32, device=q.device) if return_stats else None
+        stats = torch.empty(-(-cross_attn_stats_size(w) // 4), dtype=torch.float32, device=q.device) if return_stats else None
         n = cross_attn_workspace_size(w)
         ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
         cross_attn_forward(w, tensor(q), tensor(k), tensor(v), tensor(out), stats, ws, n, s)
@@ -173,8 +181,8 @@ def cross_attention_backward(q, k, v, out, stats, dout, bias=None, mask=None, sc
         raise ValueError("a bias that is repeated along an axis has that axis of length 1 for its gradient")
     _heads_tensor("out", out, q.dtype, q.device, q.shape)
     _heads_tensor("dout", dout, q.dtype, q.device, q.shape)
-    if stats.dtype != torch.float32 or stats.device != q.device or tuple(stats.shape) != (2, w.batch, w.heads, w.nq) or not stats.is_contiguous():
-        raise ValueError("stats must be the contiguous [2][batch][heads][nq] float32 tensor of the forward")
+    if stats.dtype != torch.float32 or stats.device != q.device or stats.dim() != 1 or not stats.is_contiguous() or 4 * stats.numel() < cross_attn_stats_size(w):
+        raise ValueError("stats must be the tensor that the forward of these arguments returned")
     with on_stream(q.device, stream) as s:
         dq = q.new_empty(q.shape)
         dk, dv = (k.new_empty(k.shape), v.new_empty(v.shape)) if need_kv else (None, None)

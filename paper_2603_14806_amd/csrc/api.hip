@@ -1312,6 +1312,16 @@ int cross_bias_splits(const cross_attn_view_t* v) {
     return v->bias.data ? trimul::cross_dbias_splits(v->dtype, cross_slots(v), cross_shared(v), v->nq, v->nk) : 1;
 }
 
+// Maxima and sums, then (bf16) what rounding took from out.
+size_t cross_sums_bytes(const cross_attn_view_t* v) { return round256((size_t)v->batch * v->heads * v->nq * 8); }
+size_t cross_stats_bytes(const cross_attn_view_t* v) {
+    return cross_sums_bytes(v) + (v->dtype == TRI_MUL_BF16 ? (size_t)v->batch * v->heads * v->nq * v->d * 2 : 0);
+}
+void cross_stats_args(const cross_attn_view_t* v, const float* stats, trimul::CrossArgs* a) {
+    a->stats = const_cast<float*>(stats);
+    if (stats) a->rest = reinterpret_cast<char*>(const_cast<float*>(stats)) + cross_sums_bytes(v);
+}
+
 trimul::CrossKvPlan cross_kv(const cross_attn_view_t* v) {
     return trimul::cross_kv_plan(v->dtype, v->d, v->batch * v->kv_heads, v->nk, v->nq, v->heads / v->kv_heads);
 }
@@ -1328,6 +1338,13 @@ int cross_attn_workspace_size(const cross_attn_view_t* v, size_t* bytes) {
     return ok();
 }
 
+int cross_attn_stats_size(const cross_attn_view_t* v, size_t* bytes) {
+    if (int rc = cross_check(v)) return rc;
+    if (!bytes) return fail(TRI_MUL_EINVAL, "null bytes pointer");
+    *bytes = cross_stats_bytes(v);
+    return ok();
+}
+
 int cross_attn_forward(const cross_attn_view_t* v, const cross_attn_tensor_t* q, const cross_attn_tensor_t* k,
                        const cross_attn_tensor_t* vv, const cross_attn_tensor_t* out, float* stats, void* ws,
                        size_t ws_bytes, void* stream) {
@@ -1336,6 +1353,7 @@ int cross_attn_forward(const cross_attn_view_t* v, const cross_attn_tensor_t* q,
     if (int rc = cross_tensor(v, k, "k", v->nk, v->kv_heads, false)) return rc;
     if (int rc = cross_tensor(v, vv, "v", v->nk, v->kv_heads, false)) return rc;
     if (int rc = cross_tensor(v, out, "out", v->nq, v->heads, true)) return rc;
+    if (!aligned16(stats)) return fail(TRI_MUL_EINVAL, "stats must be 16-byte aligned");
     const trimul::CrossPlan p = trimul::cross_plan(v->batch, cross_col_heads(v), cross_cols(v), v->nk);
     const int64_t bh = v->batch * cross_col_heads(v);
     if (bh > kMaxGroups || bh * ((cross_cols(v) + p.cols - 1) / p.cols) * p.splits > kMaxGroups)
@@ -1343,7 +1361,7 @@ int cross_attn_forward(const cross_attn_view_t* v, const cross_attn_tensor_t* q,
     if (int rc = cross_workspace(ws, ws_bytes, trimul::cross_part_floats(p, v->batch, v->nq, v->heads, v->d) * 4)) return rc;
     if (v->batch == 0 || v->nq == 0) return ok();
     trimul::CrossArgs a = cross_args(v, q, k, vv, out);
-    a.stats = stats;
+    cross_stats_args(v, stats, &a);
     a.part = static_cast<float*>(ws);
     const hipError_t e = trimul::launch_cross_forward(v->dtype, a, p, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "attention kernel launch");
@@ -1385,6 +1403,7 @@ int cross_attn_backward(const cross_attn_view_t* v, const cross_attn_tensor_t* q
     }
     const bool queries = v->batch > 0 && v->nq > 0;
     if (queries && !stats) return fail(TRI_MUL_EINVAL, "null stats");
+    if (!aligned16(stats)) return fail(TRI_MUL_EINVAL, "stats must be 16-byte aligned");
     const int splits = cross_bias_splits(v);
     const int64_t bh = v->batch * cross_col_heads(v);
     if (bh > kMaxGroups || bh * ((cross_cols(v) + 127) / 128) > kMaxGroups || bh * ((v->nk + 127) / 128) > kMaxGroups / 2 ||
@@ -1401,7 +1420,7 @@ int cross_attn_backward(const cross_attn_view_t* v, const cross_attn_tensor_t* q
     a.dv = cross_arg(dv);
     if (dbias) a.dbias = {dbias->data, dbias->batch, dbias->head, dbias->row};
     a.direct_bias = dbias && cross_shared(v) == 1;
-    a.stats = const_cast<float*>(stats);
+    cross_stats_args(v, stats, &a);
     a.rows = static_cast<float*>(ws);
     a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + cross_rows_bytes(v));
     a.splits = splits;

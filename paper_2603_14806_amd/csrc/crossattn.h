@@ -313,6 +313,19 @@ __device__ __forceinline__ void store_row(T* row, const f32x16_t (&o)[ND], int g
     }
 }
 
+// What rounding the same values to bf16 takes from them, rounded to bf16 itself.
+__device__ __forceinline__ float rounded_off(float x) { return x - bf2f(f2bf(x)); }
+template <int ND>
+__device__ __forceinline__ void store_rest(bf16_t* row, const f32x16_t (&o)[ND], int groups, int g0, int hi, int d, float scale) {
+#pragma unroll
+    for (int j = 0; j < 4 * ND; ++j) {
+        const int c = 8 * (g0 + j) + 4 * hi;
+        if (j < groups && c < d)
+            store4(row + c, rounded_off(o[j / 4][4 * (j % 4)] * scale), rounded_off(o[j / 4][4 * (j % 4) + 1] * scale),
+                   rounded_off(o[j / 4][4 * (j % 4) + 2] * scale), rounded_off(o[j / 4][4 * (j % 4) + 3] * scale));
+    }
+}
+
 // The bias of one lane's KC / 2 consecutive keys of its query, through a
 // descriptor of the rows of its wave's 32 columns: from the first one's to the
 // end of the last one's keys (rounded up to 8: nothing behind that is read; a

@@ -219,6 +219,8 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
     }
     const float inv = Lt == 0.f ? 0.f : 1.f / Lt;
     store_row<ND>((T*)a.out.data + b * a.out.batch + (int64_t)qi * a.out.token + h * a.out.head, o, groups, g0, hi, a.d, inv);
+    if constexpr (sizeof(T) == 2)
+        if (a.stats) store_rest<ND>((bf16_t*)a.rest + row * a.d, o, groups, g0, hi, a.d, inv);
     if (a.stats && !hi && (WK == 1 || w == 0)) {
         a.stats[row] = BIAS ? M : M * a.scale;
         a.stats[a.batch * a.heads * a.nq + row] = Lt;
@@ -254,6 +256,8 @@ __global__ __launch_bounds__(64) void k_cross_join(const CrossArgs a) {
         float x = 0.f;
         for (int s = 0; s < a.splits; ++s) x += wt[s] * a.part[((int64_t)s * rows + row) * a.d + c];
         Store<T>::st(po + c, x * inv);
+        if constexpr (sizeof(T) == 2)
+            if (a.stats) ((bf16_t*)a.rest)[row * a.d + c] = f2bf(rounded_off(x * inv));
     }
     if (a.stats && lane == 0) {
         a.stats[row] = a.bias.data ? M : M * a.scale;

@@ -104,6 +104,10 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
             load_row(gr, s, hi, a.d, gf[s]);
             load_row(orow, s, hi, a.d, of);
             D += Frag<T>::dot(gf[s], of);
+            if constexpr (sizeof(T) == 2) {
+                load_row((const bf16_t*)a.rest + row * a.d, s, hi, a.d, of);
+                D += Frag<T>::dot(gf[s], of);
+            }
         }
         D += xor32(D);
     }

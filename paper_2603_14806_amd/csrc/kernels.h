@@ -206,6 +206,7 @@ struct CrossArgs {
     const uint8_t* mask;
     int64_t mask_batch;
     float* stats;      // [2][batch][heads][nq]: maximum, sum
+    void* rest;        // [batch][heads][nq][d] bf16: out before its rounding less out (bf16 storage)
     float* rows;       // [batch][heads][nq][4]: statistics and dout . out (written by the query pass, read by the other two)
     float* part;       // partial results of split calls
     int64_t batch;

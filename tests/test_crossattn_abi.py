@@ -111,6 +111,13 @@ def test_null_and_workspace_refusals(lib):
     assert forward(lib, few, ws=(1 << 12) + 16, n=n.value) == EINVAL
     assert lib.cross_attn_workspace_size(ctypes.byref(view(batch=300)), ctypes.byref(n)) == T.TRI_MUL_OK and n.value == 0
     assert backward(lib, view(), stats=None) == EINVAL and "stats" in T.last_error()
+    assert backward(lib, view(), stats=(1 << 12) + 4) == EINVAL and "stats" in T.last_error()
+    assert forward(lib, view(), stats=(1 << 12) + 8) == EINVAL and "stats" in T.last_error()
+    assert lib.cross_attn_stats_size(ctypes.byref(view()), None) == EINVAL
+    assert lib.cross_attn_stats_size(ctypes.byref(view()), ctypes.byref(n)) == T.TRI_MUL_OK
+    assert n.value == 2 * 4 * 40 * 8 + 2 * 4 * 40 * 32 * 2     # 2560 bytes of sums are a multiple of 256
+    assert lib.cross_attn_stats_size(ctypes.byref(view(dtype=T.TRI_MUL_F32, nq=41)), ctypes.byref(n)) == T.TRI_MUL_OK
+    assert n.value == -(-2 * 4 * 41 * 8 // 256) * 256
     assert backward(lib, view(), ws=None) == EINVAL
     assert backward(lib, view(), n=16) == ENOMEM
     assert backward(lib, view(), dk=None) == EINVAL and "dk and dv" in T.last_error()
