@@ -1261,27 +1261,29 @@ int cross_tensor(const cross_attn_view_t* v, const cross_attn_tensor_t* t, const
     if (v->batch == 0 || tokens == 0) return TRI_MUL_OK;
     if (!t->data) return fail(TRI_MUL_EINVAL, "null %s", name);
     if (!aligned16(t->data)) return fail(TRI_MUL_EINVAL, "%s must be 16-byte aligned", name);
+    // (an axis of length 1 has no stride)
     const int64_t per = 16 / (int64_t)esize(v->dtype);
-    if (t->batch < 0 || t->token < 0 || t->head < 0 || t->batch % per || t->token % per || t->head % per)
-        return fail(TRI_MUL_EINVAL, "strides of %s must be multiples of 16 bytes, and not negative", name);
+    const struct { int64_t length, stride; } axes[] = {{v->batch, t->batch}, {tokens, t->token}, {heads, t->head}};
+    for (const auto& x : axes)
+        if (x.length > 1 && (x.stride < 0 || x.stride % per)) return fail(TRI_MUL_EINVAL, "strides of %s must be multiples of 16 bytes, and not negative", name);
     if (tokens > 1 && t->token < v->d) return fail(TRI_MUL_EINVAL, "token stride %lld of %s below d = %d", (long long)t->token, name, v->d);
-    if (t->token >= kCrossMaxToken) return fail(TRI_MUL_EUNSUPPORTED, "token stride %lld of %s is 2^23 or more", (long long)t->token, name);
+    if (tokens > 1 && t->token >= kCrossMaxToken) return fail(TRI_MUL_EUNSUPPORTED, "token stride %lld of %s is 2^23 or more", (long long)t->token, name);
     if ((heads > 1 && t->head < v->d && (written || t->head)) || (v->batch > 1 && t->batch < v->d && (written || t->batch)))
         return fail(TRI_MUL_EINVAL, "batch or head stride of %s below d = %d", name, v->d);
     return TRI_MUL_OK;
 }
 
-trimul::CrossTensor cross_arg(const cross_attn_tensor_t* t) {
-    return t ? trimul::CrossTensor{t->data, t->batch, t->token, t->head} : trimul::CrossTensor{};
+trimul::CrossTensor cross_arg(const cross_attn_view_t* v, const cross_attn_tensor_t* t, int64_t tokens) {
+    return t ? trimul::CrossTensor{t->data, t->batch, tokens > 1 ? t->token : v->d, t->head} : trimul::CrossTensor{};
 }
 
 trimul::CrossArgs cross_args(const cross_attn_view_t* v, const cross_attn_tensor_t* q, const cross_attn_tensor_t* k,
                              const cross_attn_tensor_t* vv, const cross_attn_tensor_t* out) {
     trimul::CrossArgs a{};
-    a.q = cross_arg(q);
-    a.k = cross_arg(k);
-    a.v = cross_arg(vv);
-    a.out = cross_arg(out);
+    a.q = cross_arg(v, q, v->nq);
+    a.k = cross_arg(v, k, v->nk);
+    a.v = cross_arg(v, vv, v->nk);
+    a.out = cross_arg(v, out, v->nq);
     a.bias = {v->bias.data, v->bias.batch, v->bias.head, v->bias.row};
     a.mask = v->mask;
     a.mask_batch = v->mask_batch;
@@ -1414,10 +1416,10 @@ int cross_attn_backward(const cross_attn_view_t* v, const cross_attn_tensor_t* q
     if (int rc = cross_attn_backward_workspace_size(v, &need)) return rc;
     if (int rc = cross_workspace(ws, ws_bytes, need)) return rc;
     trimul::CrossArgs a = cross_args(v, q, k, vv, out);
-    a.dout = cross_arg(dout);
-    a.dq = cross_arg(dq);
-    a.dk = cross_arg(dk);
-    a.dv = cross_arg(dv);
+    a.dout = cross_arg(v, dout, v->nq);
+    a.dq = cross_arg(v, dq, v->nq);
+    a.dk = cross_arg(v, dk, v->nk);
+    a.dv = cross_arg(v, dv, v->nk);
     if (dbias) a.dbias = {dbias->data, dbias->batch, dbias->head, dbias->row};
     a.direct_bias = dbias && cross_shared(v) == 1;
     cross_stats_args(v, stats, &a);

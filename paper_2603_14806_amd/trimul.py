@@ -488,17 +488,17 @@ class TriMul:
         """z + dropout(update of z) in the storage dtype (include/pair_dropout.h; the pair stack shares the mask
         along the rows); with p = 0 the plain residual addition.  out may be z itself."""
         from . import dropout
-        with on_stream(z.device, stream) as s:
-            return dropout.dropout_add(self(z, mask, direction, stream=s), z, p, seed, offset, share, out=out, stream=s)
+        with on_stream(z.device, stream):
+            return dropout.dropout_add(self(z, mask, direction), z, p, seed, offset, share, out=out)
 
     def residual_backward(self, z, dout, mask=None, direction="outgoing", p=0.25, seed=0, offset=0, share="rows",
                           stream=None, saved=None):
         """Gradients of sum(residual(z) * dout): (dz, grads), dout and dz in the storage dtype."""
         from . import dropout
-        with on_stream(z.device, stream) as s:
-            du = dropout.dropout_backward(dout, p, seed, offset, share, dtype=self.out_dtype, stream=s)
-            dz, grads = self.backward(z, du, mask, direction, s, saved)
-            return dropout.dropout_add(dz, dout, 0.0, stream=s), grads
+        with on_stream(z.device, stream):
+            du = dropout.dropout_backward(dout, p, seed, offset, share, dtype=self.out_dtype)
+            dz, grads = self.backward(z, du, mask, direction, saved=saved)
+            return dropout.dropout_add(dz, dout, 0.0), grads
 
     def block_accumulate(self, view, a_panel, b_panel, acc, mask=None, z_tile=None, out_tile=None, stream=None,
                          ws=None):

@@ -234,6 +234,16 @@ def test_strides(dtype, kind, nq):
     check(got, x, f"{kind} {dtype}", dtype)
 
 
+def test_axes_of_length_one_have_no_stride():
+    """What torch reports as the stride of an axis of length 1 may be anything."""
+    x = cuda(make(1, 1, 70, 1, 1, 32, "bf16", (1, 1)))
+    want, _ = call(x)
+    y = {n: t.as_strided(t.shape, (3, 5 if t.shape[1] == 1 else t.stride(1), 7, 1)) for n, t in x.items() if n != "bias"}
+    y["bias"] = x["bias"].as_strided(x["bias"].shape, (1, 1, 72, 1))
+    got, _ = call(y)
+    assert all(torch.equal(got[n], want[n]) for n in want)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_writes_nothing_else(dtype):
     """Outputs inside larger buffers through the C names: the values around them stay."""
