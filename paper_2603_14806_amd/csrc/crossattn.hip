@@ -21,17 +21,22 @@ constexpr int forward_waves() {
 // WK = 1: a wave takes 32 columns and every chunk, the chunks staged by all
 // four waves (double-buffered).  WK = 4: 32 columns, wave w takes chunks w,
 // w + 4, ..., stages them for itself, and the four results are merged at the end.
-template <typename T, int DP, int KC, int WK, bool BIAS>
+// SOLO (WK = 4): each wave has a key head of its own, with 32 columns at most.
+template <typename T, int DP, int KC, int WK, bool SOLO, bool BIAS>
 __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_forward(const CrossArgs a, int ctiles) {
     using TL = Tile<T, DP, KC>;
     constexpr int NT = 256 / WK, NB = KC / 32, ND = DP / 32, NS = DP / 16;
     __shared__ __align__(16) char mem[(WK == 1 ? 2 : 4) * 2 * TL::kBytes];
-    __shared__ float red[WK == 1 ? 1 : 2][WK == 1 ? 1 : 4][32];
+    __shared__ float red[WK == 1 || SOLO ? 1 : 2][WK == 1 || SOLO ? 1 : 4][32];
     const int lane = threadIdx.x & 63, ql = lane & 31, hi = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int t = WK == 1 ? threadIdx.x : lane;
 
     int64_t blk = xcd_block();
+    if (SOLO) {
+        blk = blk * 4 + w;
+        if (blk >= a.batch * a.kv_heads) return;              // (no barrier follows in this form)
+    }
     const int split = (int)(blk % a.splits);
     blk /= a.splits;
     const int ct = (int)(blk % ctiles);
@@ -79,13 +84,14 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
         vp.load(vb, a.v.token, k0, a.nk, a.d);
         kbyte.load(mask, k0, a.nk, lane);
     };
-    const int c0 = WK == 1 ? 0 : w;
+    constexpr int STEP = SOLO ? 1 : WK;
+    const int c0 = WK == 1 || SOLO ? 0 : w;
     load(c0);
     if (BIAS) {
         bp.init(a, b, hk, min(cw, ncols - 1), min(cw + 31, ncols - 1), qi, h, hi);
         bp.load(ks + c0 * KC, a.nk);
     }
-    for (int c = c0; c < nchunks; c += WK) {
+    for (int c = c0; c < nchunks; c += STEP) {
         char* kt = mem + (WK == 1 ? (c & 1) : w) * 2 * TL::kBytes;
         char* vt = kt + TL::kBytes;
         const int k0 = ks + c * KC;
@@ -95,7 +101,7 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
         if (WK > 1) wave_sync();
         kp.stage(kt, t, some, bits);
         vp.stage(vt, t, some, bits);
-        load(c + WK);
+        load(c + STEP);
         if (WK == 1) __syncthreads();
         else wave_sync();
         if (bits != 0 && wave_live) {
@@ -121,7 +127,7 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
                         for (int e = 0; e < 4; ++e)
                             s[n][4 * g + e] = __builtin_fmaf(s[n][4 * g + e], a.scale, f4_get(bv, e));
                     }
-                bp.load(k0 + WK * KC, a.nk);
+                bp.load(k0 + STEP * KC, a.nk);
             }
             if (some) {
                 const uint32_t mine = (uint32_t)(bits >> ((KC / 2) * hi));
@@ -177,14 +183,15 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
                     }
                 }
         } else if (BIAS) {
-            bp.load(k0 + WK * KC, a.nk);
+            bp.load(k0 + STEP * KC, a.nk);
         }
     }
 
     float Lt = L + xor32(L);
-    constexpr int groups = WK == 1 ? ND * 4 : ND;   // groups of four channels that this lane writes, from g0 on
+    constexpr bool MERGE = WK > 1 && !SOLO;
+    constexpr int groups = MERGE ? ND : ND * 4;   // groups of four channels that this lane writes, from g0 on
     int g0 = 0;
-    if constexpr (WK > 1) {                 // each wave ends up with a quarter of the channels
+    if constexpr (MERGE) {                  // each wave ends up with a quarter of the channels
         if (!hi) {
             red[0][w][ql] = M;
             red[1][w][ql] = Lt;
@@ -210,7 +217,7 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
     if (a.splits > 1) {
         const int64_t rows = a.batch * a.heads * a.nq, at = (int64_t)split * rows + row;
         store_row<ND>(a.part + at * a.d, o, groups, g0, hi, a.d, 1.f);
-        if (!hi && (WK == 1 || w == 0)) {
+        if (!hi && (!MERGE || w == 0)) {
             float* pm = a.part + (int64_t)a.splits * rows * a.d;
             pm[at] = M;
             pm[(int64_t)a.splits * rows + at] = Lt;
@@ -221,7 +228,7 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
     store_row<ND>((T*)a.out.data + b * a.out.batch + (int64_t)qi * a.out.token + h * a.out.head, o, groups, g0, hi, a.d, inv);
     if constexpr (sizeof(T) == 2)
         if (a.stats) store_rest<ND>((bf16_t*)a.rest + row * a.d, o, groups, g0, hi, a.d, inv);
-    if (a.stats && !hi && (WK == 1 || w == 0)) {
+    if (a.stats && !hi && (!MERGE || w == 0)) {
         a.stats[row] = BIAS ? M : M * a.scale;
         a.stats[a.batch * a.heads * a.nq + row] = Lt;
     }
@@ -270,10 +277,12 @@ hipError_t forward(const CrossArgs& a, const CrossPlan& p, hipStream_t s) {
     constexpr int KC = sizeof(T) == 2 ? 64 : 32;
     const int ctiles = (a.nq * a.group + p.cols - 1) / p.cols;
     const dim3 grid((unsigned)(a.batch * a.kv_heads * ctiles * p.splits));
-    if (p.cols == 128)
-        hipLaunchKernelGGL((k_cross_forward<T, DP, KC, 1, BIAS>), grid, dim3(256), 0, s, a, ctiles);
+    if (p.solo)
+        hipLaunchKernelGGL((k_cross_forward<T, DP, 32, 4, true, BIAS>), dim3((grid.x + 3) / 4), dim3(256), 0, s, a, ctiles);
+    else if (p.cols == 128)
+        hipLaunchKernelGGL((k_cross_forward<T, DP, KC, 1, false, BIAS>), grid, dim3(256), 0, s, a, ctiles);
     else
-        hipLaunchKernelGGL((k_cross_forward<T, DP, 32, 4, BIAS>), grid, dim3(256), 0, s, a, ctiles);
+        hipLaunchKernelGGL((k_cross_forward<T, DP, 32, 4, false, BIAS>), grid, dim3(256), 0, s, a, ctiles);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     hipLaunchKernelGGL((k_cross_join<T>), dim3((unsigned)(a.batch * a.heads * a.nq)), dim3(64), 0, s, a);
@@ -292,13 +301,16 @@ hipError_t forward(const CrossArgs& a, const CrossPlan& p, hipStream_t s) {
 
 }  // namespace
 
+// A wave to each key head where all have 32 columns at most and there are four
+// waves for each compute unit.
 // 128 columns to a work-group where that makes one for each compute unit; else
 // 32, its waves on different keys.  Where even that leaves compute units
 // without one, the keys are split, for two on each, as long as a split
 // keeps 512 keys (four chunks a wave): the join is a launch of 4 us, 13 for 20800
 // rows of d = 24.  (fp32, 2 entries x 4 heads, 500 x 777: 16.4 us whole, 14.9 + 4.3 us in three splits.)
 CrossPlan cross_plan(int64_t batch, int kv_heads, int64_t cols, int64_t nk) {
-    CrossPlan p{cross_few(batch * kv_heads, cols) ? 32 : 128, 1, (int)((nk + 63) / 64 * 64)};
+    CrossPlan p{cross_few(batch * kv_heads, cols) ? 32 : 128, 1, (int)((nk + 63) / 64 * 64), cross_solo(batch * kv_heads, cols)};
+    if (p.solo) p.cols = 32;
     const int64_t groups = batch * kv_heads * ((cols + p.cols - 1) / p.cols);
     if (groups > 0 && groups < 256) {
         int64_t n = (512 + groups - 1) / groups;

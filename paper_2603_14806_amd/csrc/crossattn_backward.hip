@@ -64,7 +64,8 @@ __device__ __forceinline__ void take_from(f32x16_t (&s)[NB], float scale, float 
 // ------------------------------------------------------------------ queries: dq, D
 //
 // The forward's layout (lane: one column, registers: keys): WK = 1, 32 columns
-// a wave, or WK = 4, 32 columns a work-group and its waves on different keys.
+// a wave, or WK = 4, 32 columns a work-group and its waves on different keys, or
+// SOLO (WK = 4), a key head of 32 columns at most for each wave.
 // A bias that no other entry or head shares gets its gradient, dS, from here.
 template <typename T, int DP, int WK>
 constexpr int q_waves() {
@@ -72,7 +73,7 @@ constexpr int q_waves() {
     return DP == 32 ? 3 : DP == 64 || sizeof(T) == 2 ? 2 : 1;
 }
 
-template <typename T, int DP, int KC, int WK, bool BIAS>
+template <typename T, int DP, int KC, int WK, bool SOLO, bool BIAS>
 __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_q(const CrossArgs a, int ctiles) {
     using TL = Tile<T, DP, KC>;
     constexpr int NT = 256 / WK, NB = KC / 32, ND = DP / 32, NS = DP / 16;
@@ -81,6 +82,10 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = WK == 1 ? threadIdx.x : lane;
 
     int64_t blk = xcd_block();
+    if (SOLO) {
+        blk = blk * 4 + w;
+        if (blk >= a.batch * a.kv_heads) return;              // (no barrier follows in this form)
+    }
     const int ct = (int)(blk % ctiles);
     blk /= ctiles;
     const int hk = (int)(blk % a.kv_heads);
@@ -113,7 +118,9 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
     }
     RowStat st;
     st.set(a.stats[row], a.stats[a.batch * a.heads * a.nq + row], D);
-    if (valid && !hi && (WK == 1 || w == 0)) reinterpret_cast<float4*>(a.rows)[row] = make_float4(st.M, st.n2, st.sh, D);
+    constexpr bool MERGE = WK > 1 && !SOLO;
+    constexpr int STEP = MERGE ? WK : 1;
+    if (valid && !hi && (!MERGE || w == 0)) reinterpret_cast<float4*>(a.rows)[row] = make_float4(st.M, st.n2, st.sh, D);
     const bool far = __any(st.far());
     const float coef = BIAS ? kLog2e : a.scale * kLog2e;
     const T* kb = (const T*)a.k.data + b * a.k.batch + hk / a.key_div * a.k.head;
@@ -140,13 +147,13 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
         vp.load(vb, a.v.token, c * KC, a.nk, a.d);
         kbyte.load(mask, c * KC, a.nk, lane);
     };
-    const int c0 = WK == 1 ? 0 : w;
+    const int c0 = MERGE ? w : 0;
     load(c0);
     if (BIAS) {
         bp.init(a, b, hk, min(cw, ncols - 1), min(cw + 31, ncols - 1), qi, h, hi);
         bp.load(c0 * KC, a.nk);
     }
-    for (int c = c0; c < nchunks; c += WK) {
+    for (int c = c0; c < nchunks; c += STEP) {
         char* kt = mem + (WK == 1 ? (c & 1) : w) * 2 * TL::kBytes;
         char* vt = kt + TL::kBytes;
         uint64_t bits = kbyte.bits(mask, c * KC, a.nk, lane);
@@ -155,7 +162,7 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
         if (WK > 1) wave_sync();
         kp.stage(kt, t, some, bits);
         vp.stage(vt, t, some, bits);
-        load(c + WK);
+        load(c + STEP);
         if (WK == 1) __syncthreads();
         else wave_sync();
         if (bits != 0 && wave_live) {
@@ -179,7 +186,7 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
             }
             if (BIAS) {
                 add_bias<T, KC>(s, bp, a.scale);
-                bp.load((c + WK) * KC, a.nk);
+                bp.load((c + STEP) * KC, a.nk);
             }
             if (some) drop_absent<NB>(s, (uint32_t)(bits >> ((KC / 2) * hi)));
             float cf = coef, sh = st.sh;
@@ -211,7 +218,7 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
                     }
                 }
         } else if (BIAS) {
-            bp.load((c + WK) * KC, a.nk);
+            bp.load((c + STEP) * KC, a.nk);
             if (a.direct_bias && valid) {                      // no key here: dS is 0
                 Frag<T> z;
                 z.zero();
@@ -223,13 +230,13 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
             }
         }
     }
-    if constexpr (WK > 1) {
+    if constexpr (MERGE) {
         __syncthreads();
         add_waves<ND>(acc, reinterpret_cast<float*>(mem), w, lane);
     }
     if (!valid) return;
-    store_row<ND>((T*)a.dq.data + b * a.dq.batch + (int64_t)qi * a.dq.token + h * a.dq.head, acc, WK == 1 ? 4 * ND : ND,
-                  WK == 1 ? 0 : w * ND, hi, a.d, a.scale);
+    store_row<ND>((T*)a.dq.data + b * a.dq.batch + (int64_t)qi * a.dq.token + h * a.dq.head, acc, MERGE ? ND : 4 * ND,
+                  MERGE ? w * ND : 0, hi, a.d, a.scale);
 }
 
 // ------------------------------------------------------------------ keys: dk, dv
@@ -724,12 +731,13 @@ int key_chunk(int dtype) { return dtype == 1 ? 64 : 32; }
 template <typename T, int DP, bool BIAS>
 hipError_t backward_q(const CrossArgs& a, hipStream_t s) {
     const int cols = a.nq * a.group;
-    const bool few = cross_few(a.batch * a.kv_heads, cols);
+    const bool solo = cross_solo(a.batch * a.kv_heads, cols), few = !solo && cross_few(a.batch * a.kv_heads, cols);
     const int ctiles = few ? (cols + 31) / 32 : (cols + 127) / 128;
     const dim3 grid((unsigned)(a.batch * a.kv_heads * ctiles));
     constexpr int KC = DP == 128 ? 32 : kKeyChunk<T>;
-    if (few) hipLaunchKernelGGL((k_cross_backward_q<T, DP, 32, 4, BIAS>), grid, dim3(256), 0, s, a, ctiles);
-    else hipLaunchKernelGGL((k_cross_backward_q<T, DP, KC, 1, BIAS>), grid, dim3(256), 0, s, a, ctiles);
+    if (solo) hipLaunchKernelGGL((k_cross_backward_q<T, DP, 32, 4, true, BIAS>), dim3((grid.x + 3) / 4), dim3(256), 0, s, a, ctiles);
+    else if (few) hipLaunchKernelGGL((k_cross_backward_q<T, DP, 32, 4, false, BIAS>), grid, dim3(256), 0, s, a, ctiles);
+    else hipLaunchKernelGGL((k_cross_backward_q<T, DP, KC, 1, false, BIAS>), grid, dim3(256), 0, s, a, ctiles);
     return hipGetLastError();
 }
 

@@ -221,11 +221,17 @@ struct CrossArgs {
 constexpr int kCrossMaxSplits = 64;   // one lane of the join each
 struct CrossPlan {
     int cols, splits, split_keys;
+    bool solo;   // a wave to each key head (32 columns at most)
 };
 // Whether tiles of 128 columns (or keys) are too few: below one for each of the
 // 256 compute units.  (16 heads of d = 24 with bias: 2600 columns, 336 tiles, 31 us
 // in tiles of 128 and 47 in tiles of 32; 1300, 176 tiles, 28 and 27.)
 inline bool cross_few(int64_t heads, int64_t n) { return heads * ((n + 127) / 128) < 256; }
+// Whether the key heads have so few columns, and are so many (four waves for each
+// compute unit), that a wave takes one alone.  (1500 windows of 32 queries and 128
+// keys, 4 heads: forward 25.6 us, dq 24.9; as 128-column tiles with three waves
+// idle 30.4 and 39.9.  256 x 8 single queries over 2000 keys, d = 128: 359 and 374 us.)
+inline bool cross_solo(int64_t heads, int64_t cols) { return cols <= 32 && heads >= 1024; }
 CrossPlan cross_plan(int64_t batch, int kv_heads, int64_t cols, int64_t nk);
 size_t cross_part_floats(const CrossPlan& p, int64_t batch, int64_t nq, int heads, int d);
 // How the key pass of a backward is laid out: 32 keys to a work-group (its waves on different queries) or 128, and

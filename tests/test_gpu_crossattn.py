@@ -138,6 +138,16 @@ def test_matches_oracle(shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(347, 5, 70, 3, 3, 24), (130, 3, 40, 16, 8, 64), (1030, 1, 33, 1, 1, 128), (264, 32, 128, 4, 4, 32)])
+def test_many_heads_of_few_queries(shape, dtype):
+    """More than 1024 key heads (no multiple of four among them) of 32 columns at most: a wave each."""
+    B, nq, nk, H, Hk, d = shape
+    for bias, mask in ((None, "pad"), ((B, H), "random"), ((1, 1), None)):
+        x = cuda(make(B, nq, nk, H, Hk, d, dtype, bias, mask))
+        check(call(x)[0], x, f"{dtype} {shape} bias={bias} mask={mask}", dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_shared_by_many_entries(dtype):
     """Triangle attention's shape: the rows of a pair tensor as the batch, one bias and its gradient for all (the
     sum over the rows split over work-groups), and the library's own triangle attention on the same inputs."""
