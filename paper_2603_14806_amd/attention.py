@@ -103,30 +103,37 @@ def bias_tensor(t):
     return CrossAttnBias(t.data_ptr(), 0 if n[0] == 1 else s[0], 0 if n[1] == 1 else s[1], s[2])
 
 
-def _heads_tensor(name, t, dtype, device, shape):
+def _checked(name, t, dtype, device, shape):
+    """tensor(t) after checking that t has this type, device and shape, and contiguous channels."""
     if t.dtype != dtype or t.device != device:
         raise ValueError(f"{name} must be a {dtype} tensor on {device}, not {t.dtype} on {t.device}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    if t.stride(3) != 1 and t.shape[3] > 1:
+    s = t.stride()
+    if s[3] != 1 and shape[3] > 1:
         raise ValueError(f"{name} must have unit stride along its last axis")
+    return CrossAttnTensor(t.data_ptr(), s[0], s[1], s[2])
 
 
 def view(q, k, v, bias=None, mask=None, scale=None):
     """cross_attn_view_t of the call (the tensors are kept alive by the caller), after checking shapes and types."""
+    return _call(q, k, v, bias, mask, scale)[0]
+
+
+def _call(q, k, v, bias, mask, scale):
+    """The call's cross_attn_view_t and its q, k and v."""
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q, k and v must be [batch][tokens][heads][d]")
-    if q.dtype not in _DTYPES:
-        raise ValueError(f"q must be float32 or bfloat16, not {q.dtype}")
-    if q.device.type != "cuda":
+    dtype, shape = q.dtype, q.shape
+    if dtype not in _DTYPES:
+        raise ValueError(f"q must be float32 or bfloat16, not {dtype}")
+    if not q.is_cuda:
         raise ValueError("tensors passed to the library must live on the GPU")
-    batch, nq, heads, d = q.shape
+    device = q.device
+    batch, nq, heads, d = shape
     _, nk, kv_heads, _ = k.shape
-    dtype, device, keys = q.dtype, q.device, (batch, nk, kv_heads, d)
-    if q.stride(3) != 1 and d > 1:
-        raise ValueError("q must have unit stride along its last axis")
-    _heads_tensor("k", k, dtype, device, keys)
-    _heads_tensor("v", v, dtype, device, keys)
+    keys = (batch, nk, kv_heads, d)
+    args = _checked("q", q, dtype, device, shape), _checked("k", k, dtype, device, keys), _checked("v", v, dtype, device, keys)
     w = CrossAttnView(batch, nq, nk, heads, kv_heads, d, _DTYPES[dtype], d ** -0.5 if scale is None else scale)
     if bias is not None:
         if bias.dtype != dtype or bias.device != device:
@@ -149,7 +156,7 @@ def view(q, k, v, bias=None, mask=None, scale=None):
         if mask.numel():
             w.mask = mask.data_ptr()
             w.mask_batch = 0 if mask.shape[0] == 1 else mask.stride(0)
-    return w
+    return (w,) + args
 
 
 def cross_attention(q, k, v, bias=None, mask=None, scale=None, return_stats=False, stream=None):
@@ -161,13 +168,13 @@ def cross_attention(q, k, v, bias=None, mask=None, scale=None, return_stats=Fals
     uint8 or bool, nonzero where the key is present.  scale: default 1 / sqrt(d).  With return_stats also what
     cross_attention_backward takes: a flat float32 tensor of the library's own layout (first the maxima and the sums,
     [2][batch][heads][nq])."""
-    w = view(q, k, v, bias, mask, scale)
+    w, tq, tk, tv = _call(q, k, v, bias, mask, scale)
     with on_stream(q.device, stream) as s:
         out = q.new_empty(q.shape)
         stats = torch.empty(-(-cross_attn_stats_size(w) // 4), dtype=torch.float32, device=q.device) if return_stats else None
         n = cross_attn_workspace_size(w)
         ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-        cross_attn_forward(w, tensor(q), tensor(k), tensor(v), tensor(out), stats, ws, n, s)
+        cross_attn_forward(w, tq, tk, tv, tensor(out), stats, ws, n, s)
     return (out, stats) if return_stats else out
 
 
@@ -176,11 +183,10 @@ def cross_attention_backward(q, k, v, out, stats, dout, bias=None, mask=None, sc
     """(dq, dk, dv, dbias) for dout, from the forward's arguments, its out and its stats.  dk and dv are None
     without need_kv, dbias is None without a bias or need_bias; dbias has the bias's shape, its rows padded to a
     multiple of 8 values as the bias's are (the view returned ends at nk)."""
-    w = view(q, k, v, bias, mask, scale)
+    w, tq, tk, tv = _call(q, k, v, bias, mask, scale)
     if need_bias and bias is not None and any(n > 1 and st == 0 for n, st in zip(bias.shape[:-1], bias.stride())):
         raise ValueError("a bias that is repeated along an axis has that axis of length 1 for its gradient")
-    _heads_tensor("out", out, q.dtype, q.device, q.shape)
-    _heads_tensor("dout", dout, q.dtype, q.device, q.shape)
+    to, tg = (_checked(n, t, q.dtype, q.device, q.shape) for n, t in (("out", out), ("dout", dout)))
     if stats.dtype != torch.float32 or stats.device != q.device or stats.dim() != 1 or not stats.is_contiguous() or 4 * stats.numel() < cross_attn_stats_size(w):
         raise ValueError("stats must be the tensor that the forward of these arguments returned")
     with on_stream(q.device, stream) as s:
@@ -193,6 +199,6 @@ def cross_attention_backward(q, k, v, out, stats, dout, bias=None, mask=None, sc
                 grad = bias_tensor(dbias if dbias.dim() == 4 else dbias[None])
         n = cross_attn_backward_workspace_size(w)
         ws = torch.empty(n, dtype=torch.uint8, device=q.device)
-        cross_attn_backward(w, tensor(q), tensor(k), tensor(v), tensor(out), stats, tensor(dout), tensor(dq),
+        cross_attn_backward(w, tq, tk, tv, to, stats, tg, tensor(dq),
                             tensor(dk) if need_kv else None, tensor(dv) if need_kv else None, grad, ws, n, s)
     return dq, dk, dv, dbias

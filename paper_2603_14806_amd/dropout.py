@@ -66,12 +66,14 @@ def _rows(name, t, shape=None, device=None):
 
 
 def _view(shape, ld_x, ld_out, x_dtype, out_dtype, p, seed, offset, share, row0, col0, n_cols):
-    if share not in SHARE:
+    code = SHARE.get(share)
+    if code is None:
         raise ValueError(f"share must be one of {sorted(SHARE)}, not {share!r}")
     if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
         raise ValueError("seed and offset must be in [0, 2^64)")
-    return PairDropoutView(*shape, row0, col0, shape[1] if n_cols is None else n_cols, ld_x, ld_out, x_dtype,
-                           out_dtype, SHARE[share], p, seed, offset)
+    rows, cols, channels = shape
+    return PairDropoutView(rows, cols, channels, row0, col0, cols if n_cols is None else n_cols, ld_x, ld_out, x_dtype,
+                           out_dtype, code, p, seed, offset)
 
 
 def dropout_add(x, residual=None, p=0.25, seed=0, offset=0, share="none", row0=0, col0=0, n_cols=None, out=None,
