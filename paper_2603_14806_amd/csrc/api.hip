@@ -1311,7 +1311,7 @@ int cross_workspace(const void* ws, size_t ws_bytes, size_t need) {
 // The backward's workspace: four values of every query and head, then the partial sums of dbias.
 size_t cross_rows_bytes(const cross_attn_view_t* v) { return round256((size_t)v->batch * v->heads * v->nq * 16); }
 int cross_bias_splits(const cross_attn_view_t* v) {
-    return v->bias.data ? trimul::cross_dbias_splits(v->dtype, cross_slots(v), cross_shared(v), v->nq, v->nk) : 1;
+    return v->bias.data ? trimul::cross_dbias_splits(v->dtype, v->d, cross_slots(v), cross_shared(v), v->nq, v->nk) : 1;
 }
 
 // Maxima and sums, then (bf16) what rounding took from out.

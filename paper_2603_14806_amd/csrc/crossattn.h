@@ -26,6 +26,12 @@ namespace trimul {
 
 __device__ __forceinline__ float xor32(float v) { return __shfl_xor(v, 32); }
 
+// x where bit i of `bits` is set, else -inf: a sign-extended bit and a bitwise select.
+__device__ __forceinline__ float present_or_inf(float x, uint32_t bits, int i) {
+    const uint32_t m = (uint32_t)((int32_t)(bits << (31 - i)) >> 31);
+    return __uint_as_float((__float_as_uint(x) & m) | (0xff800000u & ~m));
+}
+
 // ds_read_b64_tr_b16: in each 16-lane group g, lane 16 g + 4 a + b receives
 // element b of the 8-byte chunks addressed by lanes 16 g + a, + 4, + 8, + 12.
 typedef short v4i16_t __attribute__((ext_vector_type(4)));
@@ -111,8 +117,9 @@ __device__ __forceinline__ void store8(float* p, const Frag<float>& f, int n) {
 // .. + 7 of a row of d channels (zero past d).
 __device__ __forceinline__ void load_row(const bf16_t* row, int s2, int hi, int d, Frag<bf16_t>& f) {
     const int c = 16 * s2 + 8 * hi;
-    f.u = *reinterpret_cast<const uint4*>(row + (c < d ? c : 0));
-    if (c >= d) f.zero();
+    const uint4 x = *reinterpret_cast<const uint4*>(row + (c < d ? c : 0));
+    const uint32_t m = c < d ? ~0u : 0u;   // (an `if` here becomes a branch around the load, and a wait for each)
+    f.u = make_uint4(x.x & m, x.y & m, x.z & m, x.w & m);
 }
 __device__ __forceinline__ void load_row(const float* row, int s2, int hi, int d, Frag<float>& f) {
     const int c = 16 * s2 + 8 * hi;
@@ -237,9 +244,11 @@ struct Part {
 
 // Work-groups go to the eight XCDs in turn; this order gives each XCD consecutive
 // ones, which read the same keys (or queries), so that its L2 serves the repeats.
-__device__ __forceinline__ int64_t xcd_block() {
+// (32 bits: a grid is below 2^24, and the divisions that take the number apart
+// are four times as long in 64.)
+__device__ __forceinline__ uint32_t xcd_block() {
     const uint32_t n = gridDim.x, x = blockIdx.x & 7, i = blockIdx.x >> 3;
-    return (int64_t)x * (n >> 3) + min(x, n & 7) + i;
+    return x * (n >> 3) + min(x, n & 7) + i;
 }
 
 // Wave-private LDS: a wave's LDS operations run in order, only the compiler has to be kept from moving them.

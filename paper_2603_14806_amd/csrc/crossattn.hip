@@ -42,17 +42,17 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int t = WK == 1 ? threadIdx.x : lane;
 
-    int64_t blk = xcd_block();
+    uint32_t blk = xcd_block();
     if (SOLO) {
         blk = blk * 4 + w;
-        if (blk >= a.batch * a.kv_heads) return;              // (no barrier follows in this form)
+        if (blk >= (uint32_t)(a.batch * a.kv_heads)) return;             // (no barrier follows in this form)
     }
-    const int split = (int)(blk % a.splits);
-    blk /= a.splits;
-    const int ct = (int)(blk % ctiles);
-    blk /= ctiles;
-    const int hk = (int)(blk % a.kv_heads);
-    const int64_t b = blk / a.kv_heads;
+    const int split = (int)(blk % (uint32_t)a.splits);
+    blk /= (uint32_t)a.splits;
+    const int ct = (int)(blk % (uint32_t)ctiles);
+    blk /= (uint32_t)ctiles;
+    const int hk = (int)(blk % (uint32_t)a.kv_heads);
+    const int64_t b = blk / (uint32_t)a.kv_heads;
     const int ncols = a.nq * a.group;
     const int cw = ct * (128 / WK) + (WK == 1 ? 32 * w : 0);      // the wave's first column
     const bool wave_live = cw < ncols;
@@ -60,12 +60,6 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
     const int col = min(cw + ql, ncols - 1);
     const int qi = col / a.group, h = hk * a.group + (col - qi * a.group);
 
-    Frag<T> qf[NS];
-    {
-        const T* row = (const T*)a.q.data + b * a.q.batch + (int64_t)qi * a.q.token + h * a.q.head;
-#pragma unroll
-        for (int s = 0; s < NS; ++s) load_row(row, s, hi, a.d, qf[s]);
-    }
     const T* kb = (const T*)a.k.data + b * a.k.batch + hk / a.key_div * a.k.head;
     const T* vb = (const T*)a.v.data + b * a.v.batch + hk / a.key_div * a.v.head;
     const uint8_t* mask = a.mask ? a.mask + b * a.mask_batch : nullptr;
@@ -100,6 +94,12 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
     if (BIAS) {
         bp.init(a, b, hk, min(cw, ncols - 1), min(cw + 31, ncols - 1), qi, h, hi);
         bp.load(ks + c0 * KC, a.nk);
+    }
+    Frag<T> qf[NS];
+    {
+        const T* row = (const T*)a.q.data + b * a.q.batch + (int64_t)qi * a.q.token + h * a.q.head;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) load_row(row, s, hi, a.d, qf[s]);
     }
     for (int c = c0; c < nchunks; c += STEP) {
         char* kt = mem + (WK == 1 ? (c & 1) : w) * 2 * TL::kBytes;
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[n][r] = (mine >> (16 * n + r)) & 1 ? s[n][r] : -INFINITY;
+                    for (int r = 0; r < 16; ++r) s[n][r] = present_or_inf(s[n][r], mine, 16 * n + r);
             }
             float cm = -INFINITY;
 #pragma unroll

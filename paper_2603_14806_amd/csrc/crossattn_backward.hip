@@ -11,7 +11,7 @@
 // heads) and, where a bias is given, tiles of it (whose loop runs over the
 // entries and heads that share it).  Each recomputes S and dP: writing dS
 // down instead would cost more than it saves (384 entries x 4 heads of 384 x 384 in
-// bf16: 0.45 GB, 180 us there and back, against a pass's 113).
+// bf16: 0.45 GB, 180 us there and back, against a pass's 100).
 #include "crossattn.h"
 
 #include <algorithm>
@@ -34,33 +34,25 @@ struct RowStat {
     __device__ __forceinline__ bool far() const { return !(fabsf(M * kLog2e) <= kFmaMax); }
 };
 
-// x = q . k scale + bias of a lane's keys.
+// x = q . k scale + bias of a lane's 16 keys of the n-th 32.
 template <typename T, int KC>
-__device__ __forceinline__ void add_bias(f32x16_t (&s)[KC / 32], const BiasRow<T, KC>& bp, float scale) {
+__device__ __forceinline__ void add_bias(f32x16_t& s, int n, const BiasRow<T, KC>& bp, float scale) {
 #pragma unroll
-    for (int n = 0; n < KC / 32; ++n)
+    for (int g = 0; g < 4; ++g) {
+        const float4 bv = bp.get(n, g);
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const float4 bv = bp.get(n, g);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][4 * g + e] = __builtin_fmaf(s[n][4 * g + e], scale, f4_get(bv, e));
-        }
+        for (int e = 0; e < 4; ++e) s[4 * g + e] = __builtin_fmaf(s[4 * g + e], scale, f4_get(bv, e));
+    }
 }
 // Absent keys (their bit of `mine` is 0): x = -inf.
-template <int NB>
-__device__ __forceinline__ void drop_absent(f32x16_t (&s)[NB], uint32_t mine) {
+__device__ __forceinline__ void drop_absent(f32x16_t& s, uint32_t mine) {
 #pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[n][r] = (mine >> (16 * n + r)) & 1 ? s[n][r] : -INFINITY;
+    for (int r = 0; r < 16; ++r) s[r] = present_or_inf(s[r], mine, r);
 }
 // x - M where M is large.
-template <int NB>
-__device__ __forceinline__ void take_from(f32x16_t (&s)[NB], float scale, float M) {
+__device__ __forceinline__ void take_from(f32x16_t& s, float scale, float M) {
 #pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[n][r] = __builtin_fmaf(s[n][r], scale, -M);
+    for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], scale, -M);
 }
 
 // ------------------------------------------------------------------ queries: dq, D
@@ -68,7 +60,8 @@ __device__ __forceinline__ void take_from(f32x16_t (&s)[NB], float scale, float 
 // The forward's layout (lane: one column, registers: keys): WK = 1, 32 columns
 // a wave, or WK = 4, 32 columns a work-group and its waves on different keys, or
 // SOLO (WK = 4), a key head of 32 columns at most for each wave.
-// A bias that no other entry or head shares gets its gradient, dS, from here.
+// A bias that no other entry or head shares gets its gradient, dS, from here (DIRECT; asked
+// at each product instead, the branches there cut the others' code into pieces).
 // Bound by instruction issue: three products a score and channel, and the
 // exponential (384 entries x 4 heads of 384 x 384, d = 32, bias: 122 us; 2 entries x 16 heads, 2048 x 3000,
 // d = 128: 158 us, 480 TFLOP/s).
@@ -78,28 +71,58 @@ constexpr int q_waves() {
     return DP == 32 ? 3 : DP == 64 || sizeof(T) == 2 ? 2 : 1;
 }
 
-template <typename T, int DP, int KC, int WK, bool SOLO, bool BIAS>
+template <typename T, int DP, int KC, int WK, bool SOLO, bool BIAS, bool DIRECT>
 __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_q(const CrossArgs a, int ctiles) {
     using TL = Tile<T, DP, KC>;
     constexpr int NT = 256 / WK, NB = KC / 32, ND = DP / 32, NS = DP / 16;
+    constexpr bool FOLD = sizeof(T) == 2 && DP <= 64;          // dP's sum starts at -D (16 registers that hold it)
     __shared__ __align__(16) char mem[(WK == 1 ? 2 : 4) * 2 * TL::kBytes];
     const int lane = threadIdx.x & 63, ql = lane & 31, hi = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = WK == 1 ? threadIdx.x : lane;
 
-    int64_t blk = xcd_block();
+    uint32_t blk = xcd_block();
     if (SOLO) {
         blk = blk * 4 + w;
-        if (blk >= a.batch * a.kv_heads) return;              // (no barrier follows in this form)
+        if (blk >= (uint32_t)(a.batch * a.kv_heads)) return;             // (no barrier follows in this form)
     }
-    const int ct = (int)(blk % ctiles);
-    blk /= ctiles;
-    const int hk = (int)(blk % a.kv_heads);
-    const int64_t b = blk / a.kv_heads;
+    const int ct = (int)(blk % (uint32_t)ctiles);
+    blk /= (uint32_t)ctiles;
+    const int hk = (int)(blk % (uint32_t)a.kv_heads);
+    const int64_t b = blk / (uint32_t)a.kv_heads;
     const int ncols = a.nq * a.group, cw = ct * (128 / WK) + (WK == 1 ? 32 * w : 0);
     const bool wave_live = cw < ncols, valid = cw + ql < ncols;
     const int col = min(cw + ql, ncols - 1);
     const int qi = col / a.group, h = hk * a.group + (col - qi * a.group);
     const int64_t row = (b * a.heads + h) * a.nq + qi;
+
+    constexpr bool MERGE = WK > 1 && !SOLO;
+    constexpr int STEP = MERGE ? WK : 1;
+    const float coef = BIAS ? kLog2e : a.scale * kLog2e;
+    const T* kb = (const T*)a.k.data + b * a.k.batch + hk / a.key_div * a.k.head;
+    const T* vb = (const T*)a.v.data + b * a.v.batch + hk / a.key_div * a.v.head;
+    const uint8_t* mask = a.mask ? a.mask + b * a.mask_batch : nullptr;
+    const int nchunks = (a.nk + KC - 1) / KC;
+    T* const drow = DIRECT ? (T*)a.dbias.data + b * a.dbias.batch + h * a.dbias.head + (int64_t)qi * a.dbias.row : nullptr;
+
+    // the first chunk is asked for before the rows' own values are waited for
+    TL tl;
+    tl.init(lane);
+    Part<T, DP, KC, NT> kp, vp;
+    KeyByte kbyte;
+    BiasRow<T, KC> bp;
+    kp.init(a.k.token, a.d, t);
+    vp.init(a.v.token, a.d, t);
+    auto load = [&](int c) {
+        kp.load(kb, a.k.token, c * KC, a.nk, a.d);
+        vp.load(vb, a.v.token, c * KC, a.nk, a.d);
+        kbyte.load(mask, c * KC, a.nk, lane);
+    };
+    const int c0 = MERGE ? w : 0;
+    load(c0);
+    if (BIAS) {
+        bp.init(a, b, hk, min(cw, ncols - 1), min(cw + 31, ncols - 1), qi, h, hi);
+        bp.load(c0 * KC, a.nk);
+    }
 
     Frag<T> qf[NS], gf[NS];
     float D = 0.f;
@@ -123,41 +146,18 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
     }
     RowStat st;
     st.set(a.stats[row], a.stats[a.batch * a.heads * a.nq + row], D);
-    constexpr bool MERGE = WK > 1 && !SOLO;
-    constexpr int STEP = MERGE ? WK : 1;
     if (valid && !hi && (!MERGE || w == 0)) reinterpret_cast<float4*>(a.rows)[row] = make_float4(st.M, st.n2, st.sh, D);
     const bool far = __any(st.far());
-    const float coef = BIAS ? kLog2e : a.scale * kLog2e;
-    const T* kb = (const T*)a.k.data + b * a.k.batch + hk / a.key_div * a.k.head;
-    const T* vb = (const T*)a.v.data + b * a.v.batch + hk / a.key_div * a.v.head;
-    const uint8_t* mask = a.mask ? a.mask + b * a.mask_batch : nullptr;
-    const int nchunks = (a.nk + KC - 1) / KC;
-    T* const drow = BIAS && a.direct_bias ? (T*)a.dbias.data + b * a.dbias.batch + h * a.dbias.head + (int64_t)qi * a.dbias.row : nullptr;
-
     f32x16_t acc[ND];
 #pragma unroll
     for (int i = 0; i < ND; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
 
-    TL tl;
-    tl.init(lane);
-    Part<T, DP, KC, NT> kp, vp;
-    KeyByte kbyte;
-    BiasRow<T, KC> bp;
-    kp.init(a.k.token, a.d, t);
-    vp.init(a.v.token, a.d, t);
-    auto load = [&](int c) {
-        kp.load(kb, a.k.token, c * KC, a.nk, a.d);
-        vp.load(vb, a.v.token, c * KC, a.nk, a.d);
-        kbyte.load(mask, c * KC, a.nk, lane);
-    };
-    const int c0 = MERGE ? w : 0;
-    load(c0);
-    if (BIAS) {
-        bp.init(a, b, hk, min(cw, ncols - 1), min(cw + 31, ncols - 1), qi, h, hi);
-        bp.load(c0 * KC, a.nk);
-    }
+    f32x16_t start;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) start[r] = FOLD ? -D : 0.f;
+
     for (int c = c0; c < nchunks; c += STEP) {
         char* kt = mem + (WK == 1 ? (c & 1) : w) * 2 * TL::kBytes;
         char* vt = kt + TL::kBytes;
@@ -171,47 +171,43 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
         if (WK == 1) __syncthreads();
         else wave_sync();
         if (bits != 0 && wave_live) {
-            f32x16_t s[NB], dp[NB];
+            const uint32_t mine = (uint32_t)(bits >> ((KC / 2) * hi));
 #pragma unroll
-            for (int n = 0; n < NB; ++n) {
+            for (int n = 0; n < NB; ++n) {                     // 32 keys at a time: their scores are all that is live
+                f32x16_t s, dp = start;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[n][r] = dp[n][r] = 0.f;
+                for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
                     Frag<T> f;
                     tl.rows(kt, n, i, f);
-                    s[n] = mma(f, qf[i], s[n]);
+                    s = mma(f, qf[i], s);
                 }
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
                     Frag<T> f;
                     tl.rows(vt, n, i, f);
-                    dp[n] = mma(f, gf[i], dp[n]);
+                    dp = mma(f, gf[i], dp);
                 }
-            }
-            if (BIAS) {
-                add_bias<T, KC>(s, bp, a.scale);
-                bp.load((c + STEP) * KC, a.nk);
-            }
-            if (some) drop_absent<NB>(s, (uint32_t)(bits >> ((KC / 2) * hi)));
-            float cf = coef, sh = st.sh;
-            if (far) {
-                take_from<NB>(s, BIAS ? 1.f : a.scale, st.M);
-                cf = kLog2e;
-                sh = st.n2;
-            }
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
+                if (BIAS) {
+                    add_bias<T, KC>(s, n, bp, a.scale);
+                    if (n == NB - 1) bp.load((c + STEP) * KC, a.nk);
+                }
+                if (some) drop_absent(s, mine >> (16 * n));
+                float cf = coef, sh = st.sh;
+                if (far) {
+                    take_from(s, BIAS ? 1.f : a.scale, st.M);
+                    cf = kLog2e;
+                    sh = st.n2;
+                }
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    s[n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], cf, sh)) * (dp[n][r] - D);
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
+                    s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], cf, sh)) * (FOLD ? dp[r] : dp[r] - D);
 #pragma unroll
                 for (int tt = 0; tt < 2; ++tt) {
                     Frag<T> pf;
-                    take8(s[n], tt, pf);
-                    if (BIAS && a.direct_bias) {
+                    take8(s, tt, pf);
+                    if (DIRECT) {
                         const int k = c * KC + (KC / 2) * hi + 16 * n + 8 * tt;
                         if (valid) store8(drow + k, pf, a.nk - k);
                     }
@@ -222,9 +218,10 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
                         acc[i] = mma(kf, pf, acc[i]);
                     }
                 }
+            }
         } else if (BIAS) {
             bp.load((c + STEP) * KC, a.nk);
-            if (a.direct_bias && valid) {                      // no key here: dS is 0
+            if (DIRECT && valid) {                      // no key here: dS is 0
                 Frag<T> z;
                 z.zero();
 #pragma unroll
@@ -278,14 +275,14 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
     const int w = TWO ? wid & 3 : wid;
     const bool for_k = TWO && wid >= 4;                        // TWO: this wave's half
 
-    int64_t blk = xcd_block();
-    const int kt_ = (int)(blk % ktiles);
-    blk /= ktiles;
-    const int split = (int)(blk % a.splits);
-    blk /= a.splits;
+    uint32_t blk = xcd_block();
+    const int kt_ = (int)(blk % (uint32_t)ktiles);
+    blk /= (uint32_t)ktiles;
+    const int split = (int)(blk % (uint32_t)a.splits);
+    blk /= (uint32_t)a.splits;
     const int kv_heads = a.kv_heads / a.key_div, group = a.group * a.key_div;
-    const int hk = (int)(blk % kv_heads);
-    const int64_t b = blk / kv_heads;
+    const int hk = (int)(blk % (uint32_t)kv_heads);
+    const int64_t b = blk / (uint32_t)kv_heads;
     const int key0 = kt_ * KT, kw = WK == 1 ? 32 * w : 0, key = key0 + kw + kl;
     const bool valid = key < a.nk, wave_live = key0 + kw < a.nk;
     const int kc = min(key, a.nk - 1);
@@ -539,9 +536,12 @@ __global__ __launch_bounds__(256) void k_cross_kv_sum(const CrossArgs a, int kv_
 //
 // A bias that several entries or heads share.  One work-group: 128 queries x KC keys of it (the query
 // pass's layout), its loop over the entries and heads that share it (a split of them: the sums of the splits are added by
-// k_cross_dbias_sum).
+// k_cross_dbias_sum).  Bound by issue and the latency of its 64 keys' steps, two waves a SIMD (384 entries x
+// 4 heads of 384 x 384, d = 32: 100 us; three waves spill and take 340).
+constexpr int dbias_waves(int dtype, int d) { return d <= 32 || (d <= 64 && dtype == 1) ? 2 : 1; }
+
 template <typename T, int DP, int KC>
-__global__ __launch_bounds__(256, DP == 32 || (DP == 64 && sizeof(T) == 2) ? 2 : 1) void k_cross_dbias(const CrossArgs a, int slot_heads, int shared_heads, int shared,
+__global__ __launch_bounds__(256, dbias_waves(sizeof(T) == 2 ? 1 : 0, DP)) void k_cross_dbias(const CrossArgs a, int slot_heads, int shared_heads, int shared,
                                                      int qtiles, int ktiles) {
     using TL = Tile<T, DP, KC>;
     constexpr int NB = KC / 32, NS = DP / 16, kPer = 16 / (int)sizeof(T);
@@ -551,13 +551,13 @@ __global__ __launch_bounds__(256, DP == 32 || (DP == 64 && sizeof(T) == 2) ? 2 :
     __shared__ __align__(16) char qmem[4][2 * QL::kBytes];     // a wave's 32 queries: q and dout
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), ql = lane & 31, hi = lane >> 5;
 
-    int64_t blk = xcd_block();
-    const int kt_ = (int)(blk % ktiles);
-    blk /= ktiles;
-    const int qt_ = (int)(blk % qtiles);
-    blk /= qtiles;
-    const int split = (int)(blk % a.splits);
-    const int64_t slot = blk / a.splits;
+    uint32_t blk = xcd_block();
+    const int kt_ = (int)(blk % (uint32_t)ktiles);
+    blk /= (uint32_t)ktiles;
+    const int qt_ = (int)(blk % (uint32_t)qtiles);
+    blk /= (uint32_t)qtiles;
+    const int split = (int)(blk % (uint32_t)a.splits);
+    const int64_t slot = blk / (uint32_t)a.splits;
     const int64_t slot_b = slot / slot_heads;
     const int slot_h = (int)(slot - slot_b * slot_heads);
     const int k0 = kt_ * KC, qw = qt_ * 128 + 32 * w;
@@ -671,10 +671,13 @@ __global__ __launch_bounds__(256, DP == 32 || (DP == 64 && sizeof(T) == 2) ? 2 :
             for (int n = 0; n < NB; ++n)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[n][r] = __builtin_fmaf(s[n][r], a.scale, bv[n][r]);
-            if (some) drop_absent<NB>(s, (uint32_t)(bits >> ((KC / 2) * hi)));
+            if (some)
+#pragma unroll
+                for (int n = 0; n < NB; ++n) drop_absent(s[n], (uint32_t)(bits >> ((KC / 2) * hi + 16 * n)));
             float sh = st.sh;
             if (far) {
-                take_from<NB>(s, 1.f, st.M);
+#pragma unroll
+                for (int n = 0; n < NB; ++n) take_from(s[n], 1.f, st.M);
                 sh = st.n2;
             }
 #pragma unroll
@@ -736,16 +739,16 @@ __global__ __launch_bounds__(256) void k_cross_dbias_sum(const CrossArgs a, int 
 template <typename T> constexpr int kKeyChunk = sizeof(T) == 2 ? 64 : 32;
 int key_chunk(int dtype) { return dtype == 1 ? 64 : 32; }
 
-template <typename T, int DP, bool BIAS>
+template <typename T, int DP, bool BIAS, bool DIRECT>
 hipError_t backward_q(const CrossArgs& a, hipStream_t s) {
     const int cols = a.nq * a.group;
     const bool solo = cross_solo(a.batch * a.kv_heads, cols), few = !solo && cross_few(a.batch * a.kv_heads, cols);
     const int ctiles = few ? (cols + 31) / 32 : (cols + 127) / 128;
     const dim3 grid((unsigned)(a.batch * a.kv_heads * ctiles));
     constexpr int KC = DP == 128 ? 32 : kKeyChunk<T>;
-    if (solo) hipLaunchKernelGGL((k_cross_backward_q<T, DP, 32, 4, true, BIAS>), dim3((grid.x + 3) / 4), dim3(256), 0, s, a, ctiles);
-    else if (few) hipLaunchKernelGGL((k_cross_backward_q<T, DP, 32, 4, false, BIAS>), grid, dim3(256), 0, s, a, ctiles);
-    else hipLaunchKernelGGL((k_cross_backward_q<T, DP, KC, 1, false, BIAS>), grid, dim3(256), 0, s, a, ctiles);
+    if (solo) hipLaunchKernelGGL((k_cross_backward_q<T, DP, 32, 4, true, BIAS, DIRECT>), dim3((grid.x + 3) / 4), dim3(256), 0, s, a, ctiles);
+    else if (few) hipLaunchKernelGGL((k_cross_backward_q<T, DP, 32, 4, false, BIAS, DIRECT>), grid, dim3(256), 0, s, a, ctiles);
+    else hipLaunchKernelGGL((k_cross_backward_q<T, DP, KC, 1, false, BIAS, DIRECT>), grid, dim3(256), 0, s, a, ctiles);
     return hipGetLastError();
 }
 
@@ -826,15 +829,27 @@ size_t cross_kv_part_floats(const CrossKvPlan& p, int64_t heads, int64_t nk, int
     return p.splits > 1 ? (size_t)p.splits * 2 * (size_t)heads * (size_t)nk * (size_t)d : 0;
 }
 
-// The work-groups of the tiles alone leave compute units idle below about
-// 1024; a split keeps four entries or heads.
-int cross_dbias_splits(int dtype, int64_t slots, int64_t shared, int64_t nq, int64_t nk) {
+// The entries and heads of a bias are split where that shortens the pass: its
+// rounds of work-groups (two to a compute unit, or one) times the entries that each
+// of them takes, against the sums' launch and the bytes of the partial sums, in
+// entries' times.  A split keeps four.  (384 entries, 72 tiles, d = 32: seven splits,
+// 504 work-groups, 100 us and 5 for the sums; fifteen, 1080, 116 and 7; 28, 2016, 112 and 11.)
+int cross_dbias_splits(int dtype, int d, int64_t slots, int64_t shared, int64_t nq, int64_t nk) {
     const int kc = key_chunk(dtype);
-    const int64_t tiles = slots * ((nq + 127) / 128) * ((nk + kc - 1) / kc);
-    if (tiles < 1 || tiles >= 1024) return 1;
-    int64_t n = (1024 + tiles - 1) / tiles;
-    if (n > shared / 4) n = shared / 4;
-    return n < 1 ? 1 : (int)n;
+    const int64_t tiles = slots * ((nq + 127) / 128) * ((nk + kc - 1) / kc), places = dbias_waves(dtype, d) * 256;
+    if (tiles < 1 || tiles >= 4 * places) return 1;
+    int64_t best_n = 1;
+    double best = 0;
+    for (int rounds = 0; rounds <= 4; ++rounds) {              // one split, and the most that rounds of work-groups hold
+        const int64_t n = rounds ? std::min(rounds * places / tiles, shared / 4) : 1;
+        if (n < 1) continue;
+        const double t = (double)((tiles * n + places - 1) / places * ((shared + n - 1) / n)) + (n > 1 ? 2 + 0.01 * (double)(n * tiles) : 0);
+        if (rounds == 0 || t < 0.97 * best) {
+            best = t;
+            best_n = n;
+        }
+    }
+    return (int)best_n;
 }
 
 size_t cross_dbias_part_floats(int dtype, int splits, int64_t slots, int64_t nq, int64_t nk) {
@@ -845,7 +860,9 @@ size_t cross_dbias_part_floats(int dtype, int splits, int64_t slots, int64_t nq,
 #define CROSS_BY_TYPE(F)                                                                                        \
     (dtype == 1 ? (a.d <= 32 ? F(bf16_t, 32) : a.d <= 64 ? F(bf16_t, 64) : F(bf16_t, 128))                        \
                 : (a.d <= 32 ? F(float, 32) : a.d <= 64 ? F(float, 64) : F(float, 128)))
-#define CROSS_Q(T, DP) (a.bias.data ? backward_q<T, DP, true>(a, s) : backward_q<T, DP, false>(a, s))
+#define CROSS_Q(T, DP)                                                       \
+    (!a.bias.data ? backward_q<T, DP, false, false>(a, s)                    \
+                  : a.direct_bias ? backward_q<T, DP, true, true>(a, s) : backward_q<T, DP, true, false>(a, s))
 #define CROSS_KV(T, DP) (a.bias.data ? backward_kv<T, DP, true>(a, p, s) : backward_kv<T, DP, false>(a, p, s))
 #define CROSS_BIAS(T, DP) (backward_bias<T, DP>(a, s))
 

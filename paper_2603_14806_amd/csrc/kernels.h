@@ -243,7 +243,7 @@ struct CrossKvPlan {
 CrossKvPlan cross_kv_plan(int dtype, int d, int64_t heads, int64_t nk, int64_t per_head, int64_t group);
 size_t cross_kv_part_floats(const CrossKvPlan& p, int64_t heads, int64_t nk, int d);
 // Splits of the dbias pass over `shared` entries and heads per bias.
-int cross_dbias_splits(int dtype, int64_t slots, int64_t shared, int64_t nq, int64_t nk);
+int cross_dbias_splits(int dtype, int d, int64_t slots, int64_t shared, int64_t nq, int64_t nk);
 size_t cross_dbias_part_floats(int dtype, int splits, int64_t slots, int64_t nq, int64_t nk);
 hipError_t launch_cross_forward(int dtype, const CrossArgs& a, const CrossPlan& p, hipStream_t s);
 hipError_t launch_cross_backward_q(int dtype, const CrossArgs& a, hipStream_t s);
