@@ -1428,8 +1428,14 @@ int cross_attn_backward(const cross_attn_view_t* v, const cross_attn_tensor_t* q
     a.splits = splits;
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = hipSuccess;
-    if (queries) e = trimul::launch_cross_backward_q(v->dtype, a, s);
-    if (e == hipSuccess && dk && v->batch > 0 && v->nk > 0) e = trimul::launch_cross_backward_kv(v->dtype, a, cross_kv(v), s);
+    const bool keys = dk && v->batch > 0 && v->nk > 0;
+    const trimul::CrossKvPlan kv = cross_kv(v);
+    if (queries && keys && trimul::cross_both(a, kv)) {
+        e = trimul::launch_cross_backward_both(v->dtype, a, kv, s);
+    } else {
+        if (queries) e = trimul::launch_cross_backward_q(v->dtype, a, s);
+        if (e == hipSuccess && keys) e = trimul::launch_cross_backward_kv(v->dtype, a, kv, s);
+    }
     if (e == hipSuccess && dbias && !a.direct_bias && v->nq > 0 && v->nk > 0 && cross_slots(v) > 0)
         e = trimul::launch_cross_backward_bias(v->dtype, a, s);
     if (e != hipSuccess) return hip_fail(e, "attention backward kernel launch");

@@ -6,7 +6,8 @@
 //     dk_j = scale sum_i dS_ij q_i        dv_j = sum_i P_ij dout_i
 //
 // Three passes, each the owner of what it writes, so that every sum has one
-// order and nothing is added atomically: queries (dq, and D for the others),
+// order and nothing is added atomically (the first two side by side in one
+// launch where they are small): queries (dq, and D for the others),
 // keys (dk, dv; a key head's loop runs over the columns of all its query
 // heads) and, where a bias is given, tiles of it (whose loop runs over the
 // entries and heads that share it).  Each recomputes S and dP: writing dS
@@ -71,16 +72,19 @@ constexpr int q_waves() {
     return DP == 32 ? 3 : DP == 64 || sizeof(T) == 2 ? 2 : 1;
 }
 
-template <typename T, int DP, int KC, int WK, bool SOLO, bool BIAS, bool DIRECT>
-__global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_q(const CrossArgs a, int ctiles) {
+// LDS bytes of a work-group.
+template <typename T, int DP, int KC, int WK>
+constexpr int q_lds() { return (WK == 1 ? 2 : 4) * 2 * Tile<T, DP, KC>::kBytes; }
+
+// ROWS: leaves the statistics for the passes behind it (else k_cross_rows has done so).
+template <typename T, int DP, int KC, int WK, bool SOLO, bool BIAS, bool DIRECT, bool ROWS>
+__device__ __forceinline__ void query_pass(const CrossArgs& a, int ctiles, uint32_t blk, char* mem) {
     using TL = Tile<T, DP, KC>;
     constexpr int NT = 256 / WK, NB = KC / 32, ND = DP / 32, NS = DP / 16;
     constexpr bool FOLD = sizeof(T) == 2 && DP <= 64;          // dP's sum starts at -D (16 registers that hold it)
-    __shared__ __align__(16) char mem[(WK == 1 ? 2 : 4) * 2 * TL::kBytes];
     const int lane = threadIdx.x & 63, ql = lane & 31, hi = lane >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = WK == 1 ? threadIdx.x : lane;
 
-    uint32_t blk = xcd_block();
     if (SOLO) {
         blk = blk * 4 + w;
         if (blk >= (uint32_t)(a.batch * a.kv_heads)) return;             // (no barrier follows in this form)
@@ -146,7 +150,7 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
     }
     RowStat st;
     st.set(a.stats[row], a.stats[a.batch * a.heads * a.nq + row], D);
-    if (valid && !hi && (!MERGE || w == 0)) reinterpret_cast<float4*>(a.rows)[row] = make_float4(st.M, st.n2, st.sh, D);
+    if (ROWS && valid && !hi && (!MERGE || w == 0)) reinterpret_cast<float4*>(a.rows)[row] = make_float4(st.M, st.n2, st.sh, D);
     const bool far = __any(st.far());
     f32x16_t acc[ND];
 #pragma unroll
@@ -241,6 +245,12 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
                   MERGE ? w * ND : 0, hi, a.d, a.scale);
 }
 
+template <typename T, int DP, int KC, int WK, bool SOLO, bool BIAS, bool DIRECT>
+__global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_q(const CrossArgs a, int ctiles) {
+    __shared__ __align__(16) char mem[q_lds<T, DP, KC, WK>()];
+    query_pass<T, DP, KC, WK, SOLO, BIAS, DIRECT, true>(a, ctiles, xcd_block(), mem);
+}
+
 // ------------------------------------------------------------------ keys: dk, dv
 //
 // Lane: one key (K and V as B operands in registers), registers: the queries of
@@ -259,23 +269,29 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
 template <typename T, int DP, int WK, bool TWO>
 constexpr int kv_waves() { return TWO ? 2 : DP == 32 ? (sizeof(T) == 2 ? 3 : 2) : DP == 64 && sizeof(T) == 2 ? 2 : 1; }
 
+// LDS of a work-group: tiles, bias rows (four of them spread over the banks), statistics.
+template <typename T, int DP, int QC, int WK, bool BIAS>
+struct KvLds {
+    static constexpr int kBuf = WK == 1 ? 2 : 4, kKeys = 128 / WK;
+    static constexpr int kBRow = kKeys * (int)sizeof(T) + (sizeof(T) == 4 ? 16 : kKeys == 128 ? 64 : 0);
+    static constexpr int kBias = kBuf * 2 * Tile<T, DP, QC>::kBytes, kStat = kBias + (BIAS ? kBuf * QC * kBRow : 0);
+    static constexpr int kBytes = kStat + kBuf * 4 * QC * 4;
+};
+
 template <typename T, int DP, int QC, int WK, bool TWO, bool BIAS>
-__global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void k_cross_backward_kv(const CrossArgs a, int ktiles) {
+__device__ __forceinline__ void key_pass(const CrossArgs& a, int ktiles, uint32_t blk, char* mem) {
     using TL = Tile<T, DP, QC>;
+    using LD = KvLds<T, DP, QC, WK, BIAS>;
     constexpr int NB = QC / 32, ND = DP / 32, NS = DP / 16;
-    constexpr int NT = (TWO ? 512 : 256) / WK, KT = 128 / WK, BUF = WK == 1 ? 2 : 4;   // threads of a chunk, keys, buffers
-    // bias rows in LDS: four of them spread over the banks
-    constexpr int kBRow = KT * (int)sizeof(T) + (sizeof(T) == 4 ? 16 : KT == 128 ? 64 : 0);
-    constexpr int kBPieces = KT * (int)sizeof(T) / 16, kBN = QC * kBPieces / NT;
-    __shared__ __align__(16) char mem[BUF * 2 * TL::kBytes];
-    __shared__ __align__(16) char bmem[BIAS ? BUF * QC * kBRow : 16];
-    __shared__ __align__(16) float stat[BUF][4][QC];           // M, n2, sh, -D of a chunk's columns
+    constexpr int NT = (TWO ? 512 : 256) / WK, KT = LD::kKeys;   // threads of a chunk, keys
+    constexpr int kBRow = LD::kBRow, kBPieces = KT * (int)sizeof(T) / 16, kBN = QC * kBPieces / NT;
+    char* const bmem = mem + LD::kBias;
+    float(* const stat)[4][QC] = reinterpret_cast<float(*)[4][QC]>(mem + LD::kStat);   // M, n2, sh, -D of a chunk's columns
     const int lane = threadIdx.x & 63, kl = lane & 31, hi = lane >> 5;
     const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = WK == 1 ? threadIdx.x : lane;
     const int w = TWO ? wid & 3 : wid;
     const bool for_k = TWO && wid >= 4;                        // TWO: this wave's half
 
-    uint32_t blk = xcd_block();
     const int kt_ = (int)(blk % (uint32_t)ktiles);
     blk /= (uint32_t)ktiles;
     const int split = (int)(blk % (uint32_t)a.splits);
@@ -513,6 +529,49 @@ __global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void
         store_row<TWO ? 1 : ND>(to_k, dk, groups, g0, hi, a.d, a.scale);
         store_row<ND>(to_v, dv, groups, g0, hi, a.d, 1.f);
     }
+}
+
+template <typename T, int DP, int QC, int WK, bool TWO, bool BIAS>
+__global__ __launch_bounds__(TWO ? 512 : 256, (kv_waves<T, DP, WK, TWO>())) void k_cross_backward_kv(const CrossArgs a, int ktiles) {
+    __shared__ __align__(16) char mem[KvLds<T, DP, QC, WK, BIAS>::kBytes];
+    key_pass<T, DP, QC, WK, TWO, BIAS>(a, ktiles, xcd_block(), mem);
+}
+
+// ------------------------------------------------------------------ both at once
+//
+// Where neither pass fills the compute units they run side by side in one
+// launch; what the query pass would have left for the key pass comes from a
+// short launch of its own before it, 16 lanes of 8 channels to a row.
+template <typename T>
+__global__ __launch_bounds__(256) void k_cross_rows(const CrossArgs a) {
+    const int64_t rows = a.batch * a.heads * a.nq, at = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4), row = min(at, rows - 1);
+    const int64_t bh = row / a.nq, b = bh / a.heads;
+    const int qi = (int)(row - bh * a.nq), h = (int)(bh - b * a.heads), l = threadIdx.x & 15;
+    const T* gr = (const T*)a.dout.data + b * a.dout.batch + (int64_t)qi * a.dout.token + h * a.dout.head;
+    const T* orow = (const T*)a.out.data + b * a.out.batch + (int64_t)qi * a.out.token + h * a.out.head;
+    Frag<T> g, o;
+    load_row(gr, 0, l, a.d, g);             // (channels 8 l ..)
+    load_row(orow, 0, l, a.d, o);
+    float D = Frag<T>::dot(g, o);
+    if constexpr (sizeof(T) == 2) {
+        load_row((const bf16_t*)a.rest + row * a.d, 0, l, a.d, o);
+        D += Frag<T>::dot(g, o);
+    }
+#pragma unroll
+    for (int i = 8; i; i >>= 1) D += __shfl_xor(D, i);
+    RowStat st;
+    st.set(a.stats[row], a.stats[rows + row], D);
+    if (l == 0 && at < rows) reinterpret_cast<float4*>(a.rows)[row] = make_float4(st.M, st.n2, st.sh, D);
+}
+
+template <typename T, int DP, bool BIAS, bool DIRECT>
+__global__ __launch_bounds__(256, (q_waves<T, DP, 4>() < kv_waves<T, DP, 4, false>() ? q_waves<T, DP, 4>() : kv_waves<T, DP, 4, false>()))
+void k_cross_backward_both(const CrossArgs a, int ctiles, int ktiles, int q_blocks) {
+    constexpr int kQ = q_lds<T, DP, 32, 4>(), kKv = KvLds<T, DP, 32, 4, BIAS>::kBytes;
+    __shared__ __align__(16) char mem[kQ > kKv ? kQ : kKv];
+    const uint32_t blk = xcd_block();
+    if (blk < (uint32_t)q_blocks) query_pass<T, DP, 32, 4, false, BIAS, DIRECT, false>(a, ctiles, blk, mem);
+    else key_pass<T, DP, 32, 4, false, BIAS>(a, ktiles, blk - (uint32_t)q_blocks, mem);
 }
 
 // The splits' sums of dk and dv, four channels a thread, in the order of the splits.
@@ -777,6 +836,23 @@ hipError_t backward_kv(const CrossArgs& args, const CrossKvPlan& p, hipStream_t 
     return hipGetLastError();
 }
 
+template <typename T, int DP, bool BIAS, bool DIRECT>
+hipError_t backward_both(const CrossArgs& args, const CrossKvPlan& p, hipStream_t s) {
+    if constexpr (kv_may_be_few(sizeof(T) == 2 ? 1 : 0, DP)) {
+        CrossArgs a = args;
+        a.splits = 1;
+        const int ctiles = (a.nq * a.group + 31) / 32, q_blocks = (int)(a.batch * a.kv_heads) * ctiles;
+        hipLaunchKernelGGL((k_cross_rows<T>), dim3((unsigned)((a.batch * a.heads * a.nq + 15) / 16)), dim3(256), 0, s, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((k_cross_backward_both<T, DP, BIAS, DIRECT>), dim3((unsigned)(q_blocks + (int)(a.batch * (a.kv_heads / a.key_div)) * p.ktiles)),
+                           dim3(256), 0, s, a, ctiles, p.ktiles, q_blocks);
+        return hipGetLastError();
+    } else {
+        return hipErrorInvalidValue;        // (cross_both is false)
+    }
+}
+
 template <typename T, int DP>
 hipError_t backward_bias(const CrossArgs& a, hipStream_t s) {
     constexpr int KC = kKeyChunk<T>;
@@ -825,6 +901,17 @@ CrossKvPlan cross_kv_plan(int dtype, int d, int64_t heads, int64_t nk, int64_t p
     return p;
 }
 
+// Both passes side by side where their work-groups of 32 columns and of 32 keys together
+// are one to a compute unit at most.  (300 x 500, 8 heads of 64 with a bias, fp32, 80 + 128: 25 and
+// 23 us one after the other, 26 together and 4 for the rows before; 512 x 512, bf16,
+// 128 + 128: 12.5 and 10.7, 13.2 and 4.  With more they take turns on the compute units: 200 x 2000, 8
+// heads of 32, 56 + 504: 19.6 and 8.0, 32.9 and 3.7.)
+bool cross_both(const CrossArgs& a, const CrossKvPlan& p) {
+    const int64_t heads = a.batch * a.kv_heads, cols = (int64_t)a.nq * a.group;
+    return p.few && p.splits == 1 && a.nq > 0 && cross_few(heads, cols) && !cross_solo(heads, cols) &&
+           heads * ((cols + 31) / 32) + a.batch * (a.kv_heads / a.key_div) * p.ktiles <= 256;
+}
+
 size_t cross_kv_part_floats(const CrossKvPlan& p, int64_t heads, int64_t nk, int d) {
     return p.splits > 1 ? (size_t)p.splits * 2 * (size_t)heads * (size_t)nk * (size_t)d : 0;
 }
@@ -866,6 +953,11 @@ size_t cross_dbias_part_floats(int dtype, int splits, int64_t slots, int64_t nq,
 #define CROSS_KV(T, DP) (a.bias.data ? backward_kv<T, DP, true>(a, p, s) : backward_kv<T, DP, false>(a, p, s))
 #define CROSS_BIAS(T, DP) (backward_bias<T, DP>(a, s))
 
+#define CROSS_BOTH(T, DP)                                                    \
+    (!a.bias.data ? backward_both<T, DP, false, false>(a, p, s)              \
+                  : a.direct_bias ? backward_both<T, DP, true, true>(a, p, s) : backward_both<T, DP, true, false>(a, p, s))
+
+hipError_t launch_cross_backward_both(int dtype, const CrossArgs& a, const CrossKvPlan& p, hipStream_t s) { return CROSS_BY_TYPE(CROSS_BOTH); }
 hipError_t launch_cross_backward_q(int dtype, const CrossArgs& a, hipStream_t s) { return CROSS_BY_TYPE(CROSS_Q); }
 hipError_t launch_cross_backward_kv(int dtype, const CrossArgs& a, const CrossKvPlan& p, hipStream_t s) { return CROSS_BY_TYPE(CROSS_KV); }
 hipError_t launch_cross_backward_bias(int dtype, const CrossArgs& a, hipStream_t s) { return CROSS_BY_TYPE(CROSS_BIAS); }

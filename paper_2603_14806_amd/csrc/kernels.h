@@ -246,6 +246,9 @@ size_t cross_kv_part_floats(const CrossKvPlan& p, int64_t heads, int64_t nk, int
 int cross_dbias_splits(int dtype, int d, int64_t slots, int64_t shared, int64_t nq, int64_t nk);
 size_t cross_dbias_part_floats(int dtype, int splits, int64_t slots, int64_t nq, int64_t nk);
 hipError_t launch_cross_forward(int dtype, const CrossArgs& a, const CrossPlan& p, hipStream_t s);
+// Whether the query pass and the key pass run in one launch (launch_cross_backward_both, for the two).
+bool cross_both(const CrossArgs& a, const CrossKvPlan& p);
+hipError_t launch_cross_backward_both(int dtype, const CrossArgs& a, const CrossKvPlan& p, hipStream_t s);
 hipError_t launch_cross_backward_q(int dtype, const CrossArgs& a, hipStream_t s);
 hipError_t launch_cross_backward_kv(int dtype, const CrossArgs& a, const CrossKvPlan& p, hipStream_t s);
 hipError_t launch_cross_backward_bias(int dtype, const CrossArgs& a, hipStream_t s);

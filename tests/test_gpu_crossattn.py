@@ -148,6 +148,24 @@ def test_many_heads_of_few_queries(shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(2, 130, 1500, 4, 2, 64), (1, 257, 255, 8, 8, 24), (4, 130, 700, 4, 4, 32),
+                                   (3, 400, 300, 4, 4, 128), (2, 520, 40, 8, 8, 40)])
+def test_small_backward_passes(shape, dtype):
+    """Tiles of 32 queries and of 32 keys, on both sides of 256 of them together (one launch or two); without dk
+    and dv the same dq and dbias within their error."""
+    B, nq, nk, H, Hk, d = shape
+    for bias, mask in ((None, None), ((B, H), "random"), ((1, H), "pad")):
+        what = f"{dtype} {shape} bias={bias} mask={mask}"
+        x = cuda(make(B, nq, nk, H, Hk, d, dtype, bias, mask))
+        got, _ = call(x)
+        check(got, x, what, dtype)
+        out, stats = A.cross_attention(x["q"], x["k"], x["v"], x.get("bias"), x.get("mask"), return_stats=True)
+        dq, dk, dv, dbias = A.cross_attention_backward(x["q"], x["k"], x["v"], out, stats, x["dout"], x.get("bias"), x.get("mask"), need_kv=False)
+        assert dk is None and dv is None
+        check({"dq": dq, "dbias": dbias}, x, what + " alone", dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_shared_by_many_entries(dtype):
     """Triangle attention's shape: the rows of a pair tensor as the batch, one bias and its gradient for all (the
     sum over the rows split over work-groups), and the library's own triangle attention on the same inputs."""
