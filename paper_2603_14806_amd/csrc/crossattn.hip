@@ -60,6 +60,13 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
     const int col = min(cw + ql, ncols - 1);
     const int qi = col / a.group, h = hk * a.group + (col - qi * a.group);
 
+    // (before the first chunk: behind it, 4% longer for 384 x 4 heads of 384 x 384, and 7% for 300 x 500 in fp32)
+    Frag<T> qf[NS];
+    {
+        const T* row = (const T*)a.q.data + b * a.q.batch + (int64_t)qi * a.q.token + h * a.q.head;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) load_row(row, s, hi, a.d, qf[s]);
+    }
     const T* kb = (const T*)a.k.data + b * a.k.batch + hk / a.key_div * a.k.head;
     const T* vb = (const T*)a.v.data + b * a.v.batch + hk / a.key_div * a.v.head;
     const uint8_t* mask = a.mask ? a.mask + b * a.mask_batch : nullptr;
@@ -94,12 +101,6 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
     if (BIAS) {
         bp.init(a, b, hk, min(cw, ncols - 1), min(cw + 31, ncols - 1), qi, h, hi);
         bp.load(ks + c0 * KC, a.nk);
-    }
-    Frag<T> qf[NS];
-    {
-        const T* row = (const T*)a.q.data + b * a.q.batch + (int64_t)qi * a.q.token + h * a.q.head;
-#pragma unroll
-        for (int s = 0; s < NS; ++s) load_row(row, s, hi, a.d, qf[s]);
     }
     for (int c = c0; c < nchunks; c += STEP) {
         char* kt = mem + (WK == 1 ? (c & 1) : w) * 2 * TL::kBytes;

@@ -22,7 +22,7 @@ namespace trimul {
 namespace {
 
 // A query's statistics as the weights use them: P = exp2((x - M) log2 e + n2) = exp2(x log2 e + sh).
-// A query with no key: M = 0, n2 = -inf, P = 0.  The query pass leaves them, and D, in the workspace
+// A query with no key: M = 0, n2 = -inf, P = 0.  The query pass (or k_cross_rows) leaves them, and D, in the workspace
 // for the other two.
 struct RowStat {
     float M, n2, sh, D;
