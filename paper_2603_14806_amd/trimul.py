@@ -372,6 +372,7 @@ class TriMul:
         wd = {k: v.to(self.device, TORCH_DTYPE[DTYPE_CODE[dtype]]).contiguous() for k, v in weights.items()}
         self.h = tri_mul_init(wd, dtype, out_dtype, eps, stream=stream)
         torch.cuda.synchronize(self.device)
+        self._on = wd["w_o"].device                  # self.device with its index
         self._ws = None
 
     def close(self):
@@ -397,15 +398,33 @@ class TriMul:
             out = torch.empty((N, N, 128), dtype=TORCH_DTYPE[DTYPE_CODE[self.out_dtype]], device=self.device)
         return out
 
+    def _tokens(self, z, mask=None, out=None):
+        """N of a call on the [N][N][128] tensor z, after checking what the kernels, which see addresses alone, take
+        for granted: types, sizes, contiguous data, the layer's device."""
+        N = z.shape[0] if z.dim() else 0
+        for name, t, dtype in (("z", z, self.dtype), ("out", out, self.out_dtype)):
+            if not isinstance(t, torch.Tensor):
+                continue
+            if t.dtype != TORCH_DTYPE[DTYPE_CODE[dtype]]:
+                raise ValueError(f"{name} must be of the layer's type {dtype}, not {t.dtype}")
+            if t.numel() != N * N * 128 or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous [N, N, 128] tensor, not {list(t.shape)} with strides {t.stride()}")
+        if isinstance(mask, torch.Tensor) and (mask.element_size() != 1 or mask.numel() != N or not mask.is_contiguous()):
+            raise ValueError(f"mask must hold {N} uint8 or bool values, not {list(mask.shape)} of {mask.dtype}")
+        for name, t in (("z", z), ("mask", mask), ("out", out)):
+            if isinstance(t, torch.Tensor) and t.device != self._on:
+                raise ValueError(f"{name} must live on the GPU of the layer, {self._on}, not on {t.device}")
+        return N
+
     def outgoing(self, z, mask=None, out=None, stream=None):
-        N = z.shape[0]
+        N = self._tokens(z, mask, out)
         out = self._out(N, out)
         ws, need = self.workspace(N)
         tri_mul_outgoing(self.h, z, mask, N, out, ws, need, stream)
         return out
 
     def incoming(self, z, mask=None, out=None, stream=None):
-        N = z.shape[0]
+        N = self._tokens(z, mask, out)
         out = self._out(N, out)
         ws, need = self.workspace(N)
         tri_mul_incoming(self.h, z, mask, N, out, ws, need, stream)
@@ -473,6 +492,7 @@ class TriMul:
             raise ValueError("z must have the storage dtype and dout the output dtype of the layer")
         if not (z.is_contiguous() and dout.is_contiguous()):
             raise ValueError("z and dout must be contiguous")
+        self._tokens(z, mask)
         grads = {k: torch.empty(v, dtype=torch.float32, device=self.device) for k, v in WEIGHT_SHAPES.items()}
         dz = torch.empty_like(z)
         wsb = tri_mul_backward_workspace_size(self.h, N)
@@ -486,8 +506,9 @@ class TriMul:
     def residual(self, z, mask=None, direction="outgoing", p=0.25, seed=0, offset=0, share="rows", out=None,
                  stream=None):
         """z + dropout(update of z) in the storage dtype (include/pair_dropout.h; the pair stack shares the mask
-        along the rows); with p = 0 the plain residual addition.  out may be z itself."""
+        along the rows); with p = 0 the plain residual addition.  z is contiguous; out may be z itself."""
         from . import dropout
+        self._tokens(z, mask)
         with on_stream(z.device, stream):
             return dropout.dropout_add(self(z, mask, direction), z, p, seed, offset, share, out=out)
 
@@ -495,6 +516,7 @@ class TriMul:
                           stream=None, saved=None):
         """Gradients of sum(residual(z) * dout): (dz, grads), dout and dz in the storage dtype."""
         from . import dropout
+        self._tokens(z, mask)
         with on_stream(z.device, stream):
             du = dropout.dropout_backward(dout, p, seed, offset, share, dtype=self.out_dtype)
             dz, grads = self.backward(z, du, mask, direction, saved=saved)
