@@ -212,6 +212,11 @@ class on_stream:
             self.entered.close()
 
 
+def _place(device):
+    """(The current stream's handle, whether it is being captured.)"""
+    return torch._C._cuda_getCurrentRawStream(device.index), torch.cuda.is_current_stream_capturing()
+
+
 # ---------------------------------------------------------------- C names
 
 def tri_mul_init(weights, dtype="bf16", out_dtype="f32", eps=1e-5, c_z=128, c=128, stream=None):
@@ -373,7 +378,7 @@ class TriMul:
         self.h = tri_mul_init(wd, dtype, out_dtype, eps, stream=stream)
         torch.cuda.synchronize(self.device)
         self._on = wd["w_o"].device                  # self.device with its index
-        self._ws = None
+        self._ws = {}                                # workspaces by _place
 
     def close(self):
         if self.h:
@@ -387,11 +392,15 @@ class TriMul:
             pass
 
     def workspace(self, N):
-        need = tri_mul_workspace_size(self.h, N)
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = None
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return self._ws, need
+        """The workspace of the calls on the current stream, and the bytes that one for N tokens needs.  A call leaves
+        its panels and C in it.  Each stream has its own, so that calls on two may run at once; a captured call takes
+        one for itself alone, which its graph keeps (ask for it after the call, in the same capture)."""
+        need, place = tri_mul_workspace_size(self.h, N), _place(self._on)
+        ws = self._ws.get(place)
+        if ws is None or ws.numel() < need:
+            self._ws.pop(place, None)
+            ws = self._ws[place] = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return ws, need
 
     def _out(self, N, out):
         if out is None:
@@ -416,19 +425,22 @@ class TriMul:
                 raise ValueError(f"{name} must live on the GPU of the layer, {self._on}, not on {t.device}")
         return N
 
-    def outgoing(self, z, mask=None, out=None, stream=None):
+    def _update(self, entry, z, mask, out, stream):
         N = self._tokens(z, mask, out)
-        out = self._out(N, out)
-        ws, need = self.workspace(N)
-        tri_mul_outgoing(self.h, z, mask, N, out, ws, need, stream)
+        with on_stream(self._on, stream) as s:
+            out = self._out(N, out)
+            place = _place(self._on)
+            if place[1]:
+                self._ws.pop(place, None)
+            ws, need = self.workspace(N)
+            entry(self.h, z, mask, N, out, ws, need, s)
         return out
 
+    def outgoing(self, z, mask=None, out=None, stream=None):
+        return self._update(tri_mul_outgoing, z, mask, out, stream)
+
     def incoming(self, z, mask=None, out=None, stream=None):
-        N = self._tokens(z, mask, out)
-        out = self._out(N, out)
-        ws, need = self.workspace(N)
-        tri_mul_incoming(self.h, z, mask, N, out, ws, need, stream)
-        return out
+        return self._update(tri_mul_incoming, z, mask, out, stream)
 
     def __call__(self, z, mask=None, direction="outgoing", out=None, stream=None):
         return (self.outgoing if direction == "outgoing" else self.incoming)(z, mask, out, stream)

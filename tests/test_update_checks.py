@@ -11,7 +11,7 @@ N = 6
 def layer(dtype="bf16", out_dtype="f32"):
     """A layer without a handle: whatever gets past the checks fails with another error."""
     t = T.TriMul.__new__(T.TriMul)
-    t.dtype, t.out_dtype, t.device, t.h, t._ws = dtype, out_dtype, torch.device("cpu"), None, None
+    t.dtype, t.out_dtype, t.device, t.h, t._ws = dtype, out_dtype, torch.device("cpu"), None, {}
     t._on = torch.device("cuda", 0)
     return t
 
@@ -55,3 +55,37 @@ def test_outputs_refused():
                           (torch.zeros(N, N + 1, 128)[:, :N], "out must be a contiguous")):
             with pytest.raises(ValueError, match=word):
                 getattr(layer(), name)(Z, None, out)
+
+
+def test_workspaces_by_stream_and_capture(monkeypatch):
+    """Calls on two streams may run at once and a graph keeps the memory it was captured with, so neither shares a
+    workspace; calls on one stream, outside of a capture, do (what a call leaves there can be read)."""
+    at, used = [(1, False)], []
+    monkeypatch.setattr(T, "_place", lambda device: at[0], raising=False)
+    monkeypatch.setattr(T, "tri_mul_workspace_size", lambda h, n: 4096 * n)
+    monkeypatch.setattr(T, "_stream", lambda s: at[0][0])
+
+    class Here:
+        def __init__(self, *a): pass
+        def __enter__(self): return at[0][0]
+        def __exit__(self, *a): pass
+
+    def update(h, z, mask, n, out, ws, need, stream):
+        assert ws.numel() >= need == 4096 * n
+        used.append(ws)
+    monkeypatch.setattr(T, "on_stream", Here)
+    monkeypatch.setattr(T, "tri_mul_outgoing", update)
+    t = layer()
+    t._on, t._ws = torch.device("cpu"), {}
+
+    def call(place, n):
+        at[0] = place
+        t.outgoing(torch.zeros(n, n, 128, dtype=torch.bfloat16))
+        assert t.workspace(n)[0].data_ptr() == used[-1].data_ptr()
+        return used[-1].data_ptr()
+    a, b = call((1, False), 8), call((2, False), 8)
+    assert a != b and call((1, False), 8) == a and call((2, False), 4) == b
+    graphs = [call((1, True), 8), call((1, True), 8), call((2, True), 4)]
+    assert len({a, b, *graphs}) == 5                   # (all are held here)
+    assert call((1, False), 8) == a
+    assert call((1, False), 9) not in (a, b, *graphs)
