@@ -115,6 +115,25 @@ def _checked(name, t, dtype, device, shape):
     return CrossAttnTensor(t.data_ptr(), s[0], s[1], s[2])
 
 
+def _checked_bias(t, batch, heads, nq, nk):
+    """bias_tensor(t) after checking its shape, unit stride along the keys, and that the padding of its last row, which
+    is read up to a multiple of 8 values, is memory of t's."""
+    if t.dim() == 3:
+        t = t[None]
+    n = t.shape
+    if len(n) != 4 or n[0] not in (1, batch) or n[1] not in (1, heads) or n[2] != nq or n[3] != nk:
+        raise ValueError(f"bias must be [{batch} or 1][{heads} or 1][{nq}][{nk}], not {list(n)}")
+    if not t.numel():
+        return CrossAttnBias()
+    s = t.stride()
+    if nk > 1 and s[3] != 1:
+        raise ValueError("bias must have unit stride along its last axis")
+    end = t.storage_offset() + (n[0] - 1) * s[0] + (n[1] - 1) * s[1] + (nq - 1) * s[2] + (nk + 7) // 8 * 8
+    if (nq == 1 or s[2] % 8 == 0) and end * t.element_size() > t.untyped_storage().nbytes():
+        raise ValueError("bias must be a view of a padded tensor: its last row is read up to a multiple of 8 values, past the end of its memory")
+    return bias_tensor(t)
+
+
 def view(q, k, v, bias=None, mask=None, scale=None):
     """cross_attn_view_t of the call (the tensors are kept alive by the caller), after checking shapes and types."""
     return _call(q, k, v, bias, mask, scale)[0]
@@ -138,14 +157,7 @@ def _call(q, k, v, bias, mask, scale):
     if bias is not None:
         if bias.dtype != dtype or bias.device != device:
             raise ValueError(f"bias must be a {dtype} tensor on {device}")
-        if bias.dim() == 3:
-            bias = bias[None]
-        if bias.dim() != 4 or bias.shape[0] not in (1, batch) or bias.shape[1] not in (1, heads) or tuple(bias.shape[2:]) != (nq, nk):
-            raise ValueError(f"bias must be [{batch} or 1][{heads} or 1][{nq}][{nk}], not {list(bias.shape)}")
-        if bias.numel():
-            if nk > 1 and bias.stride(3) != 1:
-                raise ValueError("bias must have unit stride along its last axis")
-            w.bias = bias_tensor(bias)
+        w.bias = _checked_bias(bias, batch, heads, nq, nk)
     if mask is not None:
         if mask.dtype not in (torch.uint8, torch.bool) or mask.device != device:
             raise ValueError(f"mask must be a uint8 or bool tensor on {device}")
@@ -164,7 +176,7 @@ def cross_attention(q, k, v, bias=None, mask=None, scale=None, return_stats=Fals
     multiple of kv_heads, d a multiple of 8 up to 128; any strides that are multiples of 16 bytes).
 
     bias: [batch or 1][heads or 1][nq][nk] (or without the first axis) of q's type whose rows are a multiple of 8
-    values apart (a view of a padded tensor is fine); an axis of length 1 is shared.  mask: [batch or 1][nk] or [nk],
+    values apart (a view of a padded tensor is fine; rows are read up to a multiple of 8 values); an axis of length 1 is shared.  mask: [batch or 1][nk] or [nk],
     uint8 or bool, nonzero where the key is present.  scale: default 1 / sqrt(d).  With return_stats also what
     cross_attention_backward takes: a flat float32 tensor of the library's own layout (first the maxima and the sums,
     [2][batch][heads][nq])."""
