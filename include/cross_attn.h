@@ -59,7 +59,8 @@ typedef struct {
 typedef struct {
     void* data;                 /* 16-byte aligned; NULL: no bias                                     */
     int64_t batch, head;        /* from an entry's (head's) bias to the next's; 0: one for all        */
-    int64_t row;                /* >= nk and at most 2^24; all three strides multiples of 8           */
+    int64_t row;                /* >= nk and at most 2^24; all three strides multiples of 8 (none is
+                                   looked at along an axis of length 1)                               */
 } cross_attn_bias_t;
 
 typedef struct {

@@ -1218,10 +1218,11 @@ namespace {
 constexpr int64_t kCrossMaxTokens = int64_t(1) << 24, kCrossMaxToken = int64_t(1) << 23;
 constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;    // work-groups of 256 threads: 2^32 threads at most
 
+// (an axis of length 1 has no stride)
 int cross_bias(const cross_attn_view_t* v, const cross_attn_bias_t* b, const char* name) {
     if (!aligned16(b->data)) return fail(TRI_MUL_EINVAL, "%s must be 16-byte aligned", name);
-    if (b->row < v->nk || b->row % 8 || b->row > kCrossMaxTokens) return fail(TRI_MUL_EINVAL, "row stride %lld of %s must be >= nk, a multiple of 8 and at most 2^24", (long long)b->row, name);
-    if (b->batch < 0 || b->head < 0 || b->batch % 8 || b->head % 8) return fail(TRI_MUL_EINVAL, "strides of %s must be multiples of 8, and not negative", name);
+    if (v->nq > 1 && (b->row < v->nk || b->row % 8 || b->row > kCrossMaxTokens)) return fail(TRI_MUL_EINVAL, "row stride %lld of %s must be >= nk, a multiple of 8 and at most 2^24", (long long)b->row, name);
+    if ((v->batch > 1 && (b->batch < 0 || b->batch % 8)) || (v->heads > 1 && (b->head < 0 || b->head % 8))) return fail(TRI_MUL_EINVAL, "strides of %s must be multiples of 8, and not negative", name);
     return TRI_MUL_OK;
 }
 
@@ -1242,11 +1243,13 @@ int cross_check(const cross_attn_view_t* v) {
     return TRI_MUL_OK;
 }
 
+int64_t cross_bias_row(const cross_attn_view_t* v) { return v->nq > 1 ? v->bias.row : (v->nk + 7) / 8 * 8; }
+
 // Query heads taken together with their key head: all of a group, unless the rows of 32 columns of the bias
 // would not fit one buffer descriptor (2^31 bytes).
 int cross_group(const cross_attn_view_t* v) {
     const int64_t group = v->heads / v->kv_heads;
-    const __int128 span = (__int128)31 * v->bias.row + (__int128)(group - 1) * v->bias.head + v->nk + 8;
+    const __int128 span = (__int128)31 * cross_bias_row(v) + (__int128)(group - 1) * v->bias.head + v->nk + 8;
     return v->bias.data && span * (int64_t)esize(v->dtype) > ((int64_t)1 << 31) ? 1 : (int)group;
 }
 int64_t cross_cols(const cross_attn_view_t* v) { return v->nq * cross_group(v); }
@@ -1284,7 +1287,7 @@ trimul::CrossArgs cross_args(const cross_attn_view_t* v, const cross_attn_tensor
     a.k = cross_arg(v, k, v->nk);
     a.v = cross_arg(v, vv, v->nk);
     a.out = cross_arg(v, out, v->nq);
-    a.bias = {v->bias.data, v->bias.batch, v->bias.head, v->bias.row};
+    a.bias = {v->bias.data, v->bias.batch, v->bias.head, cross_bias_row(v)};
     a.mask = v->mask;
     a.mask_batch = v->mask_batch;
     a.batch = v->batch;

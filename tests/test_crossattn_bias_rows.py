@@ -1,9 +1,13 @@
 """The rows of an attention bias are read up to a multiple of 8 values: the torch side refuses one whose last row's
 padding is not its own memory.  No GPU: the checks come before any launch."""
+import ctypes
+import os
+
 import pytest
 import torch
 
 from paper_2603_14806_amd import attention as A
+from paper_2603_14806_amd import trimul as T
 
 
 def check(t, batch, heads, nq, nk):
@@ -39,3 +43,44 @@ def test_padded_views_are_taken():
     for t in (full[..., :20], full[..., ::2]):
         with pytest.raises(ValueError):
             check(t, 2, 3, 5, 12)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(T.LIB_PATH):
+        from paper_2603_14806_amd import build
+        build.build()
+    return A.lib()
+
+
+@pytest.mark.parametrize("sizes,bias,ok", [
+    (dict(nq=1), (0, 56, 50), True), (dict(nq=1), (0, 56, 3), True), (dict(nq=2), (0, 56, 50), False), (dict(nq=2), (0, 56, 3), False),
+    (dict(batch=1), (5, 56, 56), True), (dict(batch=2), (5, 56, 56), False),
+    (dict(heads=1, kv_heads=1), (8, 3, 56), True), (dict(nq=1), (0, 57, 50), False)])
+def test_strides_of_axes_of_length_one_are_not_looked_at(lib, sizes, bias, ok):
+    w = A.CrossAttnView(1, 9, 50, 4, 2, 32, T.TRI_MUL_BF16, 0.5, A.CrossAttnBias(1 << 12, *bias))
+    for k, x in sizes.items():
+        setattr(w, k, x)
+    n = ctypes.c_size_t()
+    for size in (lib.cross_attn_workspace_size, lib.cross_attn_backward_workspace_size):
+        assert size(ctypes.byref(w), ctypes.byref(n)) == (T.TRI_MUL_OK if ok else T.TRI_MUL_EINVAL)
+
+
+@pytest.mark.gpu
+@pytest.mark.skipif(not torch.cuda.is_available(), reason="no GPU visible")
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,H,Hk", [(1, 4, 2), (3, 2, 2), (1, 1, 1)])
+def test_one_query_with_any_row_stride(B, H, Hk, dtype):
+    """torch names the stride of an axis of length 1 as it likes: 257 for the rows below, 264 values apart in truth."""
+    from tests.test_gpu_crossattn import call, check as against, cuda, make
+    x = cuda(make(B, 1, 257, H, Hk, 32, dtype, (B, H), "random"))
+    want, _ = call(x)
+    rows = torch.zeros(B, H, 264, dtype=x["q"].dtype, device="cuda")
+    rows[..., :257] = x["bias"][:, :, 0]
+    y = dict(x, bias=rows[..., :257].unsqueeze(2))
+    assert y["bias"].stride(2) == 257 and y["bias"].shape == x["bias"].shape
+    got, _ = call(y)
+    against(got, y, f"single query {dtype}", dtype)
+    assert all(torch.equal(got[n], want[n]) for n in want)
+    with pytest.raises(ValueError, match="padded"):            # 257 values and nothing behind them
+        A.cross_attention(x["q"], x["k"], x["v"], torch.zeros(1, 1, 1, 257, dtype=x["q"].dtype, device="cuda"))
