@@ -1480,7 +1480,9 @@ trimul::DropoutArgs dropout_args(const pair_dropout_view_t* v) {
     a.n_cols = v->n_cols;
     a.seed = v->seed;
     a.offset = v->offset;
-    a.threshold = (uint32_t)std::min(std::nearbyint(v->p * 4294967296.0), 4294967295.0);
+    const double threshold = std::nearbyint(v->p * 4294967296.0);
+    a.threshold = (uint32_t)std::min(threshold, 4294967295.0);
+    a.any = threshold < 4294967296.0 ? ~0u : 0u;
     a.scale = (float)(1.0 / (1.0 - v->p));
     return a;
 }

@@ -83,7 +83,7 @@ __device__ __forceinline__ uint32_t kept(uint64_t e, const DropoutArgs& a) {
     if constexpr (V == 1) {
         const Words w = philox(e >> 2, a.offset, a.seed);
         const uint32_t i = (uint32_t)e & 3;
-        return (i == 0 ? w.w[0] : i == 1 ? w.w[1] : i == 2 ? w.w[2] : w.w[3]) >= a.threshold ? 1u : 0u;
+        return (i == 0 ? w.w[0] : i == 1 ? w.w[1] : i == 2 ? w.w[2] : w.w[3]) >= a.threshold ? a.any & 1u : 0u;
     } else {
         uint32_t m = 0;
 #pragma unroll
@@ -92,7 +92,7 @@ __device__ __forceinline__ uint32_t kept(uint64_t e, const DropoutArgs& a) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) m |= (w.w[j] >= a.threshold ? 1u : 0u) << (4 * i + j);
         }
-        return m;
+        return m & a.any;
     }
 }
 

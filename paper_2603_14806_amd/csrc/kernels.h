@@ -260,6 +260,7 @@ struct DropoutArgs {
     int64_t rows, cols, channels, row0, col0, n_cols, ld_in, ld_res, ld_res_out;   // row strides: x, res, out
     uint64_t seed, offset;
     uint32_t threshold;   // dropped below it
+    uint32_t any;         // ~0; 0 where the threshold is 2^32, which no word reaches: nothing is kept
     float scale;
     int64_t loop;                    // filled in by the launcher, as are the next
     int blocks, lanes, span;

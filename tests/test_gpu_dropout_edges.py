@@ -1,0 +1,44 @@
+"""The dropout mask at its edges against the oracle: a rate that rounds to 2^32 steps, above every word."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2603_14806_amd import dropout as D
+from tests.gpu_util import host, needs_gpu
+
+# with seed 1 and offset 0 the word of this element is 2^32 - 1 (the largest; one in 2^32 is)
+SEED, LAST = 1, 6845800136
+
+
+def place_of(channels, n_cols, rows, cols):
+    """A tile around that element: (row0, col0) and the element's index in it."""
+    r, rest = divmod(LAST, n_cols * channels)
+    j, c = divmod(rest, channels)
+    row0, col0 = r - rows // 2, max(0, min(j - cols // 2, n_cols - cols))
+    return dict(row0=row0, col0=col0, n_cols=n_cols), (r - row0, j - col0, c)
+
+
+@pytest.mark.parametrize("channels,n_cols", [(8, 1000), (12, 97), (7, 101), (1, 5)])
+def test_the_largest_word(channels, n_cols):
+    place, at = place_of(channels, n_cols, 3, 5)
+    m = oracle.keep(3, 5, channels, 1 - 2.0 ** -32, SEED, 0, "none", **place)
+    assert m[at] and m.sum() == 1
+    assert not oracle.keep(3, 5, channels, 1 - 2.0 ** -40, SEED, 0, "none", **place).any()
+
+
+@pytest.mark.gpu
+@needs_gpu
+@pytest.mark.parametrize("channels,n_cols", [(8, 1000), (12, 97), (7, 101), (1, 5)])
+@pytest.mark.parametrize("p", [0.0, 1 - 2.0 ** -32, 1 - 2.0 ** -33, 1 - 2.0 ** -40, 1 - 2.0 ** -53])
+def test_rates_next_to_one(p, channels, n_cols):
+    """2^32 p rounds to 2^32 - 1 (kept: the largest word alone) or to 2^32 (nothing)."""
+    place, at = place_of(channels, n_cols, 3, 5)
+    x = torch.full((3, 5, channels), 0.5, device="cuda")
+    z = torch.ones_like(x)
+    keep = oracle.keep(3, 5, channels, p, SEED, 0, "none", **place)
+    assert bool(keep[at]) == (round(p * 2 ** 32) < 2 ** 32)
+    term = np.where(keep, 0.5 / (1 - p), 0.0)
+    # powers of two: exact but for the sum's own rounding
+    assert np.abs(host(D.dropout_add(x, z, p, SEED, 0, **place)) - (1 + term)).max() <= 2.0 ** -24 * (1 + term.max())
+    assert np.array_equal(host(D.dropout_backward(x, p, SEED, 0, **place)), term)
