@@ -81,18 +81,24 @@ def dropout_add(x, residual=None, p=0.25, seed=0, offset=0, share="none", row0=0
     """residual + dropout(x): [rows][cols][channels] float32 or bfloat16 tensors (x and residual of a type each; rows may
     be further apart than cols * channels), the result of the residual's type (without one: out_dtype "f32" or "bf16",
     default x's).  share: "none", "rows" (all rows have the same mask) or "columns".  row0, col0, n_cols: the
-    place of a tile in a tensor of n_cols columns.  out may be residual or x itself."""
+    place of a tile in a tensor of n_cols columns.  out may be residual or x itself; its rows are as far apart as
+    residual's (without an out, rows that are further apart are copied first)."""
     ld_x = _rows("x", x)
     dt = residual.dtype if residual is not None else x.dtype if out_dtype is None else _t.TORCH_DTYPE[DTYPE_CODE[out_dtype]]
     with on_stream(x.device, stream) as s:
+        ld_res = None if residual is None else _rows("residual", residual, x.shape, x.device)
         if out is None:
-            out, ld = x.new_empty(x.shape, dtype=dt), x.shape[1] * x.shape[2]
+            ld = x.shape[1] * x.shape[2]
+            if ld_res is None or ld_res == ld:
+                out = x.new_empty(x.shape, dtype=dt)
+            else:                                    # (the kernel has one row stride for both)
+                out = residual = residual.contiguous()
         else:
             ld = _rows("out", out, x.shape, x.device)
             if out.dtype != dt:
                 raise ValueError(f"out must be {dt}, not {out.dtype}")
-        if residual is not None and _rows("residual", residual, x.shape, x.device) != ld:
-            raise ValueError("residual and out must have the same row stride")
+            if ld_res is not None and ld_res != ld:
+                raise ValueError("residual and out must have the same row stride")
         v = _view(x.shape, ld_x, ld, _DTYPES[x.dtype], _DTYPES[dt], p, seed, offset, share, row0, col0, n_cols)
         pair_dropout_add(v, x, residual, out, s)
     return out

@@ -42,3 +42,25 @@ def test_rates_next_to_one(p, channels, n_cols):
     # powers of two: exact but for the sum's own rounding
     assert np.abs(host(D.dropout_add(x, z, p, SEED, 0, **place)) - (1 + term)).max() <= 2.0 ** -24 * (1 + term.max())
     assert np.array_equal(host(D.dropout_backward(x, p, SEED, 0, **place)), term)
+
+
+@pytest.mark.gpu
+@needs_gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_residual_rows_of_a_larger_tensor(dtype):
+    """x and residual both tiles of larger tensors, with and without an out: the result of contiguous copies."""
+    g = torch.Generator().manual_seed(4)
+    big, wide = (torch.randn((9, n, 16), generator=g).to(dtype).cuda() for n in (20, 31))
+    x, z = big[2:7, 4:15], wide[1:6, 7:18]
+    before = wide.clone()
+    place = dict(row0=2, col0=4, n_cols=20)
+    want = D.dropout_add(x.contiguous(), z.contiguous(), 0.3, 5, 1, "columns", **place)
+    got = D.dropout_add(x, z, 0.3, 5, 1, "columns", **place)
+    assert got.is_contiguous() and torch.equal(got, want) and torch.equal(wide, before)
+    assert D.dropout_add(x, z, 0.3, 5, 1, "columns", out=z, **place) is z and torch.equal(z, want)
+    before[1:6, 7:18] = want
+    assert torch.equal(wide, before)                           # and nothing around it
+    with pytest.raises(ValueError, match="row stride"):
+        D.dropout_add(x, z, 0.3, out=torch.empty_like(want))
+    one = wide[3:4, 7:18]                                      # a single row has no stride
+    assert torch.equal(D.dropout_add(big[3:4, 4:15], one, 0.3, 5), D.dropout_add(big[3:4, 4:15].contiguous(), one.contiguous(), 0.3, 5))
