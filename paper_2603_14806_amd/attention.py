@@ -153,7 +153,7 @@ def _call(q, k, v, bias, mask, scale):
     _, nk, kv_heads, _ = k.shape
     keys = (batch, nk, kv_heads, d)
     args = _checked("q", q, dtype, device, shape), _checked("k", k, dtype, device, keys), _checked("v", v, dtype, device, keys)
-    w = CrossAttnView(batch, nq, nk, heads, kv_heads, d, _DTYPES[dtype], d ** -0.5 if scale is None else scale)
+    w = CrossAttnView(batch, nq, nk, heads, kv_heads, d, _DTYPES[dtype], max(d, 1) ** -0.5 if scale is None else scale)
     if bias is not None:
         if bias.dtype != dtype or bias.device != device:
             raise ValueError(f"bias must be a {dtype} tensor on {device}")
