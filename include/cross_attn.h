@@ -10,7 +10,8 @@
  *     out_bih = sum_j softmax_j(x_ij) v_bj,hk
  *
  * An absent key (mask 0) takes no part, whatever its k, v and bias hold (NaN
- * included); a bias of -inf removes a key from one query's sum in the same way.
+ * included).  A bias of -inf gives a key weight 0 for one query; its k and v are
+ * multiplied all the same, so their products with q and dout have to be finite.
  * A query with no key left gives 0, and 0 gradients.  A finite bias is a number
  * like any other, the type's lowest value among them: a row that holds it
  * everywhere is the softmax of what fp32 keeps of the sum.

@@ -176,10 +176,12 @@ def cross_attention(q, k, v, bias=None, mask=None, scale=None, return_stats=Fals
     multiple of kv_heads, d a multiple of 8 up to 128; any strides that are multiples of 16 bytes).
 
     bias: [batch or 1][heads or 1][nq][nk] (or without the first axis) of q's type whose rows are a multiple of 8
-    values apart (a view of a padded tensor is fine; rows are read up to a multiple of 8 values, a single query's too); an axis of length 1 is shared.  mask: [batch or 1][nk] or [nk],
-    uint8 or bool, nonzero where the key is present.  scale: default 1 / sqrt(d).  With return_stats also what
-    cross_attention_backward takes: a flat float32 tensor of the library's own layout (first the maxima and the sums,
-    [2][batch][heads][nq])."""
+    values apart (a view of a padded tensor is fine; rows are read up to a multiple of 8 values, a single query's
+    too); an axis of length 1 is shared.  -inf gives a key weight 0 for one query, but its k and v are multiplied all
+    the same: NaN or infinities there show.  mask: [batch or 1][nk] or [nk], uint8 or bool, nonzero where the key is
+    present (an absent key's k, v and bias may hold anything).  scale: default 1 / sqrt(d).  With return_stats also
+    what cross_attention_backward takes: a flat float32 tensor of the library's own layout (first the maxima and the
+    sums, [2][batch][heads][nq])."""
     w, tq, tk, tv = _call(q, k, v, bias, mask, scale)
     with on_stream(q.device, stream) as s:
         out = q.new_empty(q.shape)

@@ -22,3 +22,24 @@ def test_no_heads_refused():
     with pytest.raises(T.TriMulError) as e:
         A.cross_attention(q, k, k)
     assert e.value.code == T.TRI_MUL_EINVAL
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,nq", [(2, 9), (70, 140)])
+def test_bias_of_minus_infinity_is_weight_zero(B, nq, dtype):
+    """Keys that every query's bias removes, with values of 1e30 (finite, and so are their products with dout):
+    the bits of the same keys absent by the mask, gradients included."""
+    g = torch.Generator().manual_seed(2)
+    q, dout = (torch.randn((B, nq, 4, 32), generator=g).to(dtype).cuda() for _ in range(2))
+    k, v = (torch.randn((B, 80, 4, 32), generator=g).to(dtype).cuda() for _ in range(2))
+    mask = (torch.rand((B, 80), generator=g) < 0.6).to(torch.uint8).cuda()
+    gone = mask == 0
+    v[gone] = 1e30
+    bias = torch.randn((B, 4, nq, 80), generator=g).to(dtype).cuda()
+    low = torch.where(gone[:, None, None, :], torch.full_like(bias, -float("inf")), bias)
+    results = []
+    for b, m in ((low, None), (bias, mask)):
+        out, stats = A.cross_attention(q, k, v, b, m, return_stats=True)
+        results.append((out,) + A.cross_attention_backward(q, k, v, out, stats, dout, b, m))
+    for n, a, b in zip(("out", "dq", "dk", "dv", "dbias"), *results):
+        assert torch.equal(a, b), n
