@@ -23,7 +23,9 @@
  * may be dout itself, where types and strides agree.  Arithmetic in fp32, one
  * rounding.  Conventions as in tri_mul.h: device pointers, status codes
  * TRI_MUL_*, message in tri_mul_last_error(), asynchronous on `stream`, no
- * workspace, capturable.
+ * workspace, capturable.  seed and offset are values of the call: each replay
+ * of a captured one drops the same elements, so a training step that is captured
+ * is captured again for another mask.
  */
 #ifndef PAIR_DROPOUT_H
 #define PAIR_DROPOUT_H

@@ -1,6 +1,7 @@
 """Residual addition with dropout (include/pair_dropout.h): the C names, and dropout_add / dropout_backward, which
 check their tensors and allocate outputs with torch.  The mask is a function of seed, offset and the element's place;
-nothing of it is stored.  Streams and devices as in attention.py."""
+nothing of it is stored.  A captured call keeps its seed and offset: every replay drops the same elements.  Streams and
+devices as in attention.py."""
 import ctypes
 
 import torch

@@ -518,7 +518,8 @@ class TriMul:
     def residual(self, z, mask=None, direction="outgoing", p=0.25, seed=0, offset=0, share="rows", out=None,
                  stream=None):
         """z + dropout(update of z) in the storage dtype (include/pair_dropout.h; the pair stack shares the mask
-        along the rows); with p = 0 the plain residual addition.  z is contiguous; out may be z itself."""
+        along the rows); with p = 0 the plain residual addition.  z is contiguous; out may be z itself.  Captured into
+        a graph, it drops the same elements at every replay."""
         from . import dropout
         self._tokens(z, mask)
         with on_stream(z.device, stream):

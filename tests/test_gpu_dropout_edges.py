@@ -64,3 +64,20 @@ def test_residual_rows_of_a_larger_tensor(dtype):
         D.dropout_add(x, z, 0.3, out=torch.empty_like(want))
     one = wide[3:4, 7:18]                                      # a single row has no stride
     assert torch.equal(D.dropout_add(big[3:4, 4:15], one, 0.3, 5), D.dropout_add(big[3:4, 4:15].contiguous(), one.contiguous(), 0.3, 5))
+
+
+@pytest.mark.gpu
+@needs_gpu
+def test_replays_keep_the_captured_mask():
+    """Seed and offset are the captured call's own, as documented."""
+    x = torch.ones((30, 30, 128), device="cuda")
+    D.dropout_add(x, None, 0.5, 1, 2)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = D.dropout_add(x, None, 0.5, 1, 2)
+    for i in range(3):
+        graph.replay()
+        other = D.dropout_add(x, None, 0.5, 1, 3 + i)
+        torch.cuda.synchronize()
+        assert torch.equal(y, D.dropout_add(x, None, 0.5, 1, 2)) and not torch.equal(y, other)
