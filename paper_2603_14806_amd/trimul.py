@@ -407,7 +407,7 @@ class TriMul:
             out = torch.empty((N, N, 128), dtype=TORCH_DTYPE[DTYPE_CODE[self.out_dtype]], device=self.device)
         return out
 
-    def _tokens(self, z, mask=None, out=None):
+    def _tokens(self, z, mask=None, out=None, dout=None):
         """N of a call on the [N][N][128] tensor z, after checking what the kernels, which see addresses alone, take
         for granted: types, sizes, contiguous data, the layer's device."""
         N = z.shape[0] if z.dim() else 0
@@ -420,7 +420,7 @@ class TriMul:
                 raise ValueError(f"{name} must be a contiguous [N, N, 128] tensor, not {list(t.shape)} with strides {t.stride()}")
         if isinstance(mask, torch.Tensor) and (mask.element_size() != 1 or mask.numel() != N or not mask.is_contiguous()):
             raise ValueError(f"mask must hold {N} uint8 or bool values, not {list(mask.shape)} of {mask.dtype}")
-        for name, t in (("z", z), ("mask", mask), ("out", out)):
+        for name, t in (("z", z), ("mask", mask), ("out", out), ("dout", dout)):
             if isinstance(t, torch.Tensor) and t.device != self._on:
                 raise ValueError(f"{name} must live on the GPU of the layer, {self._on}, not on {t.device}")
         return N
@@ -504,7 +504,7 @@ class TriMul:
             raise ValueError("z must have the storage dtype and dout the output dtype of the layer")
         if not (z.is_contiguous() and dout.is_contiguous()):
             raise ValueError("z and dout must be contiguous")
-        self._tokens(z, mask)
+        self._tokens(z, mask, dout=dout)
         grads = {k: torch.empty(v, dtype=torch.float32, device=self.device) for k, v in WEIGHT_SHAPES.items()}
         dz = torch.empty_like(z)
         wsb = tri_mul_backward_workspace_size(self.h, N)
@@ -529,7 +529,7 @@ class TriMul:
                           stream=None, saved=None):
         """Gradients of sum(residual(z) * dout): (dz, grads), dout and dz in the storage dtype."""
         from . import dropout
-        self._tokens(z, mask)
+        self._tokens(z, mask, dout=dout)
         with on_stream(z.device, stream):
             du = dropout.dropout_backward(dout, p, seed, offset, share, dtype=self.out_dtype)
             dz, grads = self.backward(z, du, mask, direction, saved=saved)

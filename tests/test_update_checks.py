@@ -89,3 +89,13 @@ def test_workspaces_by_stream_and_capture(monkeypatch):
     assert len({a, b, *graphs}) == 5                   # (all are held here)
     assert call((1, False), 8) == a
     assert call((1, False), 9) not in (a, b, *graphs)
+
+
+def test_gradients_on_another_device_are_refused():
+    """The kernels run on the layer's GPU, on addresses of whichever device dout is on."""
+    t = layer()
+    t._on = torch.device("meta")
+    z, dout = Z.to("meta"), torch.zeros(N, N, 128)
+    for f in (t.backward, t.residual_backward):
+        with pytest.raises(ValueError, match="dout must live on the GPU of the layer"):
+            f(z, dout)
