@@ -451,42 +451,47 @@ class TriMul:
         N = z.shape[0]
         t = TORCH_DTYPE[DTYPE_CODE[self.dtype]]
         n = tri_mul_panel_size(self.h, N) // torch.empty((), dtype=t).element_size()
-        A = torch.empty(n, dtype=t, device=self.device)
-        B = torch.empty(n, dtype=t, device=self.device)
-        tri_mul_project(self.h, z, mask, N, TRI_MUL_OUTGOING if direction == "outgoing" else TRI_MUL_INCOMING,
-                        A, B, stream)
+        with on_stream(self._on, stream) as s:
+            A = torch.empty(n, dtype=t, device=self.device)
+            B = torch.empty(n, dtype=t, device=self.device)
+            tri_mul_project(self.h, z, mask, N, TRI_MUL_OUTGOING if direction == "outgoing" else TRI_MUL_INCOMING,
+                            A, B, s)
         return A, B
 
     def contract(self, A, B, N, stream=None):
         """A, B in the panel layout (project / dense_to_panel); returns C in
         the result layout (flat; see result_to_dense)."""
-        C = torch.empty(N * (-(-N // 32) * 32) * 128, dtype=torch.float32, device=self.device)
-        tri_mul_contract(self.h, A, B, N, C, stream)
+        with on_stream(self._on, stream) as s:
+            C = torch.empty(N * (-(-N // 32) * 32) * 128, dtype=torch.float32, device=self.device)
+            tri_mul_contract(self.h, A, B, N, C, s)
         return C
 
     def contract_transposed(self, AT, BT, N, stream=None):
         """The same C as contract(A, B, N) from the operands transposed,
         i.e. from project(z, mask, <the opposite direction>)."""
-        C = torch.empty(N * (-(-N // 32) * 32) * 128, dtype=torch.float32, device=self.device)
-        tri_mul_contract_transposed(self.h, AT, BT, N, C, stream)
+        with on_stream(self._on, stream) as s:
+            C = torch.empty(N * (-(-N // 32) * 32) * 128, dtype=torch.float32, device=self.device)
+            tri_mul_contract_transposed(self.h, AT, BT, N, C, s)
         return C
 
     def epilogue(self, C, z, mask=None, out=None, stream=None):
         """C in the result layout (contract / dense_to_result)."""
         N = z.shape[0]
-        out = self._out(N, out)
-        tri_mul_epilogue(self.h, C, z, mask, N, out, stream)
+        with on_stream(self._on, stream) as s:
+            out = self._out(N, out)
+            tri_mul_epilogue(self.h, C, z, mask, N, out, s)
         return out
 
     def contract_backward(self, dC, A, B, N, stream=None):
         """Gradients of the contraction: dC in the result layout, A, B in the
         panel layout; returns (dA, dB), both in the result layout (flat)."""
         n = N * (-(-N // 32) * 32) * 128
-        dA = torch.empty(n, dtype=torch.float32, device=self.device)
-        dB = torch.empty(n, dtype=torch.float32, device=self.device)
         wsb = tri_mul_contract_backward_workspace_size(self.h, N)
-        ws = torch.empty(wsb, dtype=torch.uint8, device=self.device)
-        tri_mul_contract_backward(self.h, dC, A, B, N, dA, dB, ws, wsb, stream)
+        with on_stream(self._on, stream) as s:
+            dA = torch.empty(n, dtype=torch.float32, device=self.device)
+            dB = torch.empty(n, dtype=torch.float32, device=self.device)
+            ws = torch.empty(wsb, dtype=torch.uint8, device=self.device)
+            tri_mul_contract_backward(self.h, dC, A, B, N, dA, dB, ws, wsb, s)
         return dA, dB
 
     def backward(self, z, dout, mask=None, direction="outgoing", stream=None, saved=None):
@@ -505,14 +510,15 @@ class TriMul:
         if not (z.is_contiguous() and dout.is_contiguous()):
             raise ValueError("z and dout must be contiguous")
         self._tokens(z, mask, dout=dout)
-        grads = {k: torch.empty(v, dtype=torch.float32, device=self.device) for k, v in WEIGHT_SHAPES.items()}
-        dz = torch.empty_like(z)
         wsb = tri_mul_backward_workspace_size(self.h, N)
-        ws = torch.empty(wsb, dtype=torch.uint8, device=self.device)
-        if saved is None:
-            tri_mul_layer_backward(self.h, direction, z, mask, N, dout, dz, grads, ws, wsb, stream)
-        else:
-            tri_mul_layer_backward_saved(self.h, direction, z, mask, N, *saved, dout, dz, grads, ws, wsb, stream)
+        with on_stream(self._on, stream) as s:
+            grads = {k: torch.empty(v, dtype=torch.float32, device=self.device) for k, v in WEIGHT_SHAPES.items()}
+            dz = torch.empty_like(z)
+            ws = torch.empty(wsb, dtype=torch.uint8, device=self.device)
+            if saved is None:
+                tri_mul_layer_backward(self.h, direction, z, mask, N, dout, dz, grads, ws, wsb, s)
+            else:
+                tri_mul_layer_backward_saved(self.h, direction, z, mask, N, *saved, dout, dz, grads, ws, wsb, s)
         return dz, grads
 
     def residual(self, z, mask=None, direction="outgoing", p=0.25, seed=0, offset=0, share="rows", out=None,
@@ -705,10 +711,11 @@ class OuterProductMean:
             raise ValueError("a and b must be [S][N][32] bf16 tensors of the same shape")
         if not (a.is_contiguous() and b.is_contiguous()):
             raise ValueError("a and b must be contiguous")
-        out = self._out(N, N)
         n = opm_forward_workspace_size(self.h, S, N)
-        ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-        opm_forward(self.h, a, b, mask, S, N, out, ws, n, stream)
+        with on_stream(self._w.device, stream) as s:
+            out = self._out(N, N)
+            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+            opm_forward(self.h, a, b, mask, S, N, out, ws, n, s)
         return out
 
     def accumulator(self, rows, cols):
@@ -716,8 +723,9 @@ class OuterProductMean:
 
     def block_accumulate(self, view, a, b, mask, acc, out_tile=None, stream=None):
         n = opm_workspace_size(self.h, view.rows, view.cols, view.slen)
-        ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-        opm_block_accumulate(self.h, view, a, b, mask, acc, out_tile, ws, n, stream)
+        with on_stream(self._w.device, stream) as s:
+            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+            opm_block_accumulate(self.h, view, a, b, mask, acc, out_tile, ws, n, s)
 
 
 # ---------------------------------------------------------------- triangle attention core (include/triattn.h)
