@@ -1,13 +1,14 @@
 // Residual addition with dropout, and its backward, for [rows][cols][channels]
 // tensors with a mask that is computed where it is needed.
 //
-// Bound by memory: x, res and out once.  One Philox call (ten rounds, 20
-// 32 x 32 -> 64 bit products at a quarter of the rate) serves four elements,
-// about 30 lane operations an element, a third of what the vector units do
-// while an element's 6 to 12 bytes pass; where a mask is shared a thread
-// computes its own once and walks the axis that shares it.
-// (2048 x 2048 x 128, fp32 + bf16 -> bf16, columns: 798 us, 5.4 TB/s; 500 x 700 x 128 bf16,
-// each element its own, backward: 33 us, 5.5 TB/s; 64 x 64 x 128 fp32: 3.5 us.)
+// One Philox call (ten rounds, 20 32 x 32 -> 64 bit products at a quarter of
+// the rate) serves four elements; where a mask is shared a thread computes its
+// own once and walks the axis that shares it.  Shared: bound by memory, x, res and out
+// once, vector instructions 16% of a busy compute unit's cycles (2048 x 2048 x 128,
+// fp32 + bf16 -> bf16, columns: 807 us, 5.3 TB/s).  Each element its own: the
+// generator's 20 operations an element keep the vector units busy for 91% of the cycles, and at
+// 4 bytes an element memory is as near its rate (500 x 700 x 128 bf16, backward: 32 us, 5.6 TB/s).
+// Small: a launch (64 x 64 x 128 fp32: 3.5 us).
 #include "common.h"
 #include "kernels.h"
 
@@ -83,16 +84,16 @@ __device__ __forceinline__ uint32_t kept(uint64_t e, const DropoutArgs& a) {
     if constexpr (V == 1) {
         const Words w = philox(e >> 2, a.offset, a.seed);
         const uint32_t i = (uint32_t)e & 3;
-        return (i == 0 ? w.w[0] : i == 1 ? w.w[1] : i == 2 ? w.w[2] : w.w[3]) >= a.threshold ? a.any & 1u : 0u;
+        return (i == 0 ? w.w[0] : i == 1 ? w.w[1] : i == 2 ? w.w[2] : w.w[3]) >= a.threshold && a.any ? 1u : 0u;
     } else {
-        uint32_t m = 0;
+        uint32_t m = 0;     // (a.any asked of m at the end instead: bits are built that nothing needs, 32.3 us for 30.0)
 #pragma unroll
         for (int i = 0; i < V / 4; ++i) {
             const Words w = philox((e >> 2) + i, a.offset, a.seed);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) m |= (w.w[j] >= a.threshold ? 1u : 0u) << (4 * i + j);
+            for (int j = 0; j < 4; ++j) m |= (w.w[j] >= a.threshold && a.any ? 1u : 0u) << (4 * i + j);
         }
-        return m & a.any;
+        return m;
     }
 }
 
