@@ -8,13 +8,16 @@
 // registers' and its partner's (lane ^ 32), its bias is contiguous, and the
 // weights feed O^T += V^T P^T from the registers they are in.
 //
-// Bound by instruction issue, products and softmax in turn (they hardly
-// overlap on a SIMD).  By the counters, of a busy compute unit's cycles: at d =
-// 128 without a bias 34% products and 47% vector instructions (2 entries x 16
-// heads, 4096 queries x 6000 keys, bf16: 438 us, 920 TFLOP/s; 540 and more where the
-// clock is lower), at d = 32 with a bias 11% and 66% (384 x 4 heads of 384 x 384:
-// 98 us, 2.3e12 scores/s; 16 heads of 24, 1300 x 1300: 25 us).  Few queries over many keys are bound by
-// memory (8 x 16000 keys of 4 heads of 64, one query: 23 us, 5.7 TB/s).
+// What bounds it, by the counters, as shares of a busy compute unit's cycles in
+// products and in vector instructions (which hardly overlap on a SIMD).  Large
+// calls by the issue of both in turn: at d = 128 without a bias 44% and 51% (2 entries
+// x 16 heads, 4096 queries x 6000 keys, bf16: 438 to 560 us by the clock that a
+// card holds, 920 to 720 TFLOP/s), at d = 32 with a bias 11% and 67% (384 x 4
+// heads of 384 x 384: 98 us, 2.3e12 scores/s).  The 32-column form by waiting:
+// 16 heads of 24, 1300 x 1300, 5% and 39%, its two or three waves a SIMD
+// without anything to issue for half of their time (26 us); fp32, 500 x 777,
+// 29% and 17% with one wave a SIMD on half the compute units (16 us).  Few queries
+// over many keys by memory (8 x 16000 keys of 4 heads of 64, one query: 23 us, 5.7 TB/s).
 #include "crossattn.h"
 
 namespace trimul {
@@ -184,7 +187,7 @@ __global__ __launch_bounds__(256, (forward_waves<T, DP, WK>())) void k_cross_for
             for (int n = 0; n < NB; ++n)
 #pragma unroll
                 for (int tt = 0; tt < 2; ++tt) {
-                    Frag<T> pf;
+                    Frag<T> pf;      // (bf16: an error of the size of out's own rounding; a second, low part would be half as many products again)
                     take8(s[n], tt, pf);
 #pragma unroll
                     for (int i = 0; i < ND; ++i) {

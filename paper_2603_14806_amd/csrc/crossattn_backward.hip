@@ -63,9 +63,11 @@ __device__ __forceinline__ void take_from(f32x16_t& s, float scale, float M) {
 // SOLO (WK = 4), a key head of 32 columns at most for each wave.
 // A bias that no other entry or head shares gets its gradient, dS, from here (DIRECT; asked
 // at each product instead, the branches there cut the others' code into pieces).
-// Bound by instruction issue: three products a score and channel, and the
-// exponential (384 entries x 4 heads of 384 x 384, d = 32, bias: 122 us; 2 entries x 16 heads, 2048 x 3000,
-// d = 128: 158 us, 480 TFLOP/s).
+// Three products a score and channel, and the exponential.  At d = 32 with few keys not bound by their issue
+// (products 14%, vector instructions 51% of a busy compute unit's cycles) but by the rows that each work-group
+// waits for at its start and its bias loads (384 entries x 4 heads of 384 x 384, bias: 118 us; without the
+// exponentials it took 120 of 121 us, without any loads 96).  At d = 128 products and vector instructions are
+// 41% and 37% (2 entries x 16 heads, 2048 x 3000: 158 us, 480 TFLOP/s).
 template <typename T, int DP, int WK>
 constexpr int q_waves() {
     if (WK > 1) return sizeof(T) == 2 ? (DP == 32 ? 3 : DP == 64 ? 2 : 1) : (DP == 32 ? 2 : 1);
@@ -209,7 +211,7 @@ __device__ __forceinline__ void query_pass(const CrossArgs& a, int ctiles, uint3
                     s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], cf, sh)) * (FOLD ? dp[r] : dp[r] - D);
 #pragma unroll
                 for (int tt = 0; tt < 2; ++tt) {
-                    Frag<T> pf;
+                    Frag<T> pf;                                // (bf16: dS is rounded for its product as dq is for its store)
                     take8(s, tt, pf);
                     if (DIRECT) {
                         const int k = c * KC + (KC / 2) * hi + 16 * n + 8 * tt;
@@ -264,8 +266,9 @@ __global__ __launch_bounds__(256, (q_waves<T, DP, WK>())) void k_cross_backward_
 // The bias tile of a chunk passes through LDS too and is read transposed
 // (four queries of one key at a time).
 // Bound by instruction issue: four products a score and channel (TWO: five)
-// and their LDS reads (384 entries x 4 heads of 384 x 384, d = 32, bias: 138 us; 2 entries x 16 heads on 4,
-// 2048 x 3000, d = 128: 303 us and 18 for the sums of four splits).
+// and their LDS reads (products 20%, vector instructions 55%, LDS 13% of a busy compute unit's cycles: 384 entries
+// x 4 heads of 384 x 384, d = 32, bias: 139 us).  TWO: 38%, 34% and 11%, its two waves a SIMD waiting for each
+// other's chunk the rest (2 entries x 16 heads on 4, 2048 x 3000, d = 128: 303 to 316 us and 18 for the sums of four splits).
 template <typename T, int DP, int WK, bool TWO>
 constexpr int kv_waves() { return TWO ? 2 : DP == 32 ? (sizeof(T) == 2 ? 3 : 2) : DP == 64 && sizeof(T) == 2 ? 2 : 1; }
 
@@ -486,7 +489,7 @@ __device__ __forceinline__ void key_pass(const CrossArgs& a, int ktiles, uint32_
         for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {
-                Frag<T> pf, df;
+                Frag<T> pf, df;                                // (bf16: P and dS rounded for their products as dv and dk for their stores)
                 take8(s[n], tt, pf);
                 if (!TWO) take8(dp[n], tt, df);
 #pragma unroll
@@ -595,8 +598,9 @@ __global__ __launch_bounds__(256) void k_cross_kv_sum(const CrossArgs a, int kv_
 //
 // A bias that several entries or heads share.  One work-group: 128 queries x KC keys of it (the query
 // pass's layout), its loop over the entries and heads that share it (a split of them: the sums of the splits are added by
-// k_cross_dbias_sum).  Bound by issue and the latency of its 64 keys' steps, two waves a SIMD (384 entries x
-// 4 heads of 384 x 384, d = 32: 100 us; three waves spill and take 340).
+// k_cross_dbias_sum).  Bound by issue (products 12%, vector instructions 46%, LDS 10% of a busy compute unit's
+// cycles) and the latency of its 64 keys' steps, two waves a SIMD (384 entries x 4 heads of 384 x 384, d = 32:
+// 95 us; three waves spill and take 340).
 constexpr int dbias_waves(int dtype, int d) { return d <= 32 || (d <= 64 && dtype == 1) ? 2 : 1; }
 
 template <typename T, int DP, int KC>

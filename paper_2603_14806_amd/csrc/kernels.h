@@ -230,7 +230,9 @@ inline bool cross_few(int64_t heads, int64_t n) { return heads * ((n + 127) / 12
 // Whether the key heads have so few columns, and are so many (four waves for each
 // compute unit), that a wave takes one alone.  (1500 windows of 32 queries and 128
 // keys, 4 heads: forward 25.6 us, dq 24.9; as 128-column tiles with three waves
-// idle 30.4 and 39.9.  256 x 8 single queries over 2000 keys, d = 128: 359 and 374 us.)
+// idle 30.4 and 39.9.  256 x 8 single queries over 2000 keys, d = 128: 359 and 374 us.  At the edge, 1024 key
+// heads, one wave a SIMD: single queries over 256 keys of d = 64 13.6 and 17.5, over 8000 354 and 438; 32 queries and
+// 128 keys of d = 32 6.2 and 7.0; but 32 queries and 2000 keys of d = 32 54.7 and 45.0.)
 inline bool cross_solo(int64_t heads, int64_t cols) { return cols <= 32 && heads >= 1024; }
 CrossPlan cross_plan(int64_t batch, int kv_heads, int64_t cols, int64_t nk);
 size_t cross_part_floats(const CrossPlan& p, int64_t batch, int64_t nq, int heads, int d);
