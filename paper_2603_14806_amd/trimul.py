@@ -399,7 +399,7 @@ class TriMul:
         ws = self._ws.get(place)
         if ws is None or ws.numel() < need:
             self._ws.pop(place, None)
-            ws = self._ws[place] = torch.empty(need, dtype=torch.uint8, device=self.device)
+            ws = self._ws[place] = torch.empty(need, dtype=torch.uint8, device=self._on)
         return ws, need
 
     def _out(self, N, out):
