@@ -17,3 +17,4 @@ from .opm import (msa_mask, pair_counts, outer_sum, outer_product_mean,  # noqa:
 from .triattn import key_mask, scores, triangle_attention, chunked_attention  # noqa: F401
 from .crossattn import cross_attention, cross_attention_backward, softmax_weights  # noqa: F401
 from .dropout import dropout_add, dropout_backward, keep, philox  # noqa: F401
+from .checkpoint8 import checkpoint8, checkpoint8_values  # noqa: F401

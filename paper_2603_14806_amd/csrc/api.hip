@@ -16,6 +16,7 @@
 #include "triattn.h"
 #include "cross_attn.h"
 #include "pair_dropout.h"
+#include "checkpoint8.h"
 #include "tri_mul_check.h"
 #include "common.h"
 #include "kernels.h"
@@ -1555,6 +1556,57 @@ int tri_mul_check_contract_result(int64_t M, int64_t N, int batch, uint64_t c_by
     trimul::K2CheckCounts n;
     trimul::k2_check_c(M, N, batch, c_bytes, all_channels, n);
     *out = tri_mul_load_check_t{n.tiles, n.loads, n.elems, n.bad_tiles, n.bad_desc, n.bad_elem};
+    return ok();
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- activations in 8 bits
+
+namespace {
+
+constexpr int64_t kMaxAxis = int64_t(1) << 40;
+
+// *a and whether there is nothing to do.
+int checkpoint_check(const checkpoint8_view_t* v, trimul::CheckpointArgs* a, bool* empty) {
+    if (!v) return fail(TRI_MUL_EINVAL, "null view");
+    if (v->dtype != TRI_MUL_F32 && v->dtype != TRI_MUL_BF16) return fail(TRI_MUL_EINVAL, "bad dtype %d", v->dtype);
+    if (v->group < 8 || v->group > 256 || v->group % 8) return fail(TRI_MUL_EINVAL, "group = %d is not a multiple of 8 in [8, 256]", v->group);
+    if (v->rows < 0 || v->n < 0) return fail(TRI_MUL_EINVAL, "negative size");
+    if (v->rows > 1 && v->ld < v->n) return fail(TRI_MUL_EINVAL, "row stride %lld below n = %lld", (long long)v->ld, (long long)v->n);
+    if (v->rows >= kMaxAxis || v->n >= kMaxAxis || (v->rows > 1 && v->ld >= kMaxAxis) || (__int128)v->rows * std::max(v->n, v->ld) >= (__int128)1 << 62)
+        return fail(TRI_MUL_EUNSUPPORTED, "2^40 rows, values a row or row stride, or 2^62 values");
+    *empty = v->rows == 0 || v->n == 0;
+    *a = trimul::CheckpointArgs{v->rows, v->n, v->ld, v->group};
+    if (!*empty && trimul::checkpoint8_work_groups(*a) > kMaxGroups) return fail(TRI_MUL_EUNSUPPORTED, "too many groups for one call");
+    return TRI_MUL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int checkpoint8_pack(const checkpoint8_view_t* v, const void* x, int8_t* codes, uint8_t* powers, void* stream) {
+    trimul::CheckpointArgs a;
+    bool empty;
+    if (int rc = checkpoint_check(v, &a, &empty)) return rc;
+    if (empty) return ok();
+    if (!x || !codes || !powers) return fail(TRI_MUL_EINVAL, "null x, codes or powers");
+    if (!aligned_to(x, v->dtype)) return fail(TRI_MUL_EINVAL, "x must be aligned to its type");
+    const hipError_t e = trimul::launch_checkpoint8(v->dtype, true, a, x, powers, codes, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "checkpoint kernel launch");
+    return ok();
+}
+
+int checkpoint8_unpack(const checkpoint8_view_t* v, const int8_t* codes, const uint8_t* powers, void* out, void* stream) {
+    trimul::CheckpointArgs a;
+    bool empty;
+    if (int rc = checkpoint_check(v, &a, &empty)) return rc;
+    if (empty) return ok();
+    if (!out || !codes || !powers) return fail(TRI_MUL_EINVAL, "null out, codes or powers");
+    if (!aligned_to(out, v->dtype)) return fail(TRI_MUL_EINVAL, "out must be aligned to its type");
+    const hipError_t e = trimul::launch_checkpoint8(v->dtype, false, a, codes, powers, out, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "checkpoint kernel launch");
     return ok();
 }
 

@@ -11,6 +11,7 @@
 // Small: a launch (64 x 64 x 128 fp32: 3.5 us).
 #include "common.h"
 #include "kernels.h"
+#include "vec.h"
 
 namespace trimul {
 namespace {
@@ -33,50 +34,6 @@ __device__ __forceinline__ Words philox(uint64_t e4, uint64_t offset, uint64_t s
     }
     return Words{{a, b, c, d}};
 }
-
-// V consecutive values as floats, and back.
-template <typename T, int V> struct Vec {
-    float f[V];
-    __device__ __forceinline__ void load(const T* p) {
-        if constexpr (V == 1) {
-            f[0] = Store<T>::ld(p);
-        } else if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int i = 0; i < V / 4; ++i) {
-                const float4 x = reinterpret_cast<const float4*>(p)[i];
-                f[4 * i] = x.x; f[4 * i + 1] = x.y; f[4 * i + 2] = x.z; f[4 * i + 3] = x.w;
-            }
-        } else {
-            uint32_t w[V / 2];
-            if constexpr (V == 8) {
-                const uint4 x = *reinterpret_cast<const uint4*>(p);
-                w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-            } else {
-                const uint2 x = *reinterpret_cast<const uint2*>(p);
-                w[0] = x.x; w[1] = x.y;
-            }
-#pragma unroll
-            for (int i = 0; i < V / 2; ++i) {
-                f[2 * i] = __uint_as_float(w[i] << 16);
-                f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-            }
-        }
-    }
-    __device__ __forceinline__ void store(T* p) const {
-        if constexpr (V == 1) {
-            Store<T>::st(p, f[0]);
-        } else if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int i = 0; i < V / 4; ++i)
-                reinterpret_cast<float4*>(p)[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
-        } else if constexpr (V == 8) {
-            *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]),
-                                                      pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
-        } else {
-            *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
-        }
-    }
-};
 
 // Bit i: element e + i is kept (e a multiple of 4 for V > 1).
 template <int V>

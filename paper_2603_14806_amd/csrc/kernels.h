@@ -270,4 +270,14 @@ struct DropoutArgs {
 hipError_t launch_pair_dropout(int in_dtype, int out_dtype, int share, const DropoutArgs& a, const void* x,
                                const void* res, void* out, hipStream_t s);
 
+// Activations in 8 bits (checkpoint8.hip): x to codes and powers (pack), or codes and powers to x.
+struct CheckpointArgs {
+    int64_t rows, n, ld;      // ld: elements from one row of x to the next
+    int group;
+    int wide;                 // filled in by the launcher, as are the next: every group allows vectors of eight
+    int64_t groups, slots;    // groups of a row, and of all
+};
+int64_t checkpoint8_work_groups(CheckpointArgs a);
+hipError_t launch_checkpoint8(int dtype, bool pack, CheckpointArgs a, const void* from, const uint8_t* powers, void* to, hipStream_t s);
+
 }  // namespace trimul

@@ -1,0 +1,73 @@
+// Loads and stores of several consecutive values of a tensor as floats (gfx950).
+#pragma once
+
+#include "common.h"
+
+namespace trimul {
+
+// V consecutive values as floats, and back.
+template <typename T, int V> struct Vec {
+    float f[V];
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (V == 1) {
+            f[0] = Store<T>::ld(p);
+        } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < V / 4; ++i) {
+                const float4 x = reinterpret_cast<const float4*>(p)[i];
+                f[4 * i] = x.x; f[4 * i + 1] = x.y; f[4 * i + 2] = x.z; f[4 * i + 3] = x.w;
+            }
+        } else {
+            uint32_t w[V / 2];
+            if constexpr (V == 8) {
+                const uint4 x = *reinterpret_cast<const uint4*>(p);
+                w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2*>(p);
+                w[0] = x.x; w[1] = x.y;
+            }
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                f[2 * i] = __uint_as_float(w[i] << 16);
+                f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(T* p) const {
+        if constexpr (V == 1) {
+            Store<T>::st(p, f[0]);
+        } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < V / 4; ++i)
+                reinterpret_cast<float4*>(p)[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+        } else if constexpr (V == 8) {
+            *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]),
+                                                      pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+        } else {
+            *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
+        }
+    }
+};
+
+// Eight values of which the first n exist (the rest: 0, not read and not written); wide: p is 16-byte aligned.
+template <typename T>
+__device__ __forceinline__ void load_some(Vec<T, 8>& v, const T* p, int n, bool wide) {
+    if (wide && n >= 8) {
+        v.load(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v.f[i] = i < n ? Store<T>::ld(p + i) : 0.f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_some(const Vec<T, 8>& v, T* p, int n, bool wide) {
+    if (wide && n >= 8) {
+        v.store(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) Store<T>::st(p + i, v.f[i]);
+    }
+}
+
+}  // namespace trimul

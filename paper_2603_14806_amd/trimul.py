@@ -425,6 +425,12 @@ class TriMul:
                 raise ValueError(f"{name} must live on the GPU of the layer, {self._on}, not on {t.device}")
         return N
 
+    def _unpacked(self, z, stream):
+        """The tensor of a Checkpoint8, in the storage dtype."""
+        if z.device != self._on:
+            raise ValueError(f"z must live on the GPU of the layer, {self._on}, not on {z.device}")
+        return z.unpack(self.dtype, stream=stream)
+
     def _update(self, entry, z, mask, out, stream):
         N = self._tokens(z, mask, out)
         with on_stream(self._on, stream) as s:
@@ -500,7 +506,11 @@ class TriMul:
         saved = (AT, BT, C) skips the recomputation of the forward: AT, BT
         from project(z, mask, <the opposite direction>) -- the direction's
         operands transposed, as the full calls leave them in their workspace
-        -- and C the direction's contraction (contract_transposed(AT, BT))."""
+        -- and C the direction's contraction (contract_transposed(AT, BT)).
+        z may be a Checkpoint8 (checkpoint8.py): the gradients are those at
+        the values it stands for, dz of the storage dtype."""
+        if not isinstance(z, torch.Tensor):
+            z = self._unpacked(z, stream)
         N = z.shape[0]
         cz = 128
         if tuple(z.shape) != (N, N, cz) or tuple(dout.shape) != (N, N, cz):
@@ -533,8 +543,11 @@ class TriMul:
 
     def residual_backward(self, z, dout, mask=None, direction="outgoing", p=0.25, seed=0, offset=0, share="rows",
                           stream=None, saved=None):
-        """Gradients of sum(residual(z) * dout): (dz, grads), dout and dz in the storage dtype."""
+        """Gradients of sum(residual(z) * dout): (dz, grads), dout and dz in the storage dtype.  z may be a
+        Checkpoint8, as in backward."""
         from . import dropout
+        if not isinstance(z, torch.Tensor):
+            z = self._unpacked(z, stream)
         self._tokens(z, mask, dout=dout)
         with on_stream(z.device, stream):
             du = dropout.dropout_backward(dout, p, seed, offset, share, dtype=self.out_dtype)

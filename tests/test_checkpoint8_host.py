@@ -1,0 +1,95 @@
+"""The oracle's pins of activations in 8 bits, and the host side of include/checkpoint8.h (no GPU)."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2603_14806_amd import checkpoint8 as C
+from paper_2603_14806_amd import trimul as T
+
+HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "checkpoint8.h")
+
+
+def test_worked_values():
+    """m = 1.99: 127.36 rounds to 127; m = 1.9921875: the tie 127.5 rounds to 128, one power more; zeros; not finite."""
+    x = np.array([[1.99, -1.0, 0.5 / 64, 1.5 / 64], [1.9921875, -1.0, 0.5, 3 / 64], [0, 0, 0, -0.0], [1, np.inf, 2, 3], [1, np.nan, 2, 3]])
+    codes, powers = oracle.checkpoint8(x, 8)
+    assert powers[:, 0].tolist() == [127 - 6, 127 - 5, 0, 255, 255]
+    assert codes.tolist() == [[127, -64, 0, 2], [64, -32, 16, 2], [0] * 4, [0] * 4, [0] * 4]
+    v = oracle.checkpoint8_values(codes, powers, 8)
+    assert v[0].tolist() == [127 / 64, -1, 0, 2 / 64] and np.isnan(v[3:]).all() and (v[2] == 0).all()
+
+
+def test_error_and_idempotence():
+    rng = np.random.default_rng(1)
+    x = rng.standard_normal((50, 100)) * np.exp(rng.standard_normal(100))
+    for group in (8, 24, 32, 128):
+        codes, powers = oracle.checkpoint8(x, group)
+        v = oracle.checkpoint8_values(codes, powers, group)
+        top = np.repeat(np.maximum.reduceat(np.abs(x), range(0, 100, group), axis=1), group, axis=1)[:, :100]
+        assert (np.abs(v - x) <= top / 127).all() and np.abs(codes.astype(int)).max() <= 127
+        again = oracle.checkpoint8(v, group)
+        assert np.array_equal(oracle.checkpoint8_values(*again, group), v)
+        wide = torch.from_numpy(v).to(torch.bfloat16).double().numpy()
+        assert np.array_equal(wide, v)                                                        # exact in bf16
+    tiny = np.full((1, 8), 2.0 ** -140)
+    assert oracle.checkpoint8(tiny, 8)[1][0, 0] == 0
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(T.LIB_PATH):
+        from paper_2603_14806_amd import build
+        build.build()
+    return C.lib()
+
+
+def test_declared_exported_and_bound(lib):
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"\b(checkpoint8_[a-z]+)\s*\(", text))
+    assert names == set(C.SIGNATURES) and all(hasattr(lib, n) for n in names)
+    assert ctypes.sizeof(C.Checkpoint8View) == 3 * 8 + 2 * 4
+
+
+EINVAL, EUNSUPPORTED = T.TRI_MUL_EINVAL, T.TRI_MUL_EUNSUPPORTED
+
+
+def view(**kw):
+    v = C.Checkpoint8View(4, 96, 96, T.TRI_MUL_BF16, 32)
+    for k, x in kw.items():
+        setattr(v, k, x)
+    return ctypes.byref(v)
+
+
+@pytest.mark.parametrize("change,code,word", [
+    (dict(dtype=2), EINVAL, "dtype"), (dict(group=0), EINVAL, "group"), (dict(group=12), EINVAL, "group"), (dict(group=264), EINVAL, "group"),
+    (dict(group=-8), EINVAL, "group"), (dict(rows=-1), EINVAL, "negative"), (dict(n=-1), EINVAL, "negative"), (dict(ld=95), EINVAL, "stride"),
+    (dict(ld=-96), EINVAL, "stride"), (dict(rows=1 << 40), EUNSUPPORTED, "2^40"), (dict(n=1 << 40, ld=1 << 40), EUNSUPPORTED, "2^40"),
+    (dict(ld=1 << 40), EUNSUPPORTED, "2^40"), (dict(rows=1 << 39, ld=1 << 39), EUNSUPPORTED, "2^62"),
+    (dict(rows=1 << 36), EUNSUPPORTED, "too many")])
+def test_views_refused(lib, change, code, word):
+    assert lib.checkpoint8_pack(view(**change), 16, 16, 16, None) == code and word in T.last_error()
+    assert lib.checkpoint8_unpack(view(**change), 16, 16, 16, None) == code and word in T.last_error()
+
+
+def test_pointers_refused_and_empty_calls(lib):
+    assert lib.checkpoint8_pack(None, 16, 16, 16, None) == EINVAL
+    for bad in ((None, 16, 16), (16, None, 16), (16, 16, None), (17, 16, 16)):
+        assert lib.checkpoint8_pack(view(), *bad, None) == EINVAL
+    for bad in ((None, 16, 16), (16, None, 16), (16, 16, None), (16, 16, 17)):
+        assert lib.checkpoint8_unpack(view(), *bad, None) == EINVAL
+    for empty in (dict(rows=0), dict(n=0)):
+        assert lib.checkpoint8_pack(view(**empty), None, None, None, None) == T.TRI_MUL_OK
+        assert lib.checkpoint8_unpack(view(**empty), None, None, None, None) == T.TRI_MUL_OK
+
+
+def test_python_refusals():
+    x = torch.zeros(2, 3, 8)
+    with pytest.raises(ValueError, match="GPU"):
+        C.pack(x)
+    with pytest.raises(ValueError, match="float32 or bfloat16"):
+        C.pack(x.half())
