@@ -18,3 +18,4 @@ from .triattn import key_mask, scores, triangle_attention, chunked_attention  # 
 from .crossattn import cross_attention, cross_attention_backward, softmax_weights  # noqa: F401
 from .dropout import dropout_add, dropout_backward, keep, philox  # noqa: F401
 from .checkpoint8 import checkpoint8, checkpoint8_values  # noqa: F401
+from . import relative  # noqa: F401

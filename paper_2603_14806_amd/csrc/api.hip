@@ -17,6 +17,7 @@
 #include "cross_attn.h"
 #include "pair_dropout.h"
 #include "checkpoint8.h"
+#include "relative_bias.h"
 #include "tri_mul_check.h"
 #include "common.h"
 #include "kernels.h"
@@ -1607,6 +1608,168 @@ int checkpoint8_unpack(const checkpoint8_view_t* v, const int8_t* codes, const u
     if (!aligned_to(out, v->dtype)) return fail(TRI_MUL_EINVAL, "out must be aligned to its type");
     const hipError_t e = trimul::launch_checkpoint8(v->dtype, false, a, codes, powers, out, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "checkpoint kernel launch");
+    return ok();
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- relative position bias
+
+namespace {
+
+int relative_check(const relative_view_t* v, bool pair) {
+    if (!v) return fail(TRI_MUL_EINVAL, "null view");
+    for (int t : {v->dtype, v->table_dtype})
+        if (t != TRI_MUL_F32 && t != TRI_MUL_BF16) return fail(TRI_MUL_EINVAL, "bad dtype %d", t);
+    if (v->batch < 0 || v->nq < 0 || v->nk < 0) return fail(TRI_MUL_EINVAL, "negative size");
+    if (pair && v->batch != 1) return fail(TRI_MUL_EINVAL, "batch = %lld of a pair tensor is not 1", (long long)v->batch);
+    if (v->heads < 1 || v->heads > 1024) return fail(TRI_MUL_EINVAL, "%s = %d outside [1, 1024]", pair ? "channels" : "heads", v->heads);
+    if (v->buckets < 1 || v->buckets > 256) return fail(TRI_MUL_EINVAL, "buckets = %d outside [1, 256]", v->buckets);
+    if (v->reach < 0 || v->reach > 4095) return fail(TRI_MUL_EINVAL, "reach = %d outside [0, 4095]", v->reach);
+    const int64_t most = int64_t(1) << 24;
+    if (v->batch >= most || v->nq >= most || v->nk >= most) return fail(TRI_MUL_EUNSUPPORTED, "batch, nq or nk of 2^24 or more");
+    if (!v->lut) return fail(TRI_MUL_EINVAL, "null lut");
+    if (!v->seg_q != !v->seg_k) return fail(TRI_MUL_EINVAL, "segments of the queries and the keys are both given or both NULL");
+    if ((v->nq && !v->pos_q) || (v->nk && !v->pos_k)) return fail(TRI_MUL_EINVAL, "null positions");
+    for (const int32_t* p : {v->pos_q, v->pos_k, v->seg_q, v->seg_k})
+        if (reinterpret_cast<uintptr_t>(p) % 4) return fail(TRI_MUL_EINVAL, "positions and segments must be 4-byte aligned");
+    for (int64_t x : {v->pos_q_batch, v->pos_k_batch, v->seg_q_batch, v->seg_k_batch})
+        if (v->batch > 1 && (x < 0 || x >= kMaxAxis)) return fail(TRI_MUL_EINVAL, "a batch stride of positions or segments that is negative or above 2^40");
+    return TRI_MUL_OK;
+}
+
+bool relative_empty(const relative_view_t* v) { return v->batch == 0 || v->nq == 0 || v->nk == 0; }
+
+trimul::RelativeArgs relative_args(const relative_view_t* v) {
+    trimul::RelativeArgs a{};
+    a.batch = v->batch;
+    a.nq = v->nq;
+    a.nk = v->nk;
+    a.heads = v->heads;
+    a.buckets = v->buckets;
+    a.reach = v->reach;
+    a.table_bf16 = v->table_dtype == TRI_MUL_BF16;
+    a.lut = v->lut;
+    a.pos_q = v->pos_q;
+    a.pos_k = v->pos_k;
+    a.seg_q = v->seg_q;
+    a.seg_k = v->seg_k;
+    if (v->batch > 1) {
+        a.pos_q_batch = v->pos_q_batch;
+        a.pos_k_batch = v->pos_k_batch;
+        a.seg_q_batch = v->seg_q_batch;
+        a.seg_k_batch = v->seg_k_batch;
+    }
+    return a;
+}
+
+// A [batch][heads][nq][nk] tensor (pair: [nq][nk][heads], heads 1 here and nk * heads values a row) into *to.
+int relative_tensor(const relative_view_t* v, const cross_attn_bias_t* t, const char* name, bool written, trimul::CrossBias* to) {
+    if (!t || !t->data) return fail(TRI_MUL_EINVAL, "null %s", name);
+    if (!aligned_to(t->data, v->dtype)) return fail(TRI_MUL_EINVAL, "%s must be aligned to its type", name);
+    const struct { int64_t length, stride, least; } axes[] = {{v->batch, t->batch, 1}, {v->heads, t->head, 1}, {v->nq, t->row, v->nk}};
+    for (const auto& x : axes) {
+        if (x.length < 2) continue;
+        if (x.stride < 0 || (written && x.stride < x.least)) return fail(TRI_MUL_EINVAL, "a stride %lld of %s along an axis of %lld", (long long)x.stride, name, (long long)x.length);
+        if (x.stride >= kMaxAxis) return fail(TRI_MUL_EUNSUPPORTED, "a stride of %s of 2^40 or more", name);
+    }
+    *to = trimul::CrossBias{t->data, v->batch > 1 ? t->batch : 0, v->heads > 1 ? t->head : 0, v->nq > 1 ? t->row : 0};
+    return TRI_MUL_OK;
+}
+
+int relative_rows(const relative_view_t* v, const void* data, int64_t ld, const char* name, trimul::CrossBias* to) {
+    if (!data) return fail(TRI_MUL_EINVAL, "null %s", name);
+    if (!aligned_to(data, v->dtype)) return fail(TRI_MUL_EINVAL, "%s must be aligned to its type", name);
+    if (v->nq > 1 && ld < v->nk * v->heads) return fail(TRI_MUL_EINVAL, "row stride %lld of %s below %lld", (long long)ld, name, (long long)(v->nk * v->heads));
+    if (v->nq > 1 && ld >= kMaxAxis) return fail(TRI_MUL_EUNSUPPORTED, "row stride of %s of 2^40 or more", name);
+    *to = trimul::CrossBias{const_cast<void*>(data), 0, 0, v->nq > 1 ? ld : 0};
+    return TRI_MUL_OK;
+}
+
+int relative_gradient(const relative_view_t* v, float* dtable, int64_t groups, size_t floats, void* ws, size_t ws_bytes, trimul::RelativeArgs* a) {
+    if (!dtable) return fail(TRI_MUL_EINVAL, "null dtable");
+    if (!aligned_to(dtable, TRI_MUL_F32)) return fail(TRI_MUL_EINVAL, "dtable must be aligned to its type");
+    if (groups > kMaxGroups) return fail(TRI_MUL_EUNSUPPORTED, "too many entries and heads for one call");
+    if (int rc = cross_workspace(ws, ws_bytes, 4 * floats)) return rc;
+    a->dtable = dtable;
+    a->part = static_cast<float*>(ws);
+    return TRI_MUL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int relative_bias(const relative_view_t* v, const void* table, const cross_attn_bias_t* base,
+                  const cross_attn_bias_t* out, void* stream) {
+    if (int rc = relative_check(v, false)) return rc;
+    if (relative_empty(v)) return ok();
+    if (!table || !aligned_to(table, v->table_dtype)) return fail(TRI_MUL_EINVAL, "null or misaligned table");
+    trimul::RelativeArgs a = relative_args(v);
+    a.table = table;
+    if (base)
+        if (int rc = relative_tensor(v, base, "base", false, &a.base)) return rc;
+    if (int rc = relative_tensor(v, out, "out", true, &a.out)) return rc;
+    if (trimul::relative_bias_plan(a) > kMaxGroups) return fail(TRI_MUL_EUNSUPPORTED, "too many entries, heads, queries and keys for one call");
+    const hipError_t e = trimul::launch_relative_bias(v->dtype, a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "relative bias kernel launch");
+    return ok();
+}
+
+int relative_bias_backward_workspace_size(const relative_view_t* v, size_t* bytes) {
+    if (int rc = relative_check(v, false)) return rc;
+    if (!bytes) return fail(TRI_MUL_EINVAL, "null bytes pointer");
+    *bytes = relative_empty(v) ? 0 : 4 * trimul::relative_bias_part_floats(relative_args(v));
+    return ok();
+}
+
+int relative_bias_backward(const relative_view_t* v, const cross_attn_bias_t* dout, float* dtable, void* ws,
+                           size_t ws_bytes, void* stream) {
+    if (int rc = relative_check(v, false)) return rc;
+    trimul::RelativeArgs a = relative_args(v);
+    const bool empty = relative_empty(v);
+    if (!empty)
+        if (int rc = relative_tensor(v, dout, "dout", false, &a.out)) return rc;
+    trimul::RelativeArgs plan = a;
+    if (int rc = relative_gradient(v, dtable, empty ? 0 : trimul::relative_bias_backward_plan(plan), empty ? 0 : trimul::relative_bias_part_floats(a), ws, ws_bytes, &a)) return rc;
+    const hipError_t e = trimul::launch_relative_bias_backward(v->dtype, a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "relative bias backward kernel launch");
+    return ok();
+}
+
+int relative_pair(const relative_view_t* v, const void* table, const void* base, int64_t ld_base, void* out,
+                  int64_t ld_out, void* stream) {
+    if (int rc = relative_check(v, true)) return rc;
+    if (relative_empty(v)) return ok();
+    if (!table || !aligned_to(table, v->table_dtype)) return fail(TRI_MUL_EINVAL, "null or misaligned table");
+    trimul::RelativeArgs a = relative_args(v);
+    a.table = table;
+    if (base)
+        if (int rc = relative_rows(v, base, ld_base, "base", &a.base)) return rc;
+    if (int rc = relative_rows(v, out, ld_out, "out", &a.out)) return rc;
+    if (trimul::relative_pair_groups(a) > kMaxGroups) return fail(TRI_MUL_EUNSUPPORTED, "too many rows and columns for one call");
+    const hipError_t e = trimul::launch_relative_pair(v->dtype, a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "relative pair kernel launch");
+    return ok();
+}
+
+int relative_pair_backward_workspace_size(const relative_view_t* v, size_t* bytes) {
+    if (int rc = relative_check(v, true)) return rc;
+    if (!bytes) return fail(TRI_MUL_EINVAL, "null bytes pointer");
+    *bytes = relative_empty(v) ? 0 : 4 * trimul::relative_pair_part_floats(relative_args(v));
+    return ok();
+}
+
+int relative_pair_backward(const relative_view_t* v, const void* dout, int64_t ld_dout, float* dtable, void* ws,
+                           size_t ws_bytes, void* stream) {
+    if (int rc = relative_check(v, true)) return rc;
+    trimul::RelativeArgs a = relative_args(v);
+    const bool empty = relative_empty(v);
+    if (!empty)
+        if (int rc = relative_rows(v, dout, ld_dout, "dout", &a.out)) return rc;
+    if (int rc = relative_gradient(v, dtable, 0, empty ? 0 : trimul::relative_pair_part_floats(a), ws, ws_bytes, &a)) return rc;
+    const hipError_t e = trimul::launch_relative_pair_backward(v->dtype, a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "relative pair backward kernel launch");
     return ok();
 }
 

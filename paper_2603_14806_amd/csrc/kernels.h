@@ -280,4 +280,30 @@ struct CheckpointArgs {
 int64_t checkpoint8_work_groups(CheckpointArgs a);
 hipError_t launch_checkpoint8(int dtype, bool pack, CheckpointArgs a, const void* from, const uint8_t* powers, void* to, hipStream_t s);
 
+// Relative position bias by buckets (relative.hip).  The pair form takes its channels as heads, and of base and out the
+// data and the row stride.
+struct RelativeArgs {
+    int64_t batch, nq, nk;
+    int heads, buckets, reach, table_bf16;
+    const uint8_t* lut;
+    const int32_t *pos_q, *pos_k, *seg_q, *seg_k;                       // seg_q null: one segment
+    int64_t pos_q_batch, pos_k_batch, seg_q_batch, seg_k_batch;
+    const void* table;
+    CrossBias base, out;      // out: dout in the backward
+    float *dtable, *part;     // part: partial sums (workspace)
+    uint32_t* masks;          // which of them are there; filled in by the launcher, as are the next
+    int wide;                 // vectors of eight fit the strides and pointers
+    int hb, tx, cwidth, cblocks, hblocks, waves, splits;
+    int64_t loop, rblocks, span;
+};
+int64_t relative_bias_plan(RelativeArgs& a);                            // work-groups
+int64_t relative_bias_backward_plan(RelativeArgs& a);
+int64_t relative_pair_groups(RelativeArgs a);
+size_t relative_bias_part_floats(RelativeArgs a);
+size_t relative_pair_part_floats(RelativeArgs a);
+hipError_t launch_relative_bias(int dtype, RelativeArgs a, hipStream_t s);
+hipError_t launch_relative_bias_backward(int dtype, RelativeArgs a, hipStream_t s);
+hipError_t launch_relative_pair(int dtype, RelativeArgs a, hipStream_t s);
+hipError_t launch_relative_pair_backward(int dtype, RelativeArgs a, hipStream_t s);
+
 }  // namespace trimul

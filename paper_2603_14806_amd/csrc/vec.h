@@ -11,6 +11,13 @@ template <typename T, int V> struct Vec {
     __device__ __forceinline__ void load(const T* p) {
         if constexpr (V == 1) {
             f[0] = Store<T>::ld(p);
+        } else if constexpr (V == 2 && sizeof(T) == 4) {
+            const float2 x = *reinterpret_cast<const float2*>(p);
+            f[0] = x.x; f[1] = x.y;
+        } else if constexpr (V == 2) {
+            const uint32_t x = *reinterpret_cast<const uint32_t*>(p);
+            f[0] = __uint_as_float(x << 16);
+            f[1] = __uint_as_float(x & 0xffff0000u);
         } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int i = 0; i < V / 4; ++i) {
@@ -36,6 +43,10 @@ template <typename T, int V> struct Vec {
     __device__ __forceinline__ void store(T* p) const {
         if constexpr (V == 1) {
             Store<T>::st(p, f[0]);
+        } else if constexpr (V == 2 && sizeof(T) == 4) {
+            *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]);
+        } else if constexpr (V == 2) {
+            *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(f[0], f[1]);
         } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int i = 0; i < V / 4; ++i)
