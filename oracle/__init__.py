@@ -19,3 +19,4 @@ from .crossattn import cross_attention, cross_attention_backward, softmax_weight
 from .dropout import dropout_add, dropout_backward, keep, philox  # noqa: F401
 from .checkpoint8 import checkpoint8, checkpoint8_values  # noqa: F401
 from . import relative  # noqa: F401
+from . import normrotate  # noqa: F401

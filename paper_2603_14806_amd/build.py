@@ -14,7 +14,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libtrimul.so")
 SOURCES = ["api.hip", "project.hip", "contract.hip", "epilogue.hip", "backward.hip", "opm.hip", "triattn.hip",
-           "crossattn.hip", "crossattn_backward.hip", "dropout.hip", "checkpoint8.hip", "relative.hip"]
+           "crossattn.hip", "crossattn_backward.hip", "dropout.hip", "checkpoint8.hip", "relative.hip", "normrotate.hip"]
 ARCH = "gfx950"
 
 

@@ -18,6 +18,7 @@
 #include "pair_dropout.h"
 #include "checkpoint8.h"
 #include "relative_bias.h"
+#include "norm_rotate.h"
 #include "tri_mul_check.h"
 #include "common.h"
 #include "kernels.h"
@@ -1770,6 +1771,141 @@ int relative_pair_backward(const relative_view_t* v, const void* dout, int64_t l
     if (int rc = relative_gradient(v, dtable, 0, empty ? 0 : trimul::relative_pair_part_floats(a), ws, ws_bytes, &a)) return rc;
     const hipError_t e = trimul::launch_relative_pair_backward(v->dtype, a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "relative pair backward kernel launch");
+    return ok();
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- norms of queries and keys with the position rotation
+
+namespace {
+
+int norm_check(const norm_rotate_view_t* v, const norm_rotate_side_t* q, const norm_rotate_side_t* k) {
+    if (!v) return fail(TRI_MUL_EINVAL, "null view");
+    for (int t : {v->dtype, v->weight_dtype})
+        if (t != TRI_MUL_F32 && t != TRI_MUL_BF16) return fail(TRI_MUL_EINVAL, "bad dtype %d", t);
+    if (v->batch < 0 || v->n < 0) return fail(TRI_MUL_EINVAL, "negative size");
+    if (v->batch >= int64_t(1) << 31 || v->n >= int64_t(1) << 31) return fail(TRI_MUL_EUNSUPPORTED, "2^31 entries or tokens");
+    if (v->d < 8 || v->d > 256 || v->d % 8) return fail(TRI_MUL_EINVAL, "d = %d is not a multiple of 8 in [8, 256]", v->d);
+    if (v->rot < 0 || v->rot > v->d || v->rot % 8) return fail(TRI_MUL_EINVAL, "rot = %d is not a multiple of 8 in [0, d = %d]", v->rot, v->d);
+    if ((v->layer & ~1) || (v->adjacent & ~1)) return fail(TRI_MUL_EINVAL, "layer and adjacent are 0 or 1");
+    if (!(v->eps > 0.f) || std::isinf(v->eps)) return fail(TRI_MUL_EINVAL, "eps must be positive");
+    if (v->rot) {
+        if (!v->freqs || reinterpret_cast<uintptr_t>(v->freqs) % 8) return fail(TRI_MUL_EINVAL, "null or misaligned freqs");
+        if (v->batch && v->n && (!v->positions || reinterpret_cast<uintptr_t>(v->positions) % 4)) return fail(TRI_MUL_EINVAL, "null or misaligned positions");
+        if (v->batch > 1 && (v->positions_batch < 0 || v->positions_batch >= kMaxAxis)) return fail(TRI_MUL_EINVAL, "a batch stride of positions that is negative or above 2^40");
+    }
+    if (!q && !k) return fail(TRI_MUL_EINVAL, "neither queries nor keys");
+    for (const norm_rotate_side_t* x : {q, k}) {
+        if (!x) continue;
+        if (x->heads < 1 || x->heads > 1024) return fail(TRI_MUL_EINVAL, "heads = %d outside [1, 1024]", x->heads);
+        if (!aligned16(x->gain) || !aligned16(x->shift)) return fail(TRI_MUL_EINVAL, "gain and shift must be 16-byte aligned");
+        if (!x->codes != !x->powers) return fail(TRI_MUL_EINVAL, "codes and powers are both given or both NULL");
+        if (!aligned16(x->codes)) return fail(TRI_MUL_EINVAL, "codes must be 16-byte aligned");
+    }
+    return TRI_MUL_OK;
+}
+
+int norm_tensor(const norm_rotate_view_t* v, const cross_attn_tensor_t* t, int heads, const char* name, bool written, trimul::CrossTensor* to) {
+    if (!t) return fail(TRI_MUL_EINVAL, "null %s", name);
+    if (v->batch == 0 || v->n == 0) return TRI_MUL_OK;
+    if (!t->data) return fail(TRI_MUL_EINVAL, "null %s", name);
+    if (!aligned16(t->data)) return fail(TRI_MUL_EINVAL, "%s must be 16-byte aligned", name);
+    const int64_t per = 16 / (int64_t)esize(v->dtype);
+    const struct { int64_t length, stride; } axes[] = {{v->batch, t->batch}, {v->n, t->token}, {heads, t->head}};
+    for (const auto& x : axes) {
+        if (x.length < 2) continue;
+        if (x.stride < 0 || x.stride % per) return fail(TRI_MUL_EINVAL, "strides of %s must be multiples of 16 bytes, and not negative", name);
+        if (x.stride < v->d && (written || x.stride)) return fail(TRI_MUL_EINVAL, "stride %lld of %s below d = %d", (long long)x.stride, name, v->d);
+        if (x.stride >= kMaxAxis) return fail(TRI_MUL_EUNSUPPORTED, "a stride of %s of 2^40 or more", name);
+    }
+    *to = trimul::CrossTensor{t->data, v->batch > 1 ? t->batch : 0, v->n > 1 ? t->token : 0, heads > 1 ? t->head : 0};
+    return TRI_MUL_OK;
+}
+
+trimul::NormArgs norm_args(const norm_rotate_view_t* v, const norm_rotate_side_t* q, const norm_rotate_side_t* k) {
+    trimul::NormArgs a{};
+    a.batch = v->batch;
+    a.n = v->n;
+    a.d = v->d;
+    a.rot = v->rot;
+    a.weight_bf16 = v->weight_dtype == TRI_MUL_BF16;
+    a.layer = v->layer;
+    a.eps = v->eps;
+    a.positions = v->positions;
+    a.positions_batch = v->batch > 1 ? v->positions_batch : 0;
+    a.freqs = v->freqs;
+    const norm_rotate_side_t* sides[] = {q, k};
+    for (int i = 0; i < 2; ++i) {
+        if (!sides[i]) continue;
+        a.side[i].heads = sides[i]->heads;
+        a.side[i].gain = sides[i]->gain;
+        a.side[i].shift = sides[i]->shift;
+        a.side[i].codes = sides[i]->codes;
+        a.side[i].powers = sides[i]->powers;
+    }
+    return a;
+}
+
+size_t norm_part_bytes(const trimul::NormArgs& a) {
+    if (a.batch == 0 || a.n == 0) return 0;
+    const int64_t groups = trimul::norm_rotate_groups(a, true);
+    return groups == 1 ? 0 : (size_t)groups * 16 * a.d;
+}
+
+}  // namespace
+
+extern "C" {
+
+int norm_rotate_forward(const norm_rotate_view_t* v, const norm_rotate_side_t* q, const norm_rotate_side_t* k,
+                        const cross_attn_tensor_t* yq, const cross_attn_tensor_t* yk, void* stream) {
+    if (int rc = norm_check(v, q, k)) return rc;
+    trimul::NormArgs a = norm_args(v, q, k);
+    const struct { const norm_rotate_side_t* x; const cross_attn_tensor_t* y; const char *in, *out; } sides[] = {{q, yq, "q", "yq"}, {k, yk, "k", "yk"}};
+    for (int i = 0; i < 2; ++i) {
+        if (!sides[i].x) continue;
+        if (int rc = norm_tensor(v, &sides[i].x->x, sides[i].x->heads, sides[i].in, false, &a.side[i].x)) return rc;
+        if (int rc = norm_tensor(v, sides[i].y, sides[i].x->heads, sides[i].out, true, &a.side[i].y)) return rc;
+    }
+    const hipError_t e = trimul::launch_norm_rotate(v->dtype, v->adjacent, false, a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "norm and rotation kernel launch");
+    return ok();
+}
+
+int norm_rotate_backward_workspace_size(const norm_rotate_view_t* v, const norm_rotate_side_t* q,
+                                        const norm_rotate_side_t* k, size_t* bytes) {
+    if (int rc = norm_check(v, q, k)) return rc;
+    if (!bytes) return fail(TRI_MUL_EINVAL, "null bytes pointer");
+    *bytes = norm_part_bytes(norm_args(v, q, k));
+    return ok();
+}
+
+int norm_rotate_backward(const norm_rotate_view_t* v, const norm_rotate_side_t* q, const norm_rotate_side_t* k,
+                         const norm_rotate_grad_t* gq, const norm_rotate_grad_t* gk, void* ws, size_t ws_bytes,
+                         void* stream) {
+    if (int rc = norm_check(v, q, k)) return rc;
+    trimul::NormArgs a = norm_args(v, q, k);
+    const bool empty = v->batch == 0 || v->n == 0;
+    const bool held = !(q ? q : k)->x.data;
+    if (!empty && q && k && !q->x.data != !k->x.data) return fail(TRI_MUL_EINVAL, "queries and keys both from x or both from codes");
+    const struct { const norm_rotate_side_t* x; const norm_rotate_grad_t* g; const char *in, *dy, *dx; } sides[] = {{q, gq, "q", "dyq", "dxq"}, {k, gk, "k", "dyk", "dxk"}};
+    for (int i = 0; i < 2; ++i) {
+        const auto& x = sides[i];
+        if (!x.x) continue;
+        if (!x.g) return fail(TRI_MUL_EINVAL, "null gradients of %s", x.in);
+        if (!empty && held && !x.x->codes) return fail(TRI_MUL_EINVAL, "null %s, and no codes", x.in);
+        if (!held)
+            if (int rc = norm_tensor(v, &x.x->x, x.x->heads, x.in, false, &a.side[i].x)) return rc;
+        if (int rc = norm_tensor(v, &x.g->dy, x.x->heads, x.dy, false, &a.side[i].y)) return rc;
+        if (int rc = norm_tensor(v, &x.g->dx, x.x->heads, x.dx, true, &a.side[i].dx)) return rc;
+        if (!aligned_to(x.g->dgain, TRI_MUL_F32) || !aligned_to(x.g->dshift, TRI_MUL_F32)) return fail(TRI_MUL_EINVAL, "dgain and dshift must be aligned to their type");
+        a.side[i].dgain = x.g->dgain;
+        a.side[i].dshift = x.g->dshift;
+    }
+    if (int rc = cross_workspace(ws, ws_bytes, norm_part_bytes(a))) return rc;
+    a.part = static_cast<float*>(ws);
+    const hipError_t e = trimul::launch_norm_rotate(v->dtype, v->adjacent, true, a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "norm and rotation backward kernel launch");
     return ok();
 }
 

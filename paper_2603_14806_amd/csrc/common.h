@@ -48,6 +48,17 @@ __device__ __forceinline__ float sum_lanes8(float v) {
     return v;
 }
 
+// The same over G consecutive lanes (a power of two up to 32): 16 by the row's mirror, 32 by a shuffle.
+template <int G>
+__device__ __forceinline__ float sum_lanes(float v) {
+    if constexpr (G >= 2) v += dpp_mov<0xb1>(v);
+    if constexpr (G >= 4) v += dpp_mov<0x4e>(v);
+    if constexpr (G >= 8) v += dpp_mov<0x141>(v);
+    if constexpr (G >= 16) v += dpp_mov<0x140>(v);    // row_mirror
+    if constexpr (G >= 32) v += __shfl_xor(v, 16);
+    return v;
+}
+
 // Element e (a compile-time constant after unrolling) of a float4.
 __device__ __forceinline__ float f4_get(const float4& v, int e) {
     return e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w;

@@ -306,4 +306,30 @@ hipError_t launch_relative_bias_backward(int dtype, RelativeArgs a, hipStream_t 
 hipError_t launch_relative_pair(int dtype, RelativeArgs a, hipStream_t s);
 hipError_t launch_relative_pair_backward(int dtype, RelativeArgs a, hipStream_t s);
 
+// Norms of queries and keys by head with the position rotation (normrotate.hip).
+struct NormSide {
+    int heads;                // 0: this side is missing
+    CrossTensor x, y, dx;     // y: dy in the backward
+    const void *gain, *shift;
+    int8_t* codes;
+    uint8_t* powers;
+    float *dgain, *dshift;
+    int steps;                // filled in by the launcher: head steps of a token
+};
+struct NormArgs {
+    int64_t batch, n;
+    int d, rot, weight_bf16, layer;
+    float eps, inv_d;
+    const int32_t* positions;
+    int64_t positions_batch;
+    const double* freqs;
+    NormSide side[2];
+    float* part;              // [work-groups][4][d]: dgain and dshift of the queries, then of the keys
+    int head_slots;           // filled in by the launcher, as are the next: heads of a token that a wave takes at once
+    int64_t tiles, chunk, chunks, items;              // token tiles, entries of an item, items in all
+    int64_t waves, step_tile, step_chunk;             // waves in all; what lies between two items of one wave
+};
+int64_t norm_rotate_groups(NormArgs a, bool backward);                  // work-groups
+hipError_t launch_norm_rotate(int dtype, bool adjacent, bool backward, NormArgs a, hipStream_t s);
+
 }  // namespace trimul
