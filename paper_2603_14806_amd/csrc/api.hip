@@ -1847,10 +1847,9 @@ trimul::NormArgs norm_args(const norm_rotate_view_t* v, const norm_rotate_side_t
     return a;
 }
 
-size_t norm_part_bytes(const trimul::NormArgs& a) {
+size_t norm_part_bytes(const trimul::NormArgs& a, int dtype) {
     if (a.batch == 0 || a.n == 0) return 0;
-    const int64_t groups = trimul::norm_rotate_groups(a, true);
-    return groups == 1 ? 0 : (size_t)groups * 16 * a.d;
+    return (size_t)trimul::norm_rotate_backward_groups(a, dtype) * 8 * a.d;
 }
 
 }  // namespace
@@ -1876,7 +1875,7 @@ int norm_rotate_backward_workspace_size(const norm_rotate_view_t* v, const norm_
                                         const norm_rotate_side_t* k, size_t* bytes) {
     if (int rc = norm_check(v, q, k)) return rc;
     if (!bytes) return fail(TRI_MUL_EINVAL, "null bytes pointer");
-    *bytes = norm_part_bytes(norm_args(v, q, k));
+    *bytes = norm_part_bytes(norm_args(v, q, k), v->dtype);
     return ok();
 }
 
@@ -1902,7 +1901,7 @@ int norm_rotate_backward(const norm_rotate_view_t* v, const norm_rotate_side_t* 
         a.side[i].dgain = x.g->dgain;
         a.side[i].dshift = x.g->dshift;
     }
-    if (int rc = cross_workspace(ws, ws_bytes, norm_part_bytes(a))) return rc;
+    if (int rc = cross_workspace(ws, ws_bytes, norm_part_bytes(a, v->dtype))) return rc;
     a.part = static_cast<float*>(ws);
     const hipError_t e = trimul::launch_norm_rotate(v->dtype, v->adjacent, true, a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "norm and rotation backward kernel launch");

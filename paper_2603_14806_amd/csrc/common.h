@@ -48,13 +48,18 @@ __device__ __forceinline__ float sum_lanes8(float v) {
     return v;
 }
 
-// The same over G consecutive lanes (a power of two up to 32): 16 by the row's mirror, 32 by a shuffle.
+// The same over G consecutive lanes (a power of two up to 32): 16 by the row's mirror, 32 by a shuffle.  (A move of a lane
+// that is always there, into zero, becomes a modifier of the addition.)
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
 template <int G>
 __device__ __forceinline__ float sum_lanes(float v) {
-    if constexpr (G >= 2) v += dpp_mov<0xb1>(v);
-    if constexpr (G >= 4) v += dpp_mov<0x4e>(v);
-    if constexpr (G >= 8) v += dpp_mov<0x141>(v);
-    if constexpr (G >= 16) v += dpp_mov<0x140>(v);    // row_mirror
+    if constexpr (G >= 2) v = dpp_add<0xb1>(v);
+    if constexpr (G >= 4) v = dpp_add<0x4e>(v);
+    if constexpr (G >= 8) v = dpp_add<0x141>(v);
+    if constexpr (G >= 16) v = dpp_add<0x140>(v);    // row_mirror
     if constexpr (G >= 32) v += __shfl_xor(v, 16);
     return v;
 }

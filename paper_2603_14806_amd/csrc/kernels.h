@@ -314,7 +314,11 @@ struct NormSide {
     int8_t* codes;
     uint8_t* powers;
     float *dgain, *dshift;
-    int steps;                // filled in by the launcher: head steps of a token
+    int slots, steps;         // filled in by the launcher, as are the next: heads of a token that a wave takes at once, and
+                              // the steps that all of them take
+    int groups;                                       // work-groups
+    int64_t tiles, chunk, chunks;                     // token tiles, entries of an item, chunks of entries
+    int64_t step_tile, step_chunk;                    // what lies between two items of one wave
 };
 struct NormArgs {
     int64_t batch, n;
@@ -324,12 +328,10 @@ struct NormArgs {
     int64_t positions_batch;
     const double* freqs;
     NormSide side[2];
-    float* part;              // [work-groups][4][d]: dgain and dshift of the queries, then of the keys
-    int head_slots;           // filled in by the launcher, as are the next: heads of a token that a wave takes at once
-    int64_t tiles, chunk, chunks, items;              // token tiles, entries of an item, items in all
-    int64_t waves, step_tile, step_chunk;             // waves in all; what lies between two items of one wave
+    float* part;              // [work-groups][2][d]: dgain and dshift
+    int ragged;               // filled in by the launcher: a row has fewer eighths than lanes
 };
-int64_t norm_rotate_groups(NormArgs a, bool backward);                  // work-groups
+int64_t norm_rotate_backward_groups(NormArgs a, int dtype);             // its work-groups
 hipError_t launch_norm_rotate(int dtype, bool adjacent, bool backward, NormArgs a, hipStream_t s);
 
 }  // namespace trimul

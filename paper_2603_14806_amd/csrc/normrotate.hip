@@ -11,86 +11,104 @@
 #include "kernels.h"
 #include "vec.h"
 
+// Products and sums are joined where the source says so and nowhere else: a row has the same bits whichever of the kernels
+// below, and whichever place in its loop, it comes to.
+#pragma clang fp contract(off)
+
 namespace trimul {
 namespace {
 
-constexpr double kInvTwoPi = 0.15915494309189533577;
+constexpr double kTwoOverPi = 0.63661977236758134308;
 
-// cos and sin of p f, f in turns: the angle in quarter turns is reduced in 64 bits, where far positions keep their
-// fraction, and what is left is at most half a quarter turn either way.
+// cos and sin of p f, f in quarter turns.  The angle is reduced in 64 bits, where far positions keep their fraction:
+// adding 1.5 2^52 rounds it to whole quarters (their number in the low bits), and at most half a quarter r is left
+// either way.  There sin(pi / 2 r) = r S(r^2) and cos(pi / 2 r) = 1 + r^2 C(r^2) with cubics S and C through the
+// Chebyshev points of [0, 1/4] (3.2e-9 and 1.9e-10 off; with float32's own rounding 1.5 2^-24 and 1.0 2^-24).
+// (A library call for both took 46.2 us in place of 39.5 for 2 x 6000 tokens, 16 + 16 heads of 128, bf16.)
 __device__ __forceinline__ void turn(int p, double f, float& c, float& s) {
-    const double t = 4.0 * ((double)p * f), q = rint(t);
-    float a, b;
-    sincospif(0.5f * (float)(t - q), &b, &a);
-    const int k = (int)(q - 4.0 * floor(q * 0.25));            // quarter turns, 0..3
-    c = k == 0 ? a : k == 1 ? -b : k == 2 ? -a : b;
-    s = k == 0 ? b : k == 1 ? a : k == 2 ? -b : -a;
+    constexpr double kWhole = 6755399441055744.0;
+    const double t = (double)p * f, m = t + kWhole;
+    const float r = (float)(t - (m - kWhole)), x = r * r;
+    const uint32_t k = (uint32_t)__double2loint(m);
+    const float b = r * __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(-4.602149212632179e-3f, x, 7.968021764769763e-2f), x, -0.6459634776648043f), x, 1.5707963219532355f);
+    const float a = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(__builtin_fmaf(9.067398957297847e-4f, x, -2.086152834093593e-2f), x, 0.253669410356929f), x, -1.2337005493742117f), x, 1.f);
+    const bool odd = k & 1;
+    c = __uint_as_float(__float_as_uint(odd ? b : a) ^ ((k + 1) << 30 & 0x80000000u));
+    s = __uint_as_float(__float_as_uint(odd ? a : b) ^ (k << 30 & 0x80000000u));
 }
 
-// A lane's eight values: f[0..3] and f[4..7] are the two halves of its places lo and hi (HALVES), or eight in a row.
-template <typename T, bool HALVES>
-__device__ __forceinline__ void load8(float (&f)[8], const T* p, int lo, int hi) {
-    if constexpr (HALVES) {
-        Vec<T, 4> a, b;
-        a.load(p + lo);
-        b.load(p + hi);
+// A lane's eight values as they lie in memory: four from each of two places (HALVES), or eight in a row.
+template <typename T, bool HALVES> struct Raw {
+    static constexpr int kWords = sizeof(T) == 4 ? 8 : 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { f[i] = a.f[i]; f[4 + i] = b.f[i]; }
-    } else {
-        Vec<T, 8> a;
-        a.load(p + lo);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = a.f[i];
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
     }
-}
-template <typename T, bool HALVES>
-__device__ __forceinline__ void store8(const float (&f)[8], T* p, int lo, int hi) {
-    if constexpr (HALVES) {
-        Vec<T, 4> a, b;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { a.f[i] = f[i]; b.f[i] = f[4 + i]; }
-        a.store(p + lo);
-        b.store(p + hi);
-    } else {
-        Vec<T, 8> a;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a.f[i] = f[i];
-        a.store(p + lo);
+    __device__ __forceinline__ void load(const T* p, int lo, int hi) {
+        if constexpr (sizeof(T) == 4) {
+            put(0, *reinterpret_cast<const uint4*>(p + lo));
+            put(4, *reinterpret_cast<const uint4*>(p + (HALVES ? hi : lo + 4)));
+        } else if constexpr (HALVES) {
+            const uint2 a = *reinterpret_cast<const uint2*>(p + lo), b = *reinterpret_cast<const uint2*>(p + hi);
+            w[0] = a.x; w[1] = a.y; w[2] = b.x; w[3] = b.y;
+        } else {
+            put(0, *reinterpret_cast<const uint4*>(p + lo));
+        }
     }
-}
+    __device__ __forceinline__ void values(float (&f)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            f[i] = sizeof(T) == 4 ? __uint_as_float(w[i % kWords]) : __uint_as_float(i & 1 ? w[i / 2 % kWords] & 0xffff0000u : w[i / 2 % kWords] << 16);
+    }
+    static __device__ __forceinline__ void store(const float (&f)[8], T* p, int lo, int hi) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float4*>(p + lo) = make_float4(f[0], f[1], f[2], f[3]);
+            *reinterpret_cast<float4*>(p + (HALVES ? hi : lo + 4)) = make_float4(f[4], f[5], f[6], f[7]);
+        } else if constexpr (HALVES) {
+            *reinterpret_cast<uint2*>(p + lo) = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
+            *reinterpret_cast<uint2*>(p + hi) = make_uint2(pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+        } else {
+            *reinterpret_cast<uint4*>(p + lo) = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+        }
+    }
+private:
+    __device__ __forceinline__ void put(int i, uint4 x) { w[i % kWords] = x.x; w[(i + 1) % kWords] = x.y; w[(i + 2) % kWords] = x.z; w[(i + 3) % kWords] = x.w; }
+};
 
 // Pair m of a lane is (f[m], f[4 + m]) of halves, (f[2 m], f[2 m + 1]) of neighbours; back: by the negative angle.
 template <bool HALVES, bool BACK>
 __device__ __forceinline__ void rotate8(float (&f)[8], const float (&c)[4], const float (&s)[4]) {
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-        constexpr float sign = BACK ? -1.f : 1.f;
+        const float sine = BACK ? -s[m] : s[m];
         float& a = f[HALVES ? m : 2 * m];
         float& b = f[HALVES ? 4 + m : 2 * m + 1];
-        const float ya = a * c[m] - sign * (b * s[m]), yb = sign * (a * s[m]) + b * c[m];
+        const float ya = __builtin_fmaf(a, c[m], -(b * sine)), yb = __builtin_fmaf(b, c[m], a * sine);
         a = ya;
         b = yb;
     }
 }
 
-// A wave's place in an item: which lanes are where.
+// What a lane of a wave has of every item.
 struct Lane {
     int l, lo, hi;          // eighth of the row, and where its values are
     int head, token;        // slots
-    bool live;              // the row has an eighth l
+    bool live;              // the row has an eighth l (another lane reads the first one again, and counts for nothing)
 };
 
 template <int G, bool HALVES>
-__device__ __forceinline__ Lane lane_of(const NormArgs& a) {
+__device__ __forceinline__ Lane lane_of(const NormArgs& a, const NormSide& q) {
     const int lane = threadIdx.x % 64, slot = lane / G;
     Lane x;
     x.l = lane % G;
     x.live = 8 * x.l < a.d;
-    x.head = slot & (a.head_slots - 1);
-    x.token = slot / a.head_slots;
-    const bool turned = HALVES && 8 * x.l < a.rot;
-    x.lo = turned ? 4 * x.l : 8 * x.l;
-    x.hi = turned ? a.rot / 2 + 4 * x.l : 8 * x.l + 4;
+    x.head = slot & (q.slots - 1);
+    x.token = slot / q.slots;
+    const int l = x.live ? x.l : 0;
+    const bool turned = HALVES && 8 * l < a.rot;
+    x.lo = turned ? 4 * l : 8 * l;
+    x.hi = turned ? a.rot / 2 + 4 * l : 8 * l + 4;
     return x;
 }
 
@@ -99,249 +117,366 @@ template <bool HALVES>
 __device__ __forceinline__ void weights8(float (&f)[8], const void* w, bool bf16, const Lane& x, float none) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = none;
-    if (!w || !x.live) return;
-    if (bf16) load8<bf16_t, HALVES>(f, static_cast<const bf16_t*>(w), x.lo, x.hi);
-    else load8<float, HALVES>(f, static_cast<const float*>(w), x.lo, x.hi);
+    if (!w) return;
+    if (bf16) {
+        Raw<bf16_t, HALVES> r;
+        r.load(static_cast<const bf16_t*>(w), x.lo, x.hi);
+        r.values(f);
+    } else {
+        Raw<float, HALVES> r;
+        r.load(static_cast<const float*>(w), x.lo, x.hi);
+        r.values(f);
+    }
 }
 
 // u (in the place of x) and r of a row.
-template <int G>
+template <int G, bool LAYER>
 __device__ __forceinline__ float normalise8(float (&f)[8], const NormArgs& a, bool live) {
-    if (a.layer) {
+    if constexpr (LAYER) {
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += f[i];
-        const float mean = sum_lanes<G>(sum) * a.inv_d;
+        const float total = sum_lanes<G>(sum);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = live ? f[i] - mean : 0.f;
+        for (int i = 0; i < 8; ++i) f[i] = __builtin_fmaf(-total, a.inv_d, f[i]);
+        if (a.ragged)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = live ? f[i] : 0.f;
     }
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(f[i], f[i], sum);
-    const float r = rsqrtf(sum_lanes<G>(sum) * a.inv_d + a.eps);
+    const float r = rsqrtf(__builtin_fmaf(sum_lanes<G>(sum), a.inv_d, a.eps));
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] *= r;
     return r;
 }
 
-// The angles of a token's pairs in this lane.
-__device__ __forceinline__ void angles(const NormArgs& a, const Lane& x, const double (&f)[4], int64_t entry, int64_t token, float (&c)[4], float (&s)[4]) {
-    const bool turned = 8 * x.l < a.rot && token < a.n;
-    const int p = turned ? a.positions[entry * a.positions_batch + token] : 0;
-#pragma unroll
-    for (int m = 0; m < 4; ++m) turn(p, f[m], c[m], s[m]);
-}
-
-__device__ __forceinline__ void frequencies(const NormArgs& a, const Lane& x, double (&f)[4]) {
-#pragma unroll
-    for (int m = 0; m < 4; ++m) f[m] = 8 * x.l < a.rot ? a.freqs[4 * x.l + m] * kInvTwoPi : 0.0;
-}
-
-// A wave's items: token tile and chunk of entries, `waves` items apart.
+// A wave's items: token tile and chunk of entries, as many items apart as there are waves on its side.
 struct Item {
     int64_t tile, chunk;
-    __device__ __forceinline__ Item(const NormArgs& a, int64_t wave) : tile(wave % a.tiles), chunk(wave / a.tiles) {}
-    __device__ __forceinline__ void next(const NormArgs& a) {
-        tile += a.step_tile;
-        chunk += a.step_chunk;
-        if (tile >= a.tiles) {
-            tile -= a.tiles;
+    __device__ __forceinline__ Item(const NormArgs& a, const NormSide& q, bool keys) {
+        const int64_t wave = (int64_t)(blockIdx.x - (keys ? a.side[0].groups : 0)) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        tile = wave % q.tiles;
+        chunk = wave / q.tiles;
+    }
+    __device__ __forceinline__ void next(const NormSide& q) {
+        tile += q.step_tile;
+        chunk += q.step_chunk;
+        if (tile >= q.tiles) {
+            tile -= q.tiles;
             ++chunk;
         }
     }
 };
 
-// A row's place: head step i of an item's entries.
-struct Row {
-    int64_t entry;
-    int head;
-    bool live;
+// Where an item's rows are.
+struct Place {
+    int64_t token0, token, entry;      // the tile's first token, the lane's, the first entry
+    int rows;
+    __device__ __forceinline__ Place(const NormArgs& a, const NormSide& q, const Item& item, const Lane& x, int tokens)
+        : token0(item.tile * tokens), token(token0 + x.token), entry(item.chunk * q.chunk), rows((int)min(q.chunk, a.batch - entry) * q.steps) {}
 };
 
-template <typename T, int G, bool HALVES>
-__global__ __launch_bounds__(256) void k_norm_rotate(const NormArgs a) {
-    constexpr int U = 4;
-    const Lane x = lane_of<G, HALVES>(a);
-    const int tokens = 64 / G / a.head_slots;
+// The rows of a side in an item, one after the other: head steps of an entry, then the next entry.
+struct Rows {
+    int64_t entry;
+    int step;
+    __device__ __forceinline__ void next(int steps) {
+        if (++step == steps) {
+            step = 0;
+            ++entry;
+        }
+    }
+    // of a tensor: the part of a row's place that is the same for the wave, and the lane's own part
+    __device__ __forceinline__ int64_t of(const NormSide& q, const CrossTensor& t, int64_t token0) const {
+        return entry * t.batch + token0 * t.token + (int64_t)(step * q.slots) * t.head;
+    }
+    static __device__ __forceinline__ int64_t own(const CrossTensor& t, const Lane& x) { return x.token * t.token + x.head * t.head; }
+};
+
+// The angles' part of an item: the position is asked for early, the sines follow when the rows are on their way.
+struct Angles {
     double f[4];
-    frequencies(a, x, f);
-    const int64_t wave = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-    for (Item item(a, wave); item.chunk < a.chunks; item.next(a)) {
-        const int64_t token = item.tile * tokens + x.token, b0 = item.chunk * a.chunk;
-        const int entries = (int)min(a.chunk, a.batch - b0);
-        float c[4], s[4];
-        angles(a, x, f, b0, token, c, s);
-#pragma unroll 1
-        for (int side = 0; side < 2; ++side) {
-            const NormSide& q = a.side[side];
-            if (q.heads == 0) continue;
-            float gain[8], shift[8];
-            weights8<HALVES>(gain, q.gain, a.weight_bf16, x, 1.f);
-            weights8<HALVES>(shift, q.shift, a.weight_bf16, x, 0.f);
-            const int rows = entries * q.steps;
-            int entry = 0, step = 0;
-            for (int i = 0; i < rows; i += U) {
-                float v[U][8];
-                Row row[U];
+    int p;                  // the position that was asked for last
+    __device__ __forceinline__ Angles(const NormArgs& a, const Lane& x) : p(0) {
+        const bool turned = x.live && 8 * x.l < a.rot;
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    row[u] = Row{b0 + entry, step * a.head_slots + x.head, false};
-                    row[u].live = i + u < rows && x.live && token < a.n && row[u].head < q.heads;
-                    if (++step == q.steps) {
-                        step = 0;
-                        ++entry;
-                    }
+        for (int m = 0; m < 4; ++m) f[m] = turned ? a.freqs[4 * x.l + m] * kTwoOverPi : 0.0;
+    }
+    __device__ __forceinline__ void ask(const NormArgs& a, const Place& at) {
+        if (a.rot && at.token < a.n) p = a.positions[at.entry * a.positions_batch + at.token];
+    }
+    __device__ __forceinline__ void get(const NormArgs& a, float (&c)[4], float (&s)[4]) const {
+        if (a.rot == 0) return;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[u][e] = 0.f;
-                    if (row[u].live) load8<T, HALVES>(v[u], static_cast<const T*>(q.x.data) + row[u].entry * q.x.batch + token * q.x.token + row[u].head * q.x.head, x.lo, x.hi);
-                }
+        for (int m = 0; m < 4; ++m) turn(p, f[m], c[m], s[m]);
+    }
+};
+
+// Four rows are in flight while four are worked on, side by side (single ones at the end).
+template <typename T, int G, bool HALVES, bool LAYER, bool HOLD>
+__global__ __launch_bounds__(256, sizeof(T) == 2 && !HOLD ? 4 : 3) void k_norm_rotate(const NormArgs a) {
+    constexpr int U = 4;
+    const bool keys = blockIdx.x >= a.side[0].groups;
+    const NormSide& q = a.side[keys];
+    const Lane x = lane_of<G, HALVES>(a, q);
+    const int tokens = 64 / G / q.slots;
+    Angles angles(a, x);
+    float gain[8], shift[8];
+    weights8<HALVES>(gain, q.gain, a.weight_bf16, x, 1.f);
+    weights8<HALVES>(shift, q.shift, a.weight_bf16, x, 0.f);
+    const int64_t own_x = Rows::own(q.x, x), own_y = Rows::own(q.y, x);
+    Raw<T, HALVES> raw[U];
+    auto load = [&](const Place& at, Rows& row, int left) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (i + u >= rows) break;
-                    if (q.codes) {
-                        uint32_t top = 0;
+        for (int u = 0; u < U; ++u) {
+            raw[u].clear();
+            if (u < left && at.token < a.n && row.step * q.slots + x.head < q.heads)
+                raw[u].load(static_cast<const T*>(q.x.data) + row.of(q, q.x, at.token0) + own_x, x.lo, x.hi);
+            row.next(q.steps);
+        }
+    };
+    for (Item item(a, q, keys); item.chunk < q.chunks; item.next(q)) {
+        const Place here(a, q, item, x, tokens);
+        const int64_t token0 = here.token0, token = here.token;
+        angles.ask(a, here);
+        Rows ahead{here.entry, 0}, row{here.entry, 0};
+        load(here, ahead, here.rows);
+        float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f};
+        angles.get(a, c, s);
+        auto work = [&](auto count, const Raw<T, HALVES>* now) {
+            constexpr int N = decltype(count)::value;
+            float v[N][8];
+            bool live[N];
+            Rows at[N];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[u][e]) & 0x7fffffffu);
-                        top = umax_lanes<G>(top);
-                        const uint32_t byte = power_byte(top);
-                        const float inverse = power_inverse(byte);
+            for (int u = 0; u < N; ++u) {
+                at[u] = row;
+                live[u] = token < a.n && row.step * q.slots + x.head < q.heads && x.live;
+                row.next(q.steps);
+                now[u].values(v[u]);
+                if (a.ragged)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[u][e] = x.live ? v[u][e] : 0.f;
+            }
+            if (HOLD && q.codes) {
+#pragma unroll
+                for (int u = 0; u < N; ++u) {
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[u][e]) & 0x7fffffffu);
+                    top = umax_lanes<G>(top);
+                    const uint32_t byte = power_byte(top);
+                    const float inverse = power_inverse(byte);
+                    uint32_t lo, hi;
+                    if (power_cut(top)) {
                         float w[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) w[e] = power_cut(top) ? fminf(fmaxf(v[u][e], -kTopValue), kTopValue) : v[u][e];
-                        const uint32_t lo = codes4(w[0], w[1], w[2], w[3], inverse), hi = codes4(w[4], w[5], w[6], w[7], inverse);
-                        if (row[u].live) {
-                            const int64_t at = (row[u].entry * a.n + token) * q.heads + row[u].head;
-                            int8_t* to = q.codes + at * a.d;
-                            if constexpr (HALVES) {
-                                *reinterpret_cast<uint32_t*>(to + x.lo) = lo;
-                                *reinterpret_cast<uint32_t*>(to + x.hi) = hi;
-                            } else {
-                                *reinterpret_cast<uint2*>(to + x.lo) = make_uint2(lo, hi);
-                            }
-                            if (x.l == 0) q.powers[at] = (uint8_t)byte;
-                        }
+                        for (int e = 0; e < 8; ++e) w[e] = fminf(fmaxf(v[u][e], -kTopValue), kTopValue);
+                        lo = codes4(w[0], w[1], w[2], w[3], inverse);
+                        hi = codes4(w[4], w[5], w[6], w[7], inverse);
+                    } else {
+                        lo = codes4(v[u][0], v[u][1], v[u][2], v[u][3], inverse);
+                        hi = codes4(v[u][4], v[u][5], v[u][6], v[u][7], inverse);
                     }
-                    normalise8<G>(v[u], a, x.live);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[u][e] = __builtin_fmaf(v[u][e], gain[e], shift[e]);
-                    rotate8<HALVES, false>(v[u], c, s);
-                    if (row[u].live) store8<T, HALVES>(v[u], static_cast<T*>(q.y.data) + row[u].entry * q.y.batch + token * q.y.token + row[u].head * q.y.head, x.lo, x.hi);
+                    if (!live[u]) continue;
+                    const int64_t place = (at[u].entry * a.n + token) * q.heads + at[u].step * q.slots + x.head;
+                    int8_t* to = q.codes + place * a.d;
+                    if constexpr (HALVES) {
+                        *reinterpret_cast<uint32_t*>(to + x.lo) = lo;
+                        *reinterpret_cast<uint32_t*>(to + x.hi) = hi;
+                    } else {
+                        *reinterpret_cast<uint2*>(to + x.lo) = make_uint2(lo, hi);
+                    }
+                    if (x.l == 0) q.powers[place] = (uint8_t)byte;
                 }
+            }
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                normalise8<G, LAYER>(v[u], a, x.live);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[u][e] = __builtin_fmaf(v[u][e], gain[e], shift[e]);
+                rotate8<HALVES, false>(v[u], c, s);
+            }
+#pragma unroll
+            for (int u = 0; u < N; ++u)
+                if (live[u]) Raw<T, HALVES>::store(v[u], static_cast<T*>(q.y.data) + at[u].of(q, q.y, token0) + own_y, x.lo, x.hi);
+        };
+        for (int i = 0; i < here.rows; i += U) {
+            Raw<T, HALVES> now[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) now[u] = raw[u];
+            if (i + U < here.rows) load(here, ahead, here.rows - i - U);
+            if (i + U <= here.rows) {
+                work(std::integral_constant<int, U>{}, now);
+            } else {
+#pragma unroll
+                for (int u = 0; u < U - 1; ++u)
+                    if (i + u < here.rows) work(std::integral_constant<int, 1>{}, now + u);
             }
         }
     }
 }
 
-template <typename T, int G, bool HALVES>
+// A lane's eight inputs of the backward: values, or codes and their power.
+template <typename T, bool HALVES, bool HELD> struct Input {
+    Raw<T, HALVES> raw;
+    __device__ __forceinline__ void clear() { raw.clear(); }
+    __device__ __forceinline__ void values(float (&f)[8]) const { raw.values(f); }
+};
+template <typename T, bool HALVES> struct Input<T, HALVES, true> {
+    uint32_t lo, hi, byte;
+    __device__ __forceinline__ void clear() { lo = hi = byte = 0; }
+    __device__ __forceinline__ void values(float (&f)[8]) const {
+        const float scale = power_value(byte);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f[e] = code_value(lo, e) * scale;
+            f[4 + e] = code_value(hi, e) * scale;
+        }
+    }
+};
+
+template <typename T, int G, bool HALVES, bool LAYER, bool HELD>
 __global__ __launch_bounds__(256) void k_norm_rotate_backward(const NormArgs a) {
     constexpr int U = 2;
-    __shared__ float sums[4][4][256];                       // by wave: dgain and dshift of the queries, and of the keys
-    const Lane x = lane_of<G, HALVES>(a);
-    const int tokens = 64 / G / a.head_slots, w = threadIdx.x / 64;
-    double f[4];
-    frequencies(a, x, f);
-    float total[2][2][8];
+    __shared__ float sums[4][2][256];                       // by wave: dgain and dshift
+    const bool keys = blockIdx.x >= a.side[0].groups;
+    const NormSide& q = a.side[keys];
+    const Lane x = lane_of<G, HALVES>(a, q);
+    const int tokens = 64 / G / q.slots, w = threadIdx.x / 64;
+    Angles angles(a, x);
+    float total[2][8], gain[8];
+    weights8<HALVES>(gain, q.gain, a.weight_bf16, x, 1.f);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) total[i / 16][i / 8 % 2][i % 8] = 0.f;
-    const int64_t wave = (int64_t)blockIdx.x * 4 + w;
-    for (Item item(a, wave); item.chunk < a.chunks; item.next(a)) {
-        const int64_t token = item.tile * tokens + x.token, b0 = item.chunk * a.chunk;
-        const int entries = (int)min(a.chunk, a.batch - b0);
-        float c[4], s[4];
-        angles(a, x, f, b0, token, c, s);
+    for (int e = 0; e < 8; ++e) total[0][e] = total[1][e] = 0.f;
+    const int64_t own_x = Rows::own(q.x, x), own_y = Rows::own(q.y, x), own_dx = Rows::own(q.dx, x);
+    Input<T, HALVES, HELD> in[U];
+    Raw<T, HALVES> dy[U];
+    auto load = [&](const Place& at, Rows& row, int left) {
 #pragma unroll
-        for (int side = 0; side < 2; ++side) {
-            const NormSide& q = a.side[side];
-            if (q.heads == 0) continue;
-            float gain[8];
-            weights8<HALVES>(gain, q.gain, a.weight_bf16, x, 1.f);
-            const int rows = entries * q.steps;
-            int entry = 0, step = 0;
-            for (int i = 0; i < rows; i += U) {
-                float v[U][8], g[U][8];
-                Row row[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    row[u] = Row{b0 + entry, step * a.head_slots + x.head, false};
-                    row[u].live = i + u < rows && x.live && token < a.n && row[u].head < q.heads;
-                    if (++step == q.steps) {
-                        step = 0;
-                        ++entry;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[u][e] = g[u][e] = 0.f;
-                    if (!row[u].live) continue;
-                    if (q.x.data) {
-                        load8<T, HALVES>(v[u], static_cast<const T*>(q.x.data) + row[u].entry * q.x.batch + token * q.x.token + row[u].head * q.x.head, x.lo, x.hi);
+        for (int u = 0; u < U; ++u) {
+            in[u].clear();
+            dy[u].clear();
+            if (u < left && at.token < a.n && row.step * q.slots + x.head < q.heads) {
+                if constexpr (HELD) {
+                    const int64_t place = (row.entry * a.n + at.token) * q.heads + row.step * q.slots + x.head;
+                    const int8_t* from = q.codes + place * a.d;
+                    if constexpr (HALVES) {
+                        in[u].lo = *reinterpret_cast<const uint32_t*>(from + x.lo);
+                        in[u].hi = *reinterpret_cast<const uint32_t*>(from + x.hi);
                     } else {
-                        const int64_t at = (row[u].entry * a.n + token) * q.heads + row[u].head;
-                        const int8_t* from = q.codes + at * a.d;
-                        const float scale = power_value(q.powers[at]);
-                        const uint32_t lo = *reinterpret_cast<const uint32_t*>(from + x.lo), hi = *reinterpret_cast<const uint32_t*>(from + x.hi);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            v[u][e] = code_value(lo, e) * scale;
-                            v[u][4 + e] = code_value(hi, e) * scale;
-                        }
+                        const uint2 both = *reinterpret_cast<const uint2*>(from + x.lo);
+                        in[u].lo = both.x;
+                        in[u].hi = both.y;
                     }
-                    load8<T, HALVES>(g[u], static_cast<const T*>(q.y.data) + row[u].entry * q.y.batch + token * q.y.token + row[u].head * q.y.head, x.lo, x.hi);
+                    in[u].byte = q.powers[place];
+                } else {
+                    in[u].raw.load(static_cast<const T*>(q.x.data) + row.of(q, q.x, at.token0) + own_x, x.lo, x.hi);
                 }
+                dy[u].load(static_cast<const T*>(q.y.data) + row.of(q, q.y, at.token0) + own_y, x.lo, x.hi);
+            }
+            row.next(q.steps);
+        }
+    };
+    for (Item item(a, q, keys); item.chunk < q.chunks; item.next(q)) {
+        const Place here(a, q, item, x, tokens);
+        const int64_t token0 = here.token0, token = here.token;
+        angles.ask(a, here);
+        Rows ahead{here.entry, 0}, row{here.entry, 0};
+        load(here, ahead, here.rows);
+        float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f};
+        angles.get(a, c, s);
+        auto work = [&](auto count, const Input<T, HALVES, HELD>* in_now, const Raw<T, HALVES>* dy_now) {
+            constexpr int N = decltype(count)::value;
+            float v[N][8], g[N][8];
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (i + u >= rows) break;
-                    const float r = normalise8<G>(v[u], a, x.live);
-                    rotate8<HALVES, true>(g[u], c, s);
-                    float mean = 0.f, along = 0.f;
+            for (int u = 0; u < N; ++u) {
+                in_now[u].values(v[u]);
+                dy_now[u].values(g[u]);
+                if (a.ragged)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        total[side][0][e] = __builtin_fmaf(g[u][e], v[u][e], total[side][0][e]);
-                        total[side][1][e] += g[u][e];
-                        g[u][e] *= gain[e];
-                        mean += g[u][e];
-                        along = __builtin_fmaf(g[u][e], v[u][e], along);
+                        v[u][e] = x.live ? v[u][e] : 0.f;
+                        g[u][e] = x.live ? g[u][e] : 0.f;
                     }
-                    along = sum_lanes<G>(along) * a.inv_d;
-                    mean = a.layer ? sum_lanes<G>(mean) * a.inv_d : 0.f;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) g[u][e] = r * (g[u][e] - __builtin_fmaf(v[u][e], along, mean));
-                    if (row[u].live) store8<T, HALVES>(g[u], static_cast<T*>(q.dx.data) + row[u].entry * q.dx.batch + token * q.dx.token + row[u].head * q.dx.head, x.lo, x.hi);
-                }
             }
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const float r = normalise8<G, LAYER>(v[u], a, x.live);
+                rotate8<HALVES, true>(g[u], c, s);
+                float along = 0.f, mean = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    total[1][e] += g[u][e];
+                    total[0][e] = __builtin_fmaf(g[u][e], v[u][e], total[0][e]);
+                    g[u][e] *= gain[e];
+                    along = __builtin_fmaf(g[u][e], v[u][e], along);
+                    if constexpr (LAYER) mean += g[u][e];
+                }
+                along = sum_lanes<G>(along) * (a.inv_d * r);
+                if constexpr (LAYER) mean = sum_lanes<G>(mean) * (a.inv_d * r);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[u][e] = __builtin_fmaf(g[u][e], r, -__builtin_fmaf(v[u][e], along, mean));
+            }
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                if (token < a.n && row.step * q.slots + x.head < q.heads && x.live)
+                    Raw<T, HALVES>::store(g[u], static_cast<T*>(q.dx.data) + row.of(q, q.dx, token0) + own_dx, x.lo, x.hi);
+                row.next(q.steps);
+            }
+        };
+        for (int i = 0; i < here.rows; i += U) {
+            Input<T, HALVES, HELD> in_now[U];
+            Raw<T, HALVES> dy_now[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                in_now[u] = in[u];
+                dy_now[u] = dy[u];
+            }
+            if (i + U < here.rows) load(here, ahead, here.rows - i - U);
+            if (i + U <= here.rows) work(std::integral_constant<int, U>{}, in_now, dy_now);
+            else work(std::integral_constant<int, 1>{}, in_now, dy_now);
         }
     }
     // over the rows of the wave, then over the waves
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            float t = total[k / 2][k % 2][e];
+            float t = total[k][e];
 #pragma unroll
             for (int m = G; m < 64; m *= 2) t += __shfl_xor(t, m);
             if (threadIdx.x % 64 < G && x.live) sums[w][k][(e < 4 ? x.lo : x.hi - 4) + e] = t;
         }
     __syncthreads();
-    for (int i = threadIdx.x; i < 4 * a.d; i += 256) {
+    for (int i = threadIdx.x; i < 2 * a.d; i += 256) {
         const int k = i / a.d, e = i - k * a.d;
         const float t = sums[0][k][e] + sums[1][k][e] + (sums[2][k][e] + sums[3][k][e]);
-        if (gridDim.x == 1) {
-            float* to = k % 2 ? a.side[k / 2].dshift : a.side[k / 2].dgain;
+        if (q.groups == 1) {
+            float* to = k ? q.dshift : q.dgain;
             if (to) to[e] = t;
         } else {
-            a.part[(int64_t)blockIdx.x * 4 * a.d + i] = t;
+            a.part[(int64_t)blockIdx.x * 2 * a.d + i] = t;
         }
     }
 }
 
 // The weights' gradients from the work-groups' sums: a lane for each value, a wave for every 16th work-group.
-__global__ __launch_bounds__(1024) void k_norm_rotate_join(const NormArgs a, int groups) {
+__global__ __launch_bounds__(1024) void k_norm_rotate_join(const NormArgs a) {
     __shared__ double sums[16][64];
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, i = blockIdx.x * 64 + lane;
-    const int k = i / a.d, e = i - k * a.d;
-    float* to = k < 4 ? (k % 2 ? a.side[k / 2].dshift : a.side[k / 2].dgain) : nullptr;
+    const int side = i / (2 * a.d), k = i / a.d % 2, e = i % a.d;
+    float* to = side < 2 ? (k ? a.side[side].dshift : a.side[side].dgain) : nullptr;
     double sum = 0;
-    if (to)
+    if (to) {
+        const float* part = a.part + ((int64_t)(side ? a.side[0].groups : 0) * 2 + k) * a.d + e;
+        const int groups = a.side[side].groups;
+        if (groups == 1) to = nullptr;                      // (it has written its own)
 #pragma unroll 8
-        for (int g = wave; g < groups; g += 16) sum += a.part[(int64_t)g * 4 * a.d + i];
+        for (int g = wave; g < groups; g += 16) sum += part[(int64_t)g * 2 * a.d];
+    }
     sums[wave][lane] = sum;
     __syncthreads();
     if (wave || !to) return;
@@ -363,27 +498,48 @@ int pow2_from(int n, int most) {
     return p;
 }
 
-// Work-groups, and in a how the tokens, heads and entries lie on the waves.
-int64_t plan(NormArgs& a, bool backward) {
-    const int lanes = pow2_from(a.d / 8, 32), slots = 64 / lanes;
-    a.head_slots = pow2_from(std::max(a.side[0].heads, a.side[1].heads), slots);
-    for (NormSide& q : a.side) q.steps = (q.heads + a.head_slots - 1) / a.head_slots;
-    const int tokens = slots / a.head_slots;
-    a.tiles = (a.n + tokens - 1) / tokens;
-    const int64_t most = 4096;                                   // waves: 16 for each compute unit
-    a.chunk = a.positions_batch == 0 || a.rot == 0 ? std::max<int64_t>(1, std::min(a.batch, a.batch * a.tiles / (2 * most))) : 1;
-    a.chunks = (a.batch + a.chunk - 1) / a.chunk;
-    a.items = a.tiles * a.chunks;
-    const int64_t groups = std::min((a.items + 3) / 4, backward ? most / 4 : int64_t(1) << 20);
-    a.waves = groups * 4;
-    a.step_chunk = a.waves / a.tiles;
-    a.step_tile = a.waves % a.tiles;
-    return groups;
+// Lanes of a row: the next power of two of d / 8, and 4 for 8 and 16 channels too (heads that narrow are not worth kernels
+// of their own).
+int lanes_of(int d) { return d <= 32 ? 4 : pow2_from(d / 8, 32); }
+
+int64_t up(int64_t n, int64_t d) { return (n + d - 1) / d; }
+
+// Work-groups, and in a how the tokens, heads and entries lie on the waves.  A work-group has the queries or the keys.
+int64_t plan(NormArgs& a, int dtype, bool backward) {
+    const int rows = 64 / lanes_of(a.d);                        // of a wave at once
+    const bool shared = a.positions_batch == 0 || a.rot == 0;
+    int64_t work[2], total = 0;
+    for (int i = 0; i < 2; ++i) {
+        NormSide& q = a.side[i];
+        // An item should have at least four rows for its angles, which take as long as one: several entries, or, where
+        // each has its own positions, fewer heads at once (of 128 bytes at least) and several head steps.
+        const int least = shared ? rows : pow2_from((int)up(128, a.d * (dtype == 1 ? 2 : 4)), rows);
+        q.slots = pow2_from(shared ? q.heads : std::max((int)up(q.heads, 4), std::min(least, q.heads)), rows);
+        q.steps = (int)up(q.heads, q.slots);
+        q.tiles = up(a.n, rows / q.slots);
+        work[i] = a.batch * q.tiles * q.steps;
+        total += work[i];
+    }
+    // Waves that go round: 16 for each compute unit, 12 in the backward (what registers allow).  A forward whose entries have
+    // their own positions has short items, and a wave for each.
+    const int64_t waves = backward ? 3072 : 4096;
+    for (int i = 0; i < 2; ++i) {
+        NormSide& q = a.side[i];
+        q.chunk = shared && q.heads ? std::min(a.batch, up(std::max<int64_t>(4, total / (8 * waves)), q.steps)) : 1;
+        q.chunks = up(a.batch, q.chunk);
+        const int64_t groups = up(q.tiles * q.chunks, 4);
+        q.groups = q.heads ? (int)std::min(groups, backward || shared ? std::max<int64_t>(1, waves / 4 * work[i] / total) : int64_t(1) << 22) : 0;
+        if (q.heads) {
+            q.step_chunk = 4 * (int64_t)q.groups / q.tiles;
+            q.step_tile = 4 * (int64_t)q.groups % q.tiles;
+        }
+    }
+    return (int64_t)a.side[0].groups + a.side[1].groups;
 }
 
 }  // namespace
 
-int64_t norm_rotate_groups(NormArgs a, bool backward) { return plan(a, backward); }
+int64_t norm_rotate_backward_groups(NormArgs a, int dtype) { return plan(a, dtype, true); }
 
 hipError_t launch_norm_rotate(int dtype, bool adjacent, bool backward, NormArgs a, hipStream_t s) {
     if (a.batch == 0 || a.n == 0) {
@@ -391,31 +547,39 @@ hipError_t launch_norm_rotate(int dtype, bool adjacent, bool backward, NormArgs 
         hipLaunchKernelGGL(k_norm_rotate_zero, dim3(1), dim3(256), 0, s, a);
         return hipGetLastError();
     }
-    const int64_t groups = plan(a, backward);
+    const int64_t groups = plan(a, dtype, backward);
     a.inv_d = 1.f / (float)a.d;
-    auto go = [&](auto zero, auto lanes, auto halves) {
+    a.ragged = 8 * lanes_of(a.d) != a.d;
+    const bool held = backward && !a.side[a.side[0].heads ? 0 : 1].x.data;
+    const bool hold = a.side[0].codes || a.side[1].codes;
+    auto go = [&](auto zero, auto lanes, auto halves, auto layer) {
         using T = decltype(zero);
         constexpr int G = decltype(lanes)::value;
-        constexpr bool H = decltype(halves)::value;
-        if (backward) hipLaunchKernelGGL((k_norm_rotate_backward<T, G, H>), dim3((unsigned)groups), dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((k_norm_rotate<T, G, H>), dim3((unsigned)groups), dim3(256), 0, s, a);
+        constexpr bool H = decltype(halves)::value, L = decltype(layer)::value;
+        const dim3 grid((unsigned)groups), block(256);
+        if (backward) {
+            if (held) hipLaunchKernelGGL((k_norm_rotate_backward<T, G, H, L, true>), grid, block, 0, s, a);
+            else hipLaunchKernelGGL((k_norm_rotate_backward<T, G, H, L, false>), grid, block, 0, s, a);
+        } else {
+            if (hold) hipLaunchKernelGGL((k_norm_rotate<T, G, H, L, true>), grid, block, 0, s, a);
+            else hipLaunchKernelGGL((k_norm_rotate<T, G, H, L, false>), grid, block, 0, s, a);
+        }
         return hipGetLastError();
     };
     auto by_lanes = [&](auto zero, auto halves) {
-        switch (pow2_from(a.d / 8, 32)) {
-            case 1: return go(zero, std::integral_constant<int, 1>{}, halves);
-            case 2: return go(zero, std::integral_constant<int, 2>{}, halves);
-            case 4: return go(zero, std::integral_constant<int, 4>{}, halves);
-            case 8: return go(zero, std::integral_constant<int, 8>{}, halves);
-            case 16: return go(zero, std::integral_constant<int, 16>{}, halves);
-            default: return go(zero, std::integral_constant<int, 32>{}, halves);
+        auto by_norm = [&](auto lanes) { return a.layer ? go(zero, lanes, halves, std::true_type{}) : go(zero, lanes, halves, std::false_type{}); };
+        switch (lanes_of(a.d)) {
+            case 4: return by_norm(std::integral_constant<int, 4>{});
+            case 8: return by_norm(std::integral_constant<int, 8>{});
+            case 16: return by_norm(std::integral_constant<int, 16>{});
+            default: return by_norm(std::integral_constant<int, 32>{});
         }
     };
     const bool halves = !adjacent && a.rot > 0;
     const hipError_t e = dtype == 1 ? halves ? by_lanes(bf16_t{}, std::true_type{}) : by_lanes(bf16_t{}, std::false_type{})
                                     : halves ? by_lanes(float{}, std::true_type{}) : by_lanes(float{}, std::false_type{});
-    if (e != hipSuccess || !backward || groups == 1) return e;
-    hipLaunchKernelGGL(k_norm_rotate_join, dim3((unsigned)((4 * a.d + 63) / 64)), dim3(1024), 0, s, a, (int)groups);
+    if (e != hipSuccess || !backward || (a.side[0].groups < 2 && a.side[1].groups < 2)) return e;
+    hipLaunchKernelGGL(k_norm_rotate_join, dim3((unsigned)((4 * a.d + 63) / 64)), dim3(1024), 0, s, a);
     return hipGetLastError();
 }
 
