@@ -42,14 +42,18 @@ __global__ __launch_bounds__(256) void k_checkpoint_pack(const CheckpointArgs a,
     const int lane = threadIdx.x % G;
     const int64_t first = (int64_t)blockIdx.x * (kSlots * kCheckpointUnroll) + threadIdx.x / G;
     Place p[kCheckpointUnroll];
-    Vec<T, 8> v[kCheckpointUnroll];
+    Words<T, 8> w[kCheckpointUnroll];
 #pragma unroll
     for (int u = 0; u < kCheckpointUnroll; ++u) {
         p[u] = place<FLAT>(a, first + u * kSlots, lane);
-        load_some(v[u], x + p[u].x, p[u].n, a.wide);
+        w[u].clear();
+        if (a.wide && p[u].n >= 8) w[u].load(x + p[u].x);
+        else if (p[u].n > 0) w[u].load_some(x + p[u].x, p[u].n);
     }
+    Vec<T, 8> v[kCheckpointUnroll];
 #pragma unroll
     for (int u = 0; u < kCheckpointUnroll; ++u) {
+        v[u] = w[u].values();
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[u].f[i]) & 0x7fffffffu);

@@ -292,7 +292,7 @@ struct RelativeArgs {
     CrossBias base, out;      // out: dout in the backward
     float *dtable, *part;     // part: partial sums (workspace)
     uint32_t* masks;          // which of them are there; filled in by the launcher, as are the next
-    int wide;                 // vectors of eight fit the strides and pointers
+    int wide, wide_keys;      // vectors of eight fit the tensors, and the keys' positions and segments
     int hb, tx, cwidth, cblocks, hblocks, waves, splits;
     int64_t loop, rblocks, span;
 };

@@ -18,6 +18,13 @@ __device__ __forceinline__ int distance_index(int pk, int pq, int reach) {
     return min(max(__builtin_elementwise_sub_sat(pk, pq), -reach), reach) + reach;
 }
 
+// Work-groups go to the eight XCDs in turn; this gives each XCD neighbouring ones, so that lines which two of them share
+// (rows that are no multiple of 128 bytes) meet in one L2.
+__device__ __forceinline__ int64_t by_xcd(uint32_t group, uint32_t groups) {
+    const uint32_t per = groups / 8, rest = groups % 8, x = group % 8, i = group / 8;
+    return (int64_t)x * per + min(x, rest) + i;
+}
+
 // Lanes take eight neighbouring keys each, usually at eight neighbouring distances: with one place left free after
 // every eight, the lanes of a wave read different banks.
 __device__ __forceinline__ int skewed(int i) { return i + (i >> 3); }
@@ -29,148 +36,313 @@ __device__ __forceinline__ float table_value(const RelativeArgs& a, int row, int
 
 __device__ __forceinline__ int bucket_of(const RelativeArgs& a, int index) { return min((int)a.lut[index], a.buckets - 1); }
 
-// Positions (and segments) of eight keys from j on; those behind the last are 0.
-__device__ __forceinline__ void eight(const int32_t* p, int64_t j, int64_t n, int (&v)[8]) {
+// val[h * stride + skewed(i)]: what head h0 + h (h < nh of HB) adds at distance index i, and behind the last index what it
+// adds in another segment.  Look-ups that depend on each other, so several of them are under way at once.
+template <int HB>
+__device__ __forceinline__ void values_by_distance(const RelativeArgs& a, float* val, int h0, int nh, int entries, int stride, int threads) {
+    constexpr int U = 4;
+    for (int e0 = threadIdx.x; e0 < entries * HB; e0 += U * threads) {
+        int row[U];
+        float x[U];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = j + i < n ? p[j + i] : 0;
+        for (int u = 0; u < U; ++u) {
+            const int i = min((e0 + u * threads) / HB, entries - 1);
+            row[u] = i == entries - 1 ? a.buckets - 1 : bucket_of(a, i);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = table_value(a, row[u], h0 + min((e0 + u * threads) % HB, nh - 1));
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int e = e0 + u * threads;
+            if (e < entries * HB) val[e % HB * stride + skewed(e / HB)] = x[u];
+        }
+    }
 }
+
+__device__ __forceinline__ void lut_to_lds(const RelativeArgs& a, uint8_t* lut, int threads) {
+    for (int e = threadIdx.x; e <= 2 * a.reach; e += threads) lut[e] = (uint8_t)bucket_of(a, e);
+}
+__device__ __forceinline__ void zero_lds(float* p, int n, int threads) {      // n a multiple of 4
+    for (int e = 4 * threadIdx.x; e < n; e += 4 * threads) *reinterpret_cast<float4*>(p + e) = make_float4(0.f, 0.f, 0.f, 0.f);
+}
+
+// Eight integers of which the first n exist (the last stands for the rest); wide: p is 16-byte aligned.
+__device__ __forceinline__ void eight(const int32_t* p, int n, bool wide, int (&v)[8]) {
+    if (wide && n >= 8) {
+        const int4 x = reinterpret_cast<const int4*>(p)[0], y = reinterpret_cast<const int4*>(p)[1];
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+        v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = p[min(i, n - 1)];
+    }
+}
+
+// A lane's eight keys: the first of them, and how many exist (0: the lane is past the end, and is given the first keys to
+// look at).  whole: every lane of the wave has eight or none, which a vector load can take.
+struct KeyPlace {
+    int64_t j;
+    int n;
+    bool whole;
+    __device__ __forceinline__ KeyPlace(const RelativeArgs& a, int64_t chunk) {
+        const int64_t left = a.nk - 8 * chunk;
+        j = left > 0 ? 8 * chunk : 0;
+        n = left >= 8 ? 8 : left > 0 ? (int)left : 0;
+        whole = a.wide && a.nk >= 8 && __ballot(n > 0 && n < 8) == 0;
+    }
+};
+
+// Eight neighbouring keys (n of them exist, the last stands for the rest): positions, segments, and whether all have one
+// distance index to a query.  The index does not fall as the position rises, so the first and the last decide.
+template <bool SEG> struct Keys {
+    int pos[8], seg[8], least, most;
+    bool alike;       // one segment
+    __device__ __forceinline__ Keys(const RelativeArgs& a, int64_t b, int64_t j, int n) {
+        eight(a.pos_k + b * a.pos_k_batch + j, n, a.wide_keys, pos);
+        if constexpr (SEG) eight(a.seg_k + b * a.seg_k_batch + j, n, a.wide_keys, seg);
+        least = most = pos[0];
+        alike = true;
+#pragma unroll
+        for (int i = 1; i < 8; ++i) {
+            least = min(least, pos[i]);
+            most = max(most, pos[i]);
+            if constexpr (SEG) alike = alike && seg[i] == seg[0];
+        }
+    }
+    // The index that all eight have, other where the segments differ; -1 if there is none.
+    __device__ __forceinline__ int common(int pq, int sq, int reach, int other) const {
+        const int i = distance_index(least, pq, reach);
+        if constexpr (SEG) {
+            bool any = seg[0] == sq;
+            if (!alike)
+#pragma unroll
+                for (int e = 1; e < 8; ++e) any = any || seg[e] == sq;
+            if (!any) return other;
+            if (!alike) return -1;
+        }
+        return i == distance_index(most, pq, reach) ? i : -1;
+    }
+    __device__ __forceinline__ int index(int i, int pq, int sq, int reach, int other) const {
+        return SEG && seg[i] != sq ? other : distance_index(pos[i], pq, reach);
+    }
+};
 
 // ---------------------------------------------------------------- bias [batch][heads][nq][nk]
 
-// A work-group: `hb` heads, a.tx threads along the keys (eight each), 256 / a.tx rows at a time, a.loop times.
-template <typename T, bool SEG, bool BASE>
+// A work-group: HB heads, a.tx threads along the keys (eight each), 256 / a.tx rows at a time, a.loop times.  Where all
+// lanes of a wave have keys of one distance index each, as away from the diagonal, a head is one look-up.
+template <typename T, bool SEG, bool BASE, int HB>
 __global__ __launch_bounds__(256) void k_relative_bias(const RelativeArgs a) {
     extern __shared__ float val[];
-    int64_t at = blockIdx.x;
+    int64_t at = by_xcd(blockIdx.x, gridDim.x);
     const int cb = (int)(at % a.cblocks);
     at /= a.cblocks;
     const int rb = (int)(at % a.rblocks);
     at /= a.rblocks;
     const int hg = (int)(at % a.hblocks);
     const int64_t b = at / a.hblocks;
-    const int h0 = hg * a.hb, nh = min(a.hb, a.heads - h0);
-    const int entries = 2 * a.reach + 2, stride = skewed(entries) + 1;      // the last entry: another segment
-    for (int e = threadIdx.x; e < entries * a.hb; e += 256) {
-        const int i = e / a.hb, h = e - i * a.hb;                           // (hb is a power of two)
-        if (h < nh) val[h * stride + skewed(i)] = table_value(a, i == entries - 1 ? a.buckets - 1 : bucket_of(a, i), h0 + h);
-    }
-    __syncthreads();
+    const int h0 = hg * HB, nh = min(HB, a.heads - h0);
+    const int other = 2 * a.reach + 1, stride = skewed(other + 1) + 1;
+    values_by_distance<HB>(a, val, h0, nh, other + 1, stride, 256);
     const int tx = threadIdx.x & (a.tx - 1), ty = threadIdx.x / a.tx, rows = 256 / a.tx;
-    const int64_t j = ((int64_t)cb * a.tx + tx) * 8;
-    const int n = (int)min((int64_t)8, a.nk - j);
-    if (n <= 0) return;
-    int pk[8], sk[8];
-    eight(a.pos_k + b * a.pos_k_batch, j, a.nk, pk);
-    if constexpr (SEG) eight(a.seg_k + b * a.seg_k_batch, j, a.nk, sk);
+    const KeyPlace at_keys(a, (int64_t)cb * a.tx + tx);
+    const int64_t j = at_keys.j;
+    const int n = at_keys.n;
+    const bool whole = at_keys.whole;
+    const Keys<SEG> keys(a, b, j, max(n, 1));
+    __syncthreads();
     const T* base = static_cast<const T*>(a.base.data) + b * a.base.batch + h0 * a.base.head + j;
     T* out = static_cast<T*>(a.out.data) + b * a.out.batch + h0 * a.out.head + j;
     const int64_t r0 = (int64_t)rb * rows * a.loop, r1 = min(r0 + (int64_t)rows * a.loop, a.nq);
+    constexpr int N = HB < 4 ? HB : 4;                  // heads at once
     for (int64_t r = r0 + ty; r < r1; r += rows) {
-        const int pq = a.pos_q[b * a.pos_q_batch + r];
+        const int pq = a.pos_q[b * a.pos_q_batch + r], sq = SEG ? a.seg_q[b * a.seg_q_batch + r] : 0;
+        const T* from = base + r * a.base.row;
+        T* to = out + r * a.out.row;
+        const int common = keys.common(pq, sq, a.reach, other);
         int idx[8];
+        const bool one = __ballot(common < 0) == 0;
+        idx[0] = skewed(common);
+        if (!one)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) idx[i] = distance_index(pk[i], pq, a.reach);
-        if constexpr (SEG) {
-            const int sq = a.seg_q[b * a.seg_q_batch + r];
+            for (int i = 0; i < 8; ++i) idx[i] = skewed(keys.index(i, pq, sq, a.reach, other));
+        for (int h = 0; h < nh; h += N) {
+            Vec<T, 8> v[N];
+            if constexpr (BASE) {
+                Words<T, 8> w[N];
+                if (whole)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) idx[i] = sk[i] == sq ? idx[i] : entries - 1;
-        }
+                    for (int u = 0; u < N; ++u) w[u].load(from + min(h + u, nh - 1) * a.base.head);
+                else
 #pragma unroll
-        for (int i = 0; i < 8; ++i) idx[i] = skewed(idx[i]);
-        for (int h = 0; h < nh; h += 4) {
-            Vec<T, 8> v[4];
+                    for (int u = 0; u < N; ++u) w[u].load_some(from + min(h + u, nh - 1) * a.base.head, n);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (h + u >= nh) break;
-                if constexpr (BASE) load_some(v[u], base + (h + u) * a.base.head + r * a.base.row, n, a.wide);
+                for (int u = 0; u < N; ++u) v[u] = w[u].values();
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (h + u >= nh) break;
-                const float* t = val + (h + u) * stride;
+            for (int u = 0; u < N; ++u) {
+                const float* t = val + min(h + u, nh - 1) * stride;
+                if (one) {
+                    const float x = t[idx[0]];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[u].f[i] = BASE ? v[u].f[i] + t[idx[i]] : t[idx[i]];
-                store_some(v[u], out + (h + u) * a.out.head + r * a.out.row, n, a.wide);
+                    for (int i = 0; i < 8; ++i) v[u].f[i] = BASE ? v[u].f[i] + x : x;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[u].f[i] = BASE ? v[u].f[i] + t[idx[i]] : t[idx[i]];
+                }
             }
+#pragma unroll
+            for (int u = 0; u < N; ++u)
+                if (h + u < nh) store_some(v[u], to + (h + u) * a.out.head, n, a.wide);
         }
     }
 }
 
-// A work-group: one head of one entry, rows [split's share) on a.waves waves; 64 columns of LDS for each wave and bucket.
+// A work-group: one head of one entry, the rows of one split; a wave: a.span times the keys of its lanes.  A lane has a column of LDS
+// for itself, a place for each bucket and one for what is not to be kept.
+//   Away from the diagonal a lane's eight keys have one distance index: their sum stays in a register while its bucket
+//   does not change.  Near it a lane's buckets usually rise or fall: equal neighbours are added up, and the eight
+//   places, all different then, are read, added to and written together.  Otherwise one after the other.
 template <typename T, bool SEG>
 __global__ __launch_bounds__(256) void k_relative_bias_backward(const RelativeArgs a) {
     extern __shared__ float val[];
-    uint8_t* lut = reinterpret_cast<uint8_t*>(val + (size_t)a.waves * a.buckets * 64);
+    constexpr int U = 4;
+    const int columns = (a.buckets + 1) * 64;
+    uint8_t* lut = reinterpret_cast<uint8_t*>(val + (size_t)a.waves * columns);
     int64_t at = blockIdx.x;
+    const int group = (int)(at % a.cblocks);
+    at /= a.cblocks;
     const int split = (int)(at % a.splits);
     at /= a.splits;
     const int h = (int)(at % a.heads);
     const int64_t b = at / a.heads;
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, threads = a.waves * 64;
-    for (int e = threadIdx.x; e <= 2 * a.reach; e += threads) lut[e] = (uint8_t)bucket_of(a, e);
-    for (int e = threadIdx.x; e < a.waves * a.buckets * 64; e += threads) val[e] = 0.f;
+    const int other = 2 * a.reach + 1;                   // (its place in lut holds the last bucket)
+    lut_to_lds(a, lut, threads);
+    if (threadIdx.x == 0) lut[other] = (uint8_t)(a.buckets - 1);
+    zero_lds(val, a.waves * columns, threads);
     __syncthreads();
-    float* acc = val + wave * a.buckets * 64 + lane;
-    const int tx = lane & (a.tx - 1), ty = lane / a.tx, rows = 64 / a.tx, step = a.waves * rows;
+    float* acc = val + wave * columns + lane;
+    const int tx = lane & (a.tx - 1), ty = lane / a.tx, rows = 64 / a.tx;
     const int64_t per = (a.nq + a.splits - 1) / a.splits, r0 = split * per, r1 = min(r0 + per, a.nq);
     const T* from = static_cast<const T*>(a.out.data) + b * a.out.batch + h * a.out.head;
     const int32_t* pos_q = a.pos_q + b * a.pos_q_batch;
     const int32_t* seg_q = SEG ? a.seg_q + b * a.seg_q_batch : nullptr;
-    for (int64_t j = (int64_t)tx * 8; j < a.nk; j += (int64_t)a.tx * 8) {
-        const int n = (int)min((int64_t)8, a.nk - j);
-        int pk[8], sk[8];
-        eight(a.pos_k + b * a.pos_k_batch, j, a.nk, pk);
-        if constexpr (SEG) eight(a.seg_k + b * a.seg_k_batch, j, a.nk, sk);
-        auto add = [&](const Vec<T, 8>& v, int pq, int sq) {
+    int cur = a.buckets;                                 // the bucket of `sum` (at first: none)
+    float sum = 0.f;
+    for (int k = 0; k < a.span; ++k) {
+        const int64_t c = ((int64_t)group * a.waves + wave) * a.span + k;
+        if (c * a.tx * 8 >= a.nk) break;
+        const KeyPlace at_keys(a, c * a.tx + tx);
+        const int64_t j = at_keys.j;
+        const int n = at_keys.n;
+        const Keys<SEG> keys(a, b, j, max(n, 1));
+        Words<T, 8> ahead[U];
+        int pq_ahead[U], sq_ahead[U];
+        auto load = [&](int64_t first) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                int t = lut[distance_index(pk[i], pq, a.reach)];
-                if constexpr (SEG) t = sk[i] == sq ? t : a.buckets - 1;
-                atomicAdd(acc + t * 64, v.f[i]);        // (this lane's own: ds_add_f32 in the order of the program)
+            for (int u = 0; u < U; ++u) {
+                const int64_t r = min(first + ty + u * rows, r1 - 1);
+                if (at_keys.whole) ahead[u].load(from + r * a.out.row + j);
+                else ahead[u].load_some(from + r * a.out.row + j, n);
+                pq_ahead[u] = pos_q[r];
+                sq_ahead[u] = SEG ? seg_q[r] : 0;
             }
         };
-        int64_t r = r0 + wave * rows + ty;
-        for (; r + 3 * step < r1; r += 4 * step) {
-            Vec<T, 8> v[4];
-            int pq[4], sq[4];
+        if (r0 < r1) load(r0);
+        for (int64_t first = r0; first < r1; first += U * rows) {
+            Vec<T, 8> v[U];
+            int pq[U], sq[U], common[U];
+            const bool some = __ballot(n == 0) != 0 || first + U * rows > r1;       // lanes or rows that count for nothing
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                load_some(v[u], from + (r + u * step) * a.out.row + j, n, a.wide);
-                pq[u] = pos_q[r + u * step];
-                sq[u] = SEG ? seg_q[r + u * step] : 0;
+            for (int u = 0; u < U; ++u) {
+                v[u] = ahead[u].values();
+                if (some)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[u].f[i] = n > 0 && first + ty + u * rows < r1 ? v[u].f[i] : 0.f;
+                pq[u] = pq_ahead[u];
+                sq[u] = sq_ahead[u];
             }
+            if (first + U * rows < r1) load(first + U * rows);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) add(v[u], pq[u], sq[u]);
-        }
-        for (; r < r1; r += step) {
-            Vec<T, 8> v;
-            load_some(v, from + r * a.out.row + j, n, a.wide);
-            add(v, pos_q[r], SEG ? seg_q[r] : 0);
+            for (int u = 0; u < U; ++u) common[u] = keys.common(pq[u], sq[u], a.reach, other);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float* f = v[u].f;
+                if (__ballot(common[u] < 0) == 0) {
+                    const int t = lut[common[u]];
+                    const float x = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+                    if (__ballot(t != cur) == 0) {
+                        sum += x;
+                    } else {
+                        acc[cur * 64] += sum;
+                        cur = t;
+                        sum = x;
+                    }
+                    continue;
+                }
+                int t[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[i] = lut[keys.index(i, pq[u], sq[u], a.reach, other)];
+                bool rises = true, falls = true;
+#pragma unroll
+                for (int i = 1; i < 8; ++i) {
+                    rises = rises && t[i] >= t[i - 1];
+                    falls = falls && t[i] <= t[i - 1];
+                }
+                if (__ballot(!(rises || falls)) == 0) {
+                    float x[8], old[8];
+                    int to[8];
+                    x[0] = f[0];
+#pragma unroll
+                    for (int i = 1; i < 8; ++i) x[i] = t[i] == t[i - 1] ? x[i - 1] + f[i] : f[i];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) to[i] = (i < 7 && t[i] == t[(i + 1) & 7] ? a.buckets : t[i]) * 64;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) old[i] = acc[to[i]];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[to[i]] = old[i] + x[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[t[i] * 64] += f[i];
+                }
+            }
         }
     }
+    acc[cur * 64] += sum;
     __syncthreads();
-    for (int t = threadIdx.x; t < a.buckets; t += threads) {
+    // a bucket's columns: eight lanes, each eight columns of every wave, in an order that keeps the banks apart
+    for (int e = threadIdx.x; e < (a.buckets + 7) / 8 * 64; e += threads) {
+        const int t = e / 8, part = e % 8;
         double sum = 0;
-        for (int w = 0; w < a.waves; ++w)
-            for (int i = 0; i < 64; ++i) sum += val[(w * a.buckets + t) * 64 + ((i + t) & 63)];   // (each thread at a bank of its own)
-        if (a.batch * a.splits == 1) a.dtable[(int64_t)t * a.heads + h] = (float)sum;
-        else a.part[((b * a.splits + split) * a.heads + h) * a.buckets + t] = (float)sum;
+        if (t < a.buckets)
+            for (int w = 0; w < a.waves; ++w)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += val[w * columns + t * 64 + part * 8 + ((i + t) & 7)];
+#pragma unroll
+        for (int m = 1; m < 8; m *= 2) sum += __shfl_xor(sum, m);
+        if (t < a.buckets && part == 0) {
+            if (a.batch * a.splits * a.cblocks == 1) a.dtable[(int64_t)t * a.heads + h] = (float)sum;
+            else a.part[(((b * a.splits + split) * a.cblocks + group) * a.heads + h) * a.buckets + t] = (float)sum;
+        }
     }
 }
 
-// dtable from `slots` partial tables [heads][buckets]: a lane for each value, a wave for every fourth slot.
-__global__ __launch_bounds__(256) void k_relative_join(const RelativeArgs a, int64_t slots) {
-    __shared__ double sums[4][64];
+// dtable from `slots` partial tables [heads][buckets]: a lane for each value, a wave for every 16th slot.
+__global__ __launch_bounds__(1024) void k_relative_join(const RelativeArgs a, int64_t slots) {
+    __shared__ double sums[16][64];
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, n = a.heads * a.buckets;
     const int e = blockIdx.x * 64 + lane;
     double sum = 0;
     if (e < n)
-        for (int64_t s = wave; s < slots; s += 4) sum += a.part[s * n + e];
+#pragma unroll 8
+        for (int64_t s = wave; s < slots; s += 16) sum += a.part[s * n + e];
     sums[wave][lane] = sum;
     __syncthreads();
     if (wave == 0 && e < n) {
+        for (int w = 1; w < 16; ++w) sum += sums[w][lane];
         const int h = e / a.buckets, t = e - h * a.buckets;
-        a.dtable[(int64_t)t * a.heads + h] = (float)(sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane]);
+        a.dtable[(int64_t)t * a.heads + h] = (float)sum;
     }
 }
 
@@ -193,11 +365,12 @@ __global__ __launch_bounds__(256) void k_relative_pair(const RelativeArgs a) {
     const int cb = (int)(at % a.hblocks);
     const int64_t rb = at / a.hblocks;
     const int c0 = cb * a.cwidth, nc = min(a.cwidth, a.heads - c0);
+#pragma unroll 8
     for (int e = threadIdx.x; e < a.buckets * width; e += 256) {
-        const int t = e / width, c = e - t * width;
-        val[e] = c < nc ? table_value(a, t, c0 + c) : 0.f;
+        const int t = e / width, c = e & (width - 1);                   // (width is a power of two)
+        val[e] = table_value(a, t, c0 + min(c, nc - 1));
     }
-    for (int e = threadIdx.x; e <= 2 * a.reach; e += 256) lut[e] = (uint8_t)bucket_of(a, e);
+    lut_to_lds(a, lut, 256);
     __syncthreads();
     const int lane = threadIdx.x & (a.tx - 1), pair = threadIdx.x / a.tx, pairs = 256 / a.tx;
     if (lane * V >= nc) return;
@@ -214,13 +387,10 @@ __global__ __launch_bounds__(256) void k_relative_pair(const RelativeArgs a) {
     T* out = static_cast<T*>(a.out.data) + c0 + lane * V;
     for (int64_t r = r0; r < r1; ++r) {
         const int pq = a.pos_q[r], sq = SEG ? a.seg_q[r] : 0;
-        Vec<T, V> v[4];
+        Words<T, V> x[4];
+        if constexpr (BASE)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int64_t j = j0 + u * pairs;
-            if constexpr (BASE)
-                if (j < a.nk) v[u].load(base + r * a.base.row + j * a.heads);
-        }
+            for (int u = 0; u < 4; ++u) x[u].load(base + r * a.base.row + min(j0 + u * pairs, a.nk - 1) * a.heads);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int64_t j = j0 + u * pairs;
@@ -228,16 +398,18 @@ __global__ __launch_bounds__(256) void k_relative_pair(const RelativeArgs a) {
             if constexpr (SEG) t = sk[u] == sq ? t : a.buckets - 1;
             Vec<float, V> w;
             w.load(val + t * width + lane * V);
+            Vec<T, V> v;
+            if constexpr (BASE) v = x[u].values();
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[u].f[i] = BASE ? v[u].f[i] + w.f[i] : w.f[i];
-            if (j < a.nk) v[u].store(out + r * a.out.row + j * a.heads);
+            for (int i = 0; i < V; ++i) v.f[i] = BASE ? v.f[i] + w.f[i] : w.f[i];
+            if (j < a.nk) v.store(out + r * a.out.row + j * a.heads);
         }
     }
 }
 
 // Sums by bucket over a tile of pairs.  A wave takes one pair at a time (a lane for V of its channels), so the bucket is
 // one for the wave: the sum stays in registers while it does not change, and goes to the wave's own table in LDS
-// when it does.
+// when it does.  16 pairs are on their way while 16 are added.
 template <typename T, int V, bool SEG>
 __global__ __launch_bounds__(256) void k_relative_pair_backward(const RelativeArgs a) {
     extern __shared__ float val[];
@@ -251,44 +423,84 @@ __global__ __launch_bounds__(256) void k_relative_pair_backward(const RelativeAr
     const int64_t tile = at;
     const int64_t r0 = tile / a.cblocks * a.loop, j0 = tile % a.cblocks * a.span;
     const int64_t r1 = min(r0 + a.loop, a.nq), j1 = min(j0 + a.span, a.nk);
-    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, threads = a.waves * 64;
-    for (int e = threadIdx.x; e <= 2 * a.reach; e += threads) lut[e] = (uint8_t)bucket_of(a, e);
-    for (int e = threadIdx.x; e < a.waves * table; e += threads) val[e] = 0.f;
-    if (threadIdx.x < 8) touched[threadIdx.x] = 0;
-    __syncthreads();
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, threads = a.waves * 64;
     const int c0 = cb * 64 * V + lane * V;
     const bool live = c0 < a.heads;                    // (V = 2 only where the channels are even)
-    float* acc = val + (size_t)wave * table + lane;
+    const int per_row = (int)((j1 - j0 + kAhead - 1) / kAhead), steps = (int)(r1 - r0) * per_row;
+    const T* from = static_cast<const T*>(a.out.data) + (live ? c0 : 0);
+    Words<T, V> ahead[kAhead];
+    int index = 0;                                     // of pair (lane % kAhead) of the pairs ahead; beyond reach: other segment
+    auto load = [&](int g) {
+        const int64_t r = r0 + g / per_row, j = j0 + (int64_t)(g % per_row) * kAhead;
+        const T* row = from + r * a.out.row;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) ahead[u].load(row + min(j + u, j1 - 1) * a.heads);
+        const int64_t mine = min(j + (lane & (kAhead - 1)), j1 - 1);
+        index = distance_index(a.pos_k[mine], a.pos_q[r], a.reach);
+        if constexpr (SEG) index = a.seg_k[mine] == a.seg_q[r] ? index : 2 * a.reach + 1;
+    };
+    if (wave < steps) load(wave);
+    lut_to_lds(a, lut, threads);
+    if (threadIdx.x == 0) lut[2 * a.reach + 1] = (uint8_t)(a.buckets - 1);
+    zero_lds(val, a.waves * table, threads);
+    if (threadIdx.x < 8) touched[threadIdx.x] = 0;
+    __syncthreads();
+    float* acc = val + (size_t)wave * table + lane * V;
     float sum[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) sum[i] = 0.f;
-    int cur = -1;
-    auto flush = [&]() {
-        if (cur < 0) return;
+    // `sum` belongs to bucket cur; what left the registers before it is on its way to bucket late: the old value has been
+    // asked for, and is added to when the next one leaves.
+    int cur = -1, late = -1;
+    Vec<float, V> old;
+    float due[V];
+    auto settle = [&]() {
+        if (late < 0) return;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            atomicAdd(acc + (cur * V + i) * 64, sum[i]);
-            sum[i] = 0.f;
-        }
-        if (lane == 0) atomicOr(touched + cur / 32, 1u << (cur & 31));
+        for (int i = 0; i < V; ++i) old.f[i] += due[i];
+        old.store(acc + late * 64 * V);
+        late = -1;
     };
     auto turn_to = [&](int t) {
         if (t == cur) return;
-        flush();
+        settle();
+        if (cur >= 0) {
+            old.load(acc + cur * 64 * V);
+#pragma unroll
+            for (int i = 0; i < V; ++i) due[i] = sum[i];
+            late = cur;
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[i] = 0.f;
         cur = t;
     };
-    const int per_row = (int)((j1 - j0 + kAhead - 1) / kAhead), steps = (int)(r1 - r0) * per_row;
     for (int g = wave; g < steps; g += a.waves) {
-        const int64_t r = r0 + g / per_row, j = j0 + g % per_row * kAhead;
-        const T* from = static_cast<const T*>(a.out.data) + r * a.out.row + (live ? c0 : 0);
+        const int left = (int)min((int64_t)kAhead, j1 - j0 - (int64_t)(g % per_row) * kAhead);
         Vec<T, V> v[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) v[u].load(from + min(j + u, j1 - 1) * a.heads);
-        const int64_t mine = min(j + (lane & (kAhead - 1)), j1 - 1);
-        int t = lut[distance_index(a.pos_k[mine], a.pos_q[r], a.reach)];
-        if constexpr (SEG) t = a.seg_k[mine] == a.seg_q[r] ? t : a.buckets - 1;
-        const int first = __builtin_amdgcn_readfirstlane(t);
-        if (j + kAhead <= j1 && __ballot(t != first) == 0) {       // one bucket for all of them: a tree
+        for (int u = 0; u < kAhead; ++u) v[u] = ahead[u].values();
+        const int t = lut[index], first = __builtin_amdgcn_readfirstlane(t);
+        if (g + a.waves < steps) load(g + a.waves);
+        if (lane < left) atomicOr(touched + t / 32, 1u << (t & 31));
+        const int before = __builtin_amdgcn_update_dpp(t, t, 0x111, 0xf, 0xf, false);          // row_shr 1: the pair before
+        const uint64_t inner = 0xfffe;                                                             // lanes 1..15
+        if (left == kAhead && ((__ballot(t > before) & inner) == inner || (__ballot(t < before) & inner) == inner)) {
+            turn_to(-1);                                           // all different: read, add and write them together
+            settle();
+            Vec<float, V> x[kAhead];
+            int to[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                to[u] = __builtin_amdgcn_readlane(t, u) * 64 * V;
+                x[u].load(acc + to[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[u].f[i] += v[u].f[i];
+                x[u].store(acc + to[u]);
+            }
+        } else if (left == kAhead && __ballot(t != first) == 0) {  // one bucket for all of them: a tree
             turn_to(first);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -301,7 +513,7 @@ __global__ __launch_bounds__(256) void k_relative_pair_backward(const RelativeAr
         } else {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                if (j + u < j1) {
+                if (u < left) {
                     turn_to(__builtin_amdgcn_readlane(t, u));
 #pragma unroll
                     for (int i = 0; i < V; ++i) sum[i] += v[u].f[i];
@@ -309,10 +521,12 @@ __global__ __launch_bounds__(256) void k_relative_pair_backward(const RelativeAr
             }
         }
     }
-    flush();
+    turn_to(-1);
+    settle();
     __syncthreads();
     const int64_t slot = tile * a.hblocks + cb;
     float* part = a.part + slot * table;
+#pragma unroll 4
     for (int e = threadIdx.x; e < table; e += threads) {
         const int t = e / (64 * V);
         if (!(touched[t / 32] >> (t & 31) & 1)) continue;
@@ -336,21 +550,29 @@ __global__ __launch_bounds__(1024) void k_relative_pair_join(const RelativeArgs 
         const int64_t mine = first + 16 * lane;
         const bool set = mine < tiles && (a.masks[(mine * a.hblocks + cb) * 8 + t / 32] >> (t & 31) & 1);
         uint64_t left = __ballot(set);
-        while (left) {
-            const int k = __ffsll((unsigned long long)left) - 1;
-            left &= left - 1;
-            const float* part = a.part + ((first + 16 * k) * a.hblocks + cb) * table + t * 64 * V + lane;
+        while (left) {                                 // four tiles at a time
+            float x[4][V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum[i] += part[64 * i];
+            for (int u = 0; u < 4; ++u) {
+                const int k = left ? __ffsll((unsigned long long)left) - 1 : 0;
+                const float* part = a.part + ((first + 16 * k) * a.hblocks + cb) * table + (t * 64 + lane) * V;
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[u][i] = left ? part[i] : 0.f;
+                left &= left - 1;
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[i] += x[u][i];
         }
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) sums[wave][64 * i + lane] = sum[i];
+    for (int i = 0; i < V; ++i) sums[wave][lane * V + i] = sum[i];
     __syncthreads();
     for (int e = threadIdx.x; e < 64 * V; e += 1024) {
         double s = 0;
         for (int w = 0; w < 16; ++w) s += sums[w][e];
-        const int c = cb * 64 * V + (e % 64) * V + e / 64;
+        const int c = cb * 64 * V + e;
         if (c < a.heads) a.dtable[(int64_t)t * a.heads + c] = (float)s;
     }
 }
@@ -367,7 +589,11 @@ bool strides_wide(const CrossBias& t, int64_t batch, int64_t heads, int64_t nq) 
     return !t.data || ((reinterpret_cast<uintptr_t>(t.data) & 15) == 0 && (batch == 1 || t.batch % 8 == 0) && (heads == 1 || t.head % 8 == 0) && (nq == 1 || t.row % 8 == 0));
 }
 
-size_t lut_bytes(int reach) { return ((size_t)2 * reach + 1 + 15) & ~size_t(15); }
+bool keys_wide(const RelativeArgs& a) {
+    return ((reinterpret_cast<uintptr_t>(a.pos_k) | reinterpret_cast<uintptr_t>(a.seg_k)) & 15) == 0 && ((a.pos_k_batch | a.seg_k_batch) & 3) == 0;
+}
+
+size_t lut_bytes(int reach) { return ((size_t)2 * reach + 2 + 15) & ~size_t(15); }
 
 template <typename K>
 hipError_t with_lds(K kernel, size_t lds) {
@@ -376,16 +602,25 @@ hipError_t with_lds(K kernel, size_t lds) {
 
 }  // namespace
 
+namespace {
+size_t values_bytes(const RelativeArgs& a) {            // of one head: values_by_distance
+    const size_t entries = 2 * (size_t)a.reach + 2;
+    return (entries + entries / 8 + 1) * 4;
+}
+}  // namespace
+
 int64_t relative_bias_plan(RelativeArgs& a) {
-    a.tx = pow2_from(up(a.nk, 8), 256);
+    a.tx = pow2_from(up(a.nk, 8), 16);
     const int rows = 256 / a.tx;
-    const size_t entries = 2 * (size_t)a.reach + 2, per_head = (entries + entries / 8 + 1) * 4;
-    a.hb = pow2_from(a.heads, 8);
-    while (a.hb > 1 && a.hb * per_head > 40960) a.hb /= 2;
+    // Heads at once: without a base eight share an index (1300 x 1300, 16 heads, bf16: 17.9 us; two at once 20.0).  With one,
+    // two: each head is two streams, and heads are often as far apart as memory channels repeat (2048 x 3000, 16 heads: 96
+    // us; four at once 129, one 96).
+    a.hb = pow2_from(a.heads, a.base.data ? 2 : 8);
+    while (a.hb > 1 && a.hb * values_bytes(a) > 40960) a.hb /= 2;
     a.cblocks = (int)up(a.nk, 8 * a.tx);
     auto groups = [&]() { return a.batch * up(a.heads, a.hb) * a.cblocks * up(a.nq, rows); };
     while (a.hb > 1 && groups() < 512) a.hb /= 2;
-    a.loop = std::min<int64_t>(16, std::max<int64_t>(1, groups() / 2048));
+    a.loop = std::min<int64_t>(64, up(groups(), a.base.data ? 1024 : 512));   // (1024 and 512 work-groups, which begin by filling LDS)
     a.hblocks = (int)up(a.heads, a.hb);
     a.rblocks = up(a.nq, rows * a.loop);
     return a.batch * a.hblocks * a.cblocks * a.rblocks;
@@ -393,32 +628,50 @@ int64_t relative_bias_plan(RelativeArgs& a) {
 
 hipError_t launch_relative_bias(int dtype, RelativeArgs a, hipStream_t s) {
     const int64_t groups = relative_bias_plan(a);
+    a.wide_keys = keys_wide(a);
     a.wide = strides_wide(a.base, a.batch, a.heads, a.nq) && strides_wide(a.out, a.batch, a.heads, a.nq);
-    const size_t entries = 2 * (size_t)a.reach + 2, lds = (entries + entries / 8 + 1) * 4 * a.hb;
+    const size_t lds = values_bytes(a) * a.hb;
     const dim3 grid((unsigned)groups), block(256);
+    const bool seg = a.seg_q, base = a.base.data;
     auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, grid, block, lds, s, a);
         return hipGetLastError();
     };
-    const bool seg = a.seg_q, base = a.base.data;
-    if (dtype == 1) return seg ? base ? go(k_relative_bias<bf16_t, true, true>) : go(k_relative_bias<bf16_t, true, false>)
-                               : base ? go(k_relative_bias<bf16_t, false, true>) : go(k_relative_bias<bf16_t, false, false>);
-    return seg ? base ? go(k_relative_bias<float, true, true>) : go(k_relative_bias<float, true, false>)
-               : base ? go(k_relative_bias<float, false, true>) : go(k_relative_bias<float, false, false>);
+    auto pick = [&](auto zero, auto heads) {
+        using T = decltype(zero);
+        constexpr int HB = decltype(heads)::value;
+        return seg ? base ? go(k_relative_bias<T, true, true, HB>) : go(k_relative_bias<T, true, false, HB>)
+                   : base ? go(k_relative_bias<T, false, true, HB>) : go(k_relative_bias<T, false, false, HB>);
+    };
+    auto by_heads = [&](auto zero) {
+        switch (a.hb) {
+            case 1: return pick(zero, std::integral_constant<int, 1>{});
+            case 2: return pick(zero, std::integral_constant<int, 2>{});
+            case 4: return pick(zero, std::integral_constant<int, 4>{});
+            default: return pick(zero, std::integral_constant<int, 8>{});
+        }
+    };
+    return dtype == 1 ? by_heads(bf16_t{}) : by_heads(float{});
 }
 
-// Work-groups, and in a the split of the rows and the waves of each: as many as 128 KB of columns allow.
+// Work-groups, and in a how rows and keys lie on their waves: two (one where their columns would outgrow 64 KB).  About
+// 2048 waves in all, eight for each compute unit, which is what LDS holds of 66 buckets; the rows of a wave are split
+// where its keys are too few to fill them, and are 128 at least.
 int64_t relative_bias_backward_plan(RelativeArgs& a) {
-    a.tx = pow2_from(up(a.nk, 8), 64);
-    a.waves = std::min(4, std::max(1, 131072 / (a.buckets * 256)));
-    const int64_t heads = a.batch * a.heads, rows = a.waves * (64 / a.tx);
-    a.splits = (int)std::max<int64_t>(1, std::min(up(1024, std::max<int64_t>(1, heads)), up(a.nq, 4 * rows)));
-    return heads * a.splits;
+    a.tx = pow2_from(up(a.nk, 8), 8);
+    a.waves = a.buckets <= 127 ? 2 : 1;
+    const int64_t heads = std::max<int64_t>(1, a.batch * a.heads), keys = std::max<int64_t>(1, up(a.nk, 8 * a.tx));
+    a.splits = (int)std::max<int64_t>(1, std::min(2048 / (heads * keys), up(a.nq, 128)));
+    a.span = std::max<int64_t>(1, std::min(keys, heads * keys * a.splits / 2048));
+    a.cblocks = (int)up(keys, a.span * a.waves);
+    return heads * a.splits * a.cblocks;
 }
+namespace {
+int64_t bias_slots(const RelativeArgs& a) { return a.batch * a.splits * a.cblocks; }
+}  // namespace
 size_t relative_bias_part_floats(RelativeArgs a) {
     relative_bias_backward_plan(a);
-    const int64_t slots = a.batch * a.splits;
-    return slots <= 1 ? 0 : (size_t)slots * a.heads * a.buckets;
+    return bias_slots(a) <= 1 ? 0 : (size_t)bias_slots(a) * a.heads * a.buckets;
 }
 
 hipError_t launch_relative_bias_backward(int dtype, RelativeArgs a, hipStream_t s) {
@@ -427,8 +680,9 @@ hipError_t launch_relative_bias_backward(int dtype, RelativeArgs a, hipStream_t 
         hipLaunchKernelGGL(k_relative_zero, dim3((unsigned)up(n, 256)), dim3(256), 0, s, a.dtable, n);
         return hipGetLastError();
     }
+    a.wide_keys = keys_wide(a);
     a.wide = strides_wide(a.out, a.batch, a.heads, a.nq);
-    const size_t lds = (size_t)a.waves * a.buckets * 256 + lut_bytes(a.reach);
+    const size_t lds = (size_t)a.waves * (a.buckets + 1) * 256 + lut_bytes(a.reach);
     const dim3 grid((unsigned)groups), block(a.waves * 64);
     auto go = [&](auto kernel) {
         if (hipError_t e = with_lds(kernel, lds); e != hipSuccess) return e;
@@ -437,8 +691,8 @@ hipError_t launch_relative_bias_backward(int dtype, RelativeArgs a, hipStream_t 
     };
     const hipError_t e = dtype == 1 ? a.seg_q ? go(k_relative_bias_backward<bf16_t, true>) : go(k_relative_bias_backward<bf16_t, false>)
                                     : a.seg_q ? go(k_relative_bias_backward<float, true>) : go(k_relative_bias_backward<float, false>);
-    if (e != hipSuccess || a.batch * a.splits == 1) return e;
-    hipLaunchKernelGGL(k_relative_join, dim3((unsigned)up(n, 64)), dim3(256), 0, s, a, a.batch * a.splits);
+    if (e != hipSuccess || bias_slots(a) == 1) return e;
+    hipLaunchKernelGGL(k_relative_join, dim3((unsigned)up(n, 64)), dim3(1024), 0, s, a, bias_slots(a));
     return hipGetLastError();
 }
 
@@ -458,7 +712,7 @@ int64_t relative_pair_plan(RelativeArgs& a, int vector) {
     a.hblocks = (int)up(a.heads, a.cwidth);
     a.cblocks = (int)up(a.nk, 4 * (256 / a.tx));
     const int64_t groups = (int64_t)a.hblocks * a.cblocks * a.nq;
-    a.loop = std::min<int64_t>(64, std::max<int64_t>(1, groups / 1024));
+    a.loop = std::min<int64_t>(64, up(groups, 1024));
     a.rblocks = up(a.nq, a.loop);
     return (int64_t)a.hblocks * a.cblocks * a.rblocks;
 }
@@ -496,11 +750,11 @@ int pair_backward_vector(const RelativeArgs& a, int dtype) {
 }
 }  // namespace
 
-// Tiles of about 1 / 512 of the pairs each.
+// Tiles of about 1 / 256 of the pairs each: one for each compute unit.
 int64_t relative_pair_backward_plan(RelativeArgs& a, int vector) {
     a.hblocks = (int)up(a.heads, 64 * vector);
     a.waves = std::min(4, std::max(1, 139264 / (a.buckets * 256 * vector)));
-    const double pairs = (double)a.nq * a.nk / 512;
+    const double pairs = (double)a.nq * a.nk / 256;
     a.span = std::min<int64_t>(a.nk, std::max<int64_t>(64, up((int64_t)std::sqrt(pairs), 16) * 16));
     a.loop = std::max<int64_t>(1, (int64_t)std::ceil(pairs / a.span));
     if (a.loop > a.nq) {

@@ -60,16 +60,51 @@ template <typename T, int V> struct Vec {
     }
 };
 
-// Eight values of which the first n exist (the rest: 0, not read and not written); wide: p is 16-byte aligned.
-template <typename T>
-__device__ __forceinline__ void load_some(Vec<T, 8>& v, const T* p, int n, bool wide) {
-    if (wide && n >= 8) {
-        v.load(p);
-    } else {
+// The same values as they lie in memory.  Where loads are to be under way together, these are what is loaded: a
+// conversion beside a load, in a branch, waits for it there.
+template <typename T, int V> struct Words {
+    static constexpr int kWords = V * sizeof(T) < 4 ? 1 : V * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v.f[i] = i < n ? Store<T>::ld(p + i) : 0.f;
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
     }
-}
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (V * sizeof(T) == 2) w[0] = *reinterpret_cast<const uint16_t*>(p);
+        else if constexpr (kWords == 1) w[0] = *reinterpret_cast<const uint32_t*>(p);
+        else if constexpr (kWords == 2) {
+            const uint2 x = *reinterpret_cast<const uint2*>(p);
+            w[0] = x.x; w[1] = x.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords / 4; ++i) {
+                const uint4 x = reinterpret_cast<const uint4*>(p)[i];
+                w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+            }
+        }
+    }
+    // The first n of them, one by one; the rest are 0.
+    __device__ __forceinline__ void load_some(const T* p, int n) {
+        clear();
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < n) {
+                if constexpr (sizeof(T) == 4) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+                else w[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+            }
+    }
+    __device__ __forceinline__ Vec<T, V> values() const {
+        Vec<T, V> v;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if constexpr (sizeof(T) == 4) v.f[i] = __uint_as_float(w[i]);
+            else v.f[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        }
+        return v;
+    }
+};
+
+// Eight values of which the first n exist; wide: p is 16-byte aligned.
 template <typename T>
 __device__ __forceinline__ void store_some(const Vec<T, 8>& v, T* p, int n, bool wide) {
     if (wide && n >= 8) {
