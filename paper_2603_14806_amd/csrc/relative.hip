@@ -409,13 +409,14 @@ __global__ __launch_bounds__(256) void k_relative_pair(const RelativeArgs a) {
 
 // Sums by bucket over a tile of pairs.  A wave takes one pair at a time (a lane for V of its channels), so the bucket is
 // one for the wave: the sum stays in registers while it does not change, and goes to the wave's own table in LDS
-// when it does.  16 pairs are on their way while 16 are added.
+// when it does.  32 pairs are on their way while 32 are added; where their buckets rise or fall, as near the diagonal,
+// equal neighbours are added up and the places, all different then, are read, added to and written together.
 template <typename T, int V, bool SEG>
 __global__ __launch_bounds__(256) void k_relative_pair_backward(const RelativeArgs a) {
     extern __shared__ float val[];
-    constexpr int kAhead = 16;
-    const int table = a.buckets * 64 * V;
-    uint32_t* touched = reinterpret_cast<uint32_t*>(val + (size_t)a.waves * table);
+    constexpr int kAhead = 32;
+    const int table = a.buckets * 64 * V, own = table + 64 * V;      // (and a place for what is not to be kept)
+    uint32_t* touched = reinterpret_cast<uint32_t*>(val + (size_t)a.waves * own);
     uint8_t* lut = reinterpret_cast<uint8_t*>(touched + 8);
     int64_t at = blockIdx.x;
     const int cb = (int)(at % a.hblocks);
@@ -442,10 +443,10 @@ __global__ __launch_bounds__(256) void k_relative_pair_backward(const RelativeAr
     if (wave < steps) load(wave);
     lut_to_lds(a, lut, threads);
     if (threadIdx.x == 0) lut[2 * a.reach + 1] = (uint8_t)(a.buckets - 1);
-    zero_lds(val, a.waves * table, threads);
+    zero_lds(val, a.waves * own, threads);
     if (threadIdx.x < 8) touched[threadIdx.x] = 0;
     __syncthreads();
-    float* acc = val + (size_t)wave * table + lane * V;
+    float* acc = val + (size_t)wave * own + lane * V;
     float sum[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) sum[i] = 0.f;
@@ -482,33 +483,41 @@ __global__ __launch_bounds__(256) void k_relative_pair_backward(const RelativeAr
         const int t = lut[index], first = __builtin_amdgcn_readfirstlane(t);
         if (g + a.waves < steps) load(g + a.waves);
         if (lane < left) atomicOr(touched + t / 32, 1u << (t & 31));
-        const int before = __builtin_amdgcn_update_dpp(t, t, 0x111, 0xf, 0xf, false);          // row_shr 1: the pair before
-        const uint64_t inner = 0xfffe;                                                             // lanes 1..15
-        if (left == kAhead && ((__ballot(t > before) & inner) == inner || (__ballot(t < before) & inner) == inner)) {
-            turn_to(-1);                                           // all different: read, add and write them together
-            settle();
-            Vec<float, V> x[kAhead];
-            int to[kAhead];
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                to[u] = __builtin_amdgcn_readlane(t, u) * 64 * V;
-                x[u].load(acc + to[u]);
-            }
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) x[u].f[i] += v[u].f[i];
-                x[u].store(acc + to[u]);
-            }
-        } else if (left == kAhead && __ballot(t != first) == 0) {  // one bucket for all of them: a tree
+        const int before = __shfl_up(t, 1);
+        const uint64_t inner = 0xfffffffe;                         // lanes 1..31
+        if (left == kAhead && __ballot(t != first) == 0) {         // one bucket for all of them: a tree
             turn_to(first);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
 #pragma unroll
-                for (int level = 0; level < 4; ++level)
+                for (int level = 0; level < 5; ++level)
 #pragma unroll
-                    for (int u = 0; u < 8 >> level; ++u) v[u].f[i] += v[u + (8 >> level)].f[i];
+                    for (int u = 0; u < 16 >> level; ++u) v[u].f[i] += v[u + (16 >> level)].f[i];
                 sum[i] += v[0].f[i];
+            }
+        } else if (left == kAhead && ((__ballot(t >= before) & inner) == inner || (__ballot(t <= before) & inner) == inner)) {
+            turn_to(-1);
+            settle();
+#pragma unroll
+            for (int u0 = 0; u0 < kAhead; u0 += 16) {
+                Vec<float, V> x[16];
+                int to[16];
+#pragma unroll
+                for (int u = 0; u < 16; ++u) {
+                    const int here = __builtin_amdgcn_readlane(t, u0 + u);
+                    const bool last = u == 15 || here != __builtin_amdgcn_readlane(t, (u0 + u + 1) & 31);
+                    to[u] = (last ? here : a.buckets) * 64 * V;
+                    x[u].load(acc + to[u]);
+                    if (!last)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) v[(u0 + u + 1) & 31].f[i] += v[u0 + u].f[i];
+                }
+#pragma unroll
+                for (int u = 0; u < 16; ++u) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) x[u].f[i] += v[u0 + u].f[i];
+                    x[u].store(acc + to[u]);
+                }
             }
         } else {
 #pragma unroll
@@ -531,7 +540,7 @@ __global__ __launch_bounds__(256) void k_relative_pair_backward(const RelativeAr
         const int t = e / (64 * V);
         if (!(touched[t / 32] >> (t & 31) & 1)) continue;
         float s = 0.f;
-        for (int w = 0; w < a.waves; ++w) s += val[(size_t)w * table + e];
+        for (int w = 0; w < a.waves; ++w) s += val[(size_t)w * own + e];
         part[e] = s;
     }
     if (threadIdx.x < 8) a.masks[slot * 8 + threadIdx.x] = touched[threadIdx.x];
@@ -603,6 +612,7 @@ hipError_t with_lds(K kernel, size_t lds) {
 }  // namespace
 
 namespace {
+size_t bias_backward_lds(const RelativeArgs& a) { return (size_t)a.waves * (a.buckets + 1) * 256 + lut_bytes(a.reach); }
 size_t values_bytes(const RelativeArgs& a) {            // of one head: values_by_distance
     const size_t entries = 2 * (size_t)a.reach + 2;
     return (entries + entries / 8 + 1) * 4;
@@ -654,15 +664,16 @@ hipError_t launch_relative_bias(int dtype, RelativeArgs a, hipStream_t s) {
     return dtype == 1 ? by_heads(bf16_t{}) : by_heads(float{});
 }
 
-// Work-groups, and in a how rows and keys lie on their waves: two (one where their columns would outgrow 64 KB).  About
-// 2048 waves in all, eight for each compute unit, which is what LDS holds of 66 buckets; the rows of a wave are split
-// where its keys are too few to fill them, and are 128 at least.
+// Work-groups, and in a how rows and keys lie on their waves: two (one where their columns would outgrow 64 KB).  As many
+// as are at once on the compute units, by LDS and at most six on each (registers); rows are split where the keys are too
+// few for that, 128 to a wave at least.
 int64_t relative_bias_backward_plan(RelativeArgs& a) {
     a.tx = pow2_from(up(a.nk, 8), 8);
     a.waves = a.buckets <= 127 ? 2 : 1;
     const int64_t heads = std::max<int64_t>(1, a.batch * a.heads), keys = std::max<int64_t>(1, up(a.nk, 8 * a.tx));
-    a.splits = (int)std::max<int64_t>(1, std::min(2048 / (heads * keys), up(a.nq, 128)));
-    a.span = std::max<int64_t>(1, std::min(keys, heads * keys * a.splits / 2048));
+    const int64_t most = 256 * std::max<int64_t>(1, std::min<int64_t>(6, 163840 / (int64_t)bias_backward_lds(a)));
+    a.splits = (int)std::max<int64_t>(1, std::min(most / (heads * up(keys, a.waves)), up(a.nq, 128)));
+    a.span = std::max<int64_t>(1, std::min(keys, up(heads * keys * a.splits, most * a.waves)));
     a.cblocks = (int)up(keys, a.span * a.waves);
     return heads * a.splits * a.cblocks;
 }
@@ -682,7 +693,7 @@ hipError_t launch_relative_bias_backward(int dtype, RelativeArgs a, hipStream_t 
     }
     a.wide_keys = keys_wide(a);
     a.wide = strides_wide(a.out, a.batch, a.heads, a.nq);
-    const size_t lds = (size_t)a.waves * (a.buckets + 1) * 256 + lut_bytes(a.reach);
+    const size_t lds = bias_backward_lds(a);
     const dim3 grid((unsigned)groups), block(a.waves * 64);
     auto go = [&](auto kernel) {
         if (hipError_t e = with_lds(kernel, lds); e != hipSuccess) return e;
@@ -750,18 +761,27 @@ int pair_backward_vector(const RelativeArgs& a, int dtype) {
 }
 }  // namespace
 
-// Tiles of about 1 / 256 of the pairs each: one for each compute unit.
+namespace {
+size_t pair_backward_lds(const RelativeArgs& a, int vector) { return (size_t)a.waves * (a.buckets + 1) * 256 * vector + 32 + lut_bytes(a.reach); }
+}  // namespace
+
+// Tiles, as many as LDS lets the compute units have at once (one each for 66 buckets), about as wide as high, 64 columns at
+// least.  (Far from square, all of them would meet the diagonal; one more than fit at once takes a second round.)
 int64_t relative_pair_backward_plan(RelativeArgs& a, int vector) {
     a.hblocks = (int)up(a.heads, 64 * vector);
-    a.waves = std::min(4, std::max(1, 139264 / (a.buckets * 256 * vector)));
-    const double pairs = (double)a.nq * a.nk / 256;
-    a.span = std::min<int64_t>(a.nk, std::max<int64_t>(64, up((int64_t)std::sqrt(pairs), 16) * 16));
-    a.loop = std::max<int64_t>(1, (int64_t)std::ceil(pairs / a.span));
-    if (a.loop > a.nq) {
-        a.loop = a.nq;
-        a.span = up((int64_t)std::ceil(pairs / a.nq), 16) * 16;
-    }
+    a.waves = std::min(4, std::max(1, 143360 / ((a.buckets + 1) * 256 * vector)));
+    const int64_t at_once = 256 * std::min<int64_t>(4, std::max<int64_t>(1, 163840 / (int64_t)pair_backward_lds(a, vector)));
+    const int64_t tiles = std::max<int64_t>(1, at_once / a.hblocks);
+    const double pairs = (double)a.nq * a.nk / tiles;
+    const int64_t wide = std::max<int64_t>(64, up((int64_t)std::sqrt(pairs), 32) * 32);
+    a.span = std::min(a.nk, std::max(wide, up(a.nk, tiles)));
     a.cblocks = (int)up(a.nk, a.span);
+    a.loop = up(a.nq, std::min(a.nq, std::max<int64_t>(1, tiles / a.cblocks)));
+    if (a.loop == 1) {            // few rows: all of their tiles the same number of columns
+        a.cblocks = (int)std::max<int64_t>(1, std::min(up(a.nk, 64), tiles / a.nq));
+        a.span = up(a.nk, a.cblocks);
+        a.cblocks = (int)up(a.nk, a.span);
+    }
     a.rblocks = up(a.nq, a.loop);
     return a.cblocks * a.rblocks;
 }
@@ -784,7 +804,7 @@ hipError_t launch_relative_pair_backward(int dtype, RelativeArgs a, hipStream_t 
     const int v = pair_backward_vector(a, dtype);
     const int64_t tiles = relative_pair_backward_plan(a, v);
     a.masks = reinterpret_cast<uint32_t*>(a.part + (size_t)tiles * a.hblocks * a.buckets * 64 * v);
-    const size_t lds = (size_t)a.waves * a.buckets * 256 * v + 32 + lut_bytes(a.reach);
+    const size_t lds = pair_backward_lds(a, v);
     const dim3 grid((unsigned)(tiles * a.hblocks)), block(a.waves * 64);
     auto go = [&](auto kernel) {
         if (hipError_t e = with_lds(kernel, lds); e != hipSuccess) return e;

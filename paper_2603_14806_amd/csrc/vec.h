@@ -83,15 +83,18 @@ template <typename T, int V> struct Words {
             }
         }
     }
-    // The first n of them, one by one; the rest are 0.
+    // The first n of them, one by one (the first stands in for what is not there, and is 0 in its place; with n = 0 it
+    // has to be readable all the same).
     __device__ __forceinline__ void load_some(const T* p, int n) {
+        T x[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = p[i < n ? i : 0];
         clear();
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (i < n) {
-                if constexpr (sizeof(T) == 4) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
-                else w[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
-            }
+        for (int i = 0; i < V; ++i) {
+            if constexpr (sizeof(T) == 4) w[i] = i < n ? __float_as_uint(x[i]) : 0u;
+            else w[i / 2] |= i < n ? (uint32_t)x[i] << (16 * (i & 1)) : 0u;
+        }
     }
     __device__ __forceinline__ Vec<T, V> values() const {
         Vec<T, V> v;
