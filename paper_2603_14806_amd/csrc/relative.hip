@@ -209,7 +209,7 @@ __global__ __launch_bounds__(256) void k_relative_bias_backward(const RelativeAr
     constexpr int U = 4;
     const int columns = (a.buckets + 1) * 64;
     uint8_t* lut = reinterpret_cast<uint8_t*>(val + (size_t)a.waves * columns);
-    int64_t at = blockIdx.x;
+    int64_t at = by_xcd(blockIdx.x, gridDim.x);
     const int group = (int)(at % a.cblocks);
     at /= a.cblocks;
     const int split = (int)(at % a.splits);
@@ -433,9 +433,14 @@ __global__ __launch_bounds__(256) void k_relative_pair_backward(const RelativeAr
     int index = 0;                                     // of pair (lane % kAhead) of the pairs ahead; beyond reach: other segment
     auto load = [&](int g) {
         const int64_t r = r0 + g / per_row, j = j0 + (int64_t)(g % per_row) * kAhead;
-        const T* row = from + r * a.out.row;
+        const T* pair = from + r * a.out.row + j * a.heads;
+        if (j + kAhead <= j1) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) ahead[u].load(row + min(j + u, j1 - 1) * a.heads);
+            for (int u = 0; u < kAhead; ++u) ahead[u].load(pair + (int64_t)u * a.heads);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) ahead[u].load(pair + min((int64_t)u, j1 - 1 - j) * a.heads);
+        }
         const int64_t mine = min(j + (lane & (kAhead - 1)), j1 - 1);
         index = distance_index(a.pos_k[mine], a.pos_q[r], a.reach);
         if constexpr (SEG) index = a.seg_k[mine] == a.seg_q[r] ? index : 2 * a.reach + 1;
@@ -765,24 +770,18 @@ namespace {
 size_t pair_backward_lds(const RelativeArgs& a, int vector) { return (size_t)a.waves * (a.buckets + 1) * 256 * vector + 32 + lut_bytes(a.reach); }
 }  // namespace
 
-// Tiles, as many as LDS lets the compute units have at once (one each for 66 buckets), about as wide as high, 64 columns at
-// least.  (Far from square, all of them would meet the diagonal; one more than fit at once takes a second round.)
+// Tiles, as many as LDS lets the compute units have at once (one each for 66 buckets; one more than fit would take a
+// second round): whole rows, so that each has its share of the diagonal and reads long pieces (1000 x 1000 x 128 bf16:
+// 71 us; tiles of 64 columns, with fewer sums to join, 94), and parts of a row where there are fewer rows than tiles.
 int64_t relative_pair_backward_plan(RelativeArgs& a, int vector) {
     a.hblocks = (int)up(a.heads, 64 * vector);
     a.waves = std::min(4, std::max(1, 143360 / ((a.buckets + 1) * 256 * vector)));
     const int64_t at_once = 256 * std::min<int64_t>(4, std::max<int64_t>(1, 163840 / (int64_t)pair_backward_lds(a, vector)));
     const int64_t tiles = std::max<int64_t>(1, at_once / a.hblocks);
-    const double pairs = (double)a.nq * a.nk / tiles;
-    const int64_t wide = std::max<int64_t>(64, up((int64_t)std::sqrt(pairs), 32) * 32);
-    a.span = std::min(a.nk, std::max(wide, up(a.nk, tiles)));
-    a.cblocks = (int)up(a.nk, a.span);
-    a.loop = up(a.nq, std::min(a.nq, std::max<int64_t>(1, tiles / a.cblocks)));
-    if (a.loop == 1) {            // few rows: all of their tiles the same number of columns
-        a.cblocks = (int)std::max<int64_t>(1, std::min(up(a.nk, 64), tiles / a.nq));
-        a.span = up(a.nk, a.cblocks);
-        a.cblocks = (int)up(a.nk, a.span);
-    }
+    a.loop = up(a.nq, std::min(a.nq, tiles));
     a.rblocks = up(a.nq, a.loop);
+    a.span = up(a.nk, std::max<int64_t>(1, std::min(up(a.nk, 64), tiles / a.rblocks)));
+    a.cblocks = (int)up(a.nk, a.span);
     return a.cblocks * a.rblocks;
 }
 // Floats of the partial sums: for V = 2 and V = 1, whichever is more (the vector follows from the pointer).
