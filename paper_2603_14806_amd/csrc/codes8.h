@@ -33,7 +33,7 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, f
 // Code i (0..3) of a word, as a float.
 __device__ __forceinline__ float code_value(uint32_t w, int i) { return (float)(int)(int8_t)(w >> (8 * i)); }
 
-// The largest of G consecutive lanes (a power of two up to 64), in all of them.
+// The largest of G consecutive lanes (a power of two up to 32), in all of them.
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_umax(uint32_t v) {
     return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, false));
@@ -45,7 +45,6 @@ __device__ __forceinline__ uint32_t umax_lanes(uint32_t v) {
     if constexpr (G >= 8) v = dpp_umax<0x141>(v);    // row_half_mirror
     if constexpr (G >= 16) v = dpp_umax<0x140>(v);   // row_mirror
     if constexpr (G >= 32) v = max(v, (uint32_t)__shfl_xor((int)v, 16));
-    if constexpr (G >= 64) v = max(v, (uint32_t)__shfl_xor((int)v, 32));
     return v;
 }
 

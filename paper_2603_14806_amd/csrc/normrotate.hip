@@ -4,12 +4,19 @@
 // rotation needs no other lane.  G lanes (the next power of two of d / 8) are a row, and sum over it by DPP.  The angles
 // belong to the token: a wave turns all heads of its tokens, queries and keys, and where the entries of the batch share
 // their positions those of several entries, with one sine and cosine a pair.
+//
+// What bounds it (kernel times, bf16): memory, and next to it the vector units, busy for 61 to 67% of the cycles with 140 to 160
+// instructions for a wave's rows in the forward, 240 in the backward and with codes.  2 x 6000 tokens, 16 + 16 heads of 128, rms: 40 us (0.20 GB, 4.9
+// TB/s; a 1 GiB copy reaches 5.1).  384 x 384 tokens, 4 + 4 heads of 32, layer: 36.5 us (0.15 GB, 4.1 TB/s; neighbouring
+// pairs 34.4: half rows of 32 bytes are two accesses to each line) and backward 52 (0.23 GB, 4.3 TB/s).  4 x 2048 tokens with positions of
+// their own, 16 + 4 heads of 128, to and from 8 bits: 30 and 32 us (0.11 GB each, 3.5 and 3.3 TB/s: an item has the rows of a
+// token alone, and waits for its position and its rows once each).  4 single tokens: 5.6 us, a chain of two loads.
 #include <algorithm>
+#include <type_traits>
 
 #include "codes8.h"
 #include "common.h"
 #include "kernels.h"
-#include "vec.h"
 
 // Products and sums are joined where the source says so and nowhere else: a row has the same bits whichever of the kernels
 // below, and whichever place in its loop, it comes to.
@@ -24,7 +31,7 @@ constexpr double kTwoOverPi = 0.63661977236758134308;
 // adding 1.5 2^52 rounds it to whole quarters (their number in the low bits), and at most half a quarter r is left
 // either way.  There sin(pi / 2 r) = r S(r^2) and cos(pi / 2 r) = 1 + r^2 C(r^2) with cubics S and C through the
 // Chebyshev points of [0, 1/4] (3.2e-9 and 1.9e-10 off; with float32's own rounding 1.5 2^-24 and 1.0 2^-24).
-// (A library call for both took 46.2 us in place of 39.5 for 2 x 6000 tokens, 16 + 16 heads of 128, bf16.)
+// (A library call for both made the forward of 2 x 6000 tokens, 16 + 16 heads of 128, bf16, 46.2 us that is 42.3 with this.)
 __device__ __forceinline__ void turn(int p, double f, float& c, float& s) {
     constexpr double kWhole = 6755399441055744.0;
     const double t = (double)p * f, m = t + kWhole;
@@ -214,7 +221,8 @@ struct Angles {
     }
 };
 
-// Four rows are in flight while four are worked on, side by side (single ones at the end).
+// Four rows are in flight while four are worked on, side by side (single ones at the end).  The rows of the next item are
+// not asked for ahead: that takes 130 registers, and 12 waves a compute unit or spills (53 and 43.6 us for the 40 above).
 template <typename T, int G, bool HALVES, bool LAYER, bool HOLD>
 __global__ __launch_bounds__(256, sizeof(T) == 2 && !HOLD ? 4 : 3) void k_norm_rotate(const NormArgs a) {
     constexpr int U = 4;

@@ -5,7 +5,7 @@
 
 namespace trimul {
 
-// V consecutive values as floats, and back.
+// V consecutive values (1, 4 or 8; of floats also 2) as floats, and back.
 template <typename T, int V> struct Vec {
     float f[V];
     __device__ __forceinline__ void load(const T* p) {
@@ -14,10 +14,6 @@ template <typename T, int V> struct Vec {
         } else if constexpr (V == 2 && sizeof(T) == 4) {
             const float2 x = *reinterpret_cast<const float2*>(p);
             f[0] = x.x; f[1] = x.y;
-        } else if constexpr (V == 2) {
-            const uint32_t x = *reinterpret_cast<const uint32_t*>(p);
-            f[0] = __uint_as_float(x << 16);
-            f[1] = __uint_as_float(x & 0xffff0000u);
         } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int i = 0; i < V / 4; ++i) {
@@ -45,8 +41,6 @@ template <typename T, int V> struct Vec {
             Store<T>::st(p, f[0]);
         } else if constexpr (V == 2 && sizeof(T) == 4) {
             *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]);
-        } else if constexpr (V == 2) {
-            *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(f[0], f[1]);
         } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
             for (int i = 0; i < V / 4; ++i)
