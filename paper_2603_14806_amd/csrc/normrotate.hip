@@ -2,8 +2,8 @@
 //
 // A lane takes eight values of a row: four pairs that are turned together (halves: four values from each half), so that a
 // rotation needs no other lane.  G lanes (the next power of two of d / 8) are a row, and sum over it by DPP.  The angles
-// belong to the token: a wave turns all heads of its tokens, queries and keys, and where the entries of the batch share
-// their positions those of several entries, with one sine and cosine a pair.
+// belong to the token: a wave turns all heads of its tokens, of the queries or of the keys, and where the entries of the
+// batch share their positions those of several entries, with one sine and cosine a pair.
 //
 // What bounds it (kernel times, bf16): memory, and next to it the vector units, busy for 61 to 67% of the cycles with 140 to 160
 // instructions for a wave's rows in the forward, 240 in the backward and with codes.  2 x 6000 tokens, 16 + 16 heads of 128, rms: 40 us (0.20 GB, 4.9

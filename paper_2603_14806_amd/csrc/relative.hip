@@ -200,13 +200,14 @@ __global__ __launch_bounds__(256) void k_relative_bias(const RelativeArgs a) {
     }
 }
 
-// A work-group: one head of one entry, the rows of one split; a wave: a.span times the keys of its lanes.  A lane has a column of LDS
+// A work-group: one head of a.loop entries, the rows of one split; a wave: a.span times the keys of its lanes.  A lane has a column of LDS
 // for itself, a place for each bucket and one for what is not to be kept.
 //   Away from the diagonal a lane's eight keys have one distance index: their sum stays in a register while its bucket
 //   does not change.  Near it a lane's buckets usually rise or fall: equal neighbours are added up, and the eight
 //   places, all different then, are read, added to and written together.  Otherwise one after the other.
 // Bound by waiting: seven to twelve waves a compute unit, as LDS holds their columns, with one set of loads ahead each.  bf16, 16
-// heads, 66 buckets: 1300 x 1300 32 us in one chain, 39 in five (54 MB, 1.7 and 1.4 TB/s); 33 buckets, 2048 x 3000 73 us (2.7 TB/s).
+// heads, 66 buckets: 1300 x 1300 32 us in one chain, 39 in five (54 MB, 1.7 and 1.4 TB/s); 32 buckets, 2048 x 3000 73 us (2.7 TB/s); 1500 windows of 32 x 128, 4 heads, 38 us
+// (a work-group for each entry: 63, and 14 for their sums in place of 5).
 template <typename T, bool SEG>
 __global__ __launch_bounds__(256) void k_relative_bias_backward(const RelativeArgs a) {
     extern __shared__ float val[];
@@ -219,7 +220,7 @@ __global__ __launch_bounds__(256) void k_relative_bias_backward(const RelativeAr
     const int split = (int)(at % a.splits);
     at /= a.splits;
     const int h = (int)(at % a.heads);
-    const int64_t b = at / a.heads;
+    const int64_t part_of_batch = at / a.heads, b1 = min((part_of_batch + 1) * a.loop, a.batch);
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, threads = a.waves * 64;
     const int other = 2 * a.reach + 1;                   // (its place in lut holds the last bucket)
     lut_to_lds(a, lut, threads);
@@ -229,86 +230,88 @@ __global__ __launch_bounds__(256) void k_relative_bias_backward(const RelativeAr
     float* acc = val + wave * columns + lane;
     const int tx = lane & (a.tx - 1), ty = lane / a.tx, rows = 64 / a.tx;
     const int64_t per = (a.nq + a.splits - 1) / a.splits, r0 = split * per, r1 = min(r0 + per, a.nq);
-    const T* from = static_cast<const T*>(a.out.data) + b * a.out.batch + h * a.out.head;
-    const int32_t* pos_q = a.pos_q + b * a.pos_q_batch;
-    const int32_t* seg_q = SEG ? a.seg_q + b * a.seg_q_batch : nullptr;
     int cur = a.buckets;                                 // the bucket of `sum` (at first: none)
     float sum = 0.f;
-    for (int k = 0; k < a.span; ++k) {
-        const int64_t c = ((int64_t)group * a.waves + wave) * a.span + k;
-        if (c * a.tx * 8 >= a.nk) break;
-        const KeyPlace at_keys(a, c * a.tx + tx);
-        const int64_t j = at_keys.j;
-        const int n = at_keys.n;
-        const Keys<SEG> keys(a, b, j, max(n, 1));
-        Words<T, 8> ahead[U];
-        int pq_ahead[U], sq_ahead[U];
-        auto load = [&](int64_t first) {
+    for (int64_t b = part_of_batch * a.loop; b < b1; ++b) {
+        const T* from = static_cast<const T*>(a.out.data) + b * a.out.batch + h * a.out.head;
+        const int32_t* pos_q = a.pos_q + b * a.pos_q_batch;
+        const int32_t* seg_q = SEG ? a.seg_q + b * a.seg_q_batch : nullptr;
+        for (int k = 0; k < a.span; ++k) {
+            const int64_t c = ((int64_t)group * a.waves + wave) * a.span + k;
+            if (c * a.tx * 8 >= a.nk) break;
+            const KeyPlace at_keys(a, c * a.tx + tx);
+            const int64_t j = at_keys.j;
+            const int n = at_keys.n;
+            const Keys<SEG> keys(a, b, j, max(n, 1));
+            Words<T, 8> ahead[U];
+            int pq_ahead[U], sq_ahead[U];
+            auto load = [&](int64_t first) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t r = min(first + ty + u * rows, r1 - 1);
-                if (at_keys.whole) ahead[u].load(from + r * a.out.row + j);
-                else ahead[u].load_some(from + r * a.out.row + j, n);
-                pq_ahead[u] = pos_q[r];
-                sq_ahead[u] = SEG ? seg_q[r] : 0;
-            }
-        };
-        if (r0 < r1) load(r0);
-        for (int64_t first = r0; first < r1; first += U * rows) {
-            Vec<T, 8> v[U];
-            int pq[U], sq[U], common[U];
-            const bool some = __ballot(n == 0) != 0 || first + U * rows > r1;       // lanes or rows that count for nothing
+                for (int u = 0; u < U; ++u) {
+                    const int64_t r = min(first + ty + u * rows, r1 - 1);
+                    if (at_keys.whole) ahead[u].load(from + r * a.out.row + j);
+                    else ahead[u].load_some(from + r * a.out.row + j, n);
+                    pq_ahead[u] = pos_q[r];
+                    sq_ahead[u] = SEG ? seg_q[r] : 0;
+                }
+            };
+            if (r0 < r1) load(r0);
+            for (int64_t first = r0; first < r1; first += U * rows) {
+                Vec<T, 8> v[U];
+                int pq[U], sq[U], common[U];
+                const bool some = __ballot(n == 0) != 0 || first + U * rows > r1;       // lanes or rows that count for nothing
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                v[u] = ahead[u].values();
-                if (some)
+                for (int u = 0; u < U; ++u) {
+                    v[u] = ahead[u].values();
+                    if (some)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[u].f[i] = n > 0 && first + ty + u * rows < r1 ? v[u].f[i] : 0.f;
-                pq[u] = pq_ahead[u];
-                sq[u] = sq_ahead[u];
-            }
-            if (first + U * rows < r1) load(first + U * rows);
+                        for (int i = 0; i < 8; ++i) v[u].f[i] = n > 0 && first + ty + u * rows < r1 ? v[u].f[i] : 0.f;
+                    pq[u] = pq_ahead[u];
+                    sq[u] = sq_ahead[u];
+                }
+                if (first + U * rows < r1) load(first + U * rows);
 #pragma unroll
-            for (int u = 0; u < U; ++u) common[u] = keys.common(pq[u], sq[u], a.reach, other);
+                for (int u = 0; u < U; ++u) common[u] = keys.common(pq[u], sq[u], a.reach, other);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const float* f = v[u].f;
-                if (__ballot(common[u] < 0) == 0) {
-                    const int t = lut[common[u]];
-                    const float x = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
-                    if (__ballot(t != cur) == 0) {
-                        sum += x;
-                    } else {
-                        acc[cur * 64] += sum;
-                        cur = t;
-                        sum = x;
+                for (int u = 0; u < U; ++u) {
+                    const float* f = v[u].f;
+                    if (__ballot(common[u] < 0) == 0) {
+                        const int t = lut[common[u]];
+                        const float x = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+                        if (__ballot(t != cur) == 0) {
+                            sum += x;
+                        } else {
+                            acc[cur * 64] += sum;
+                            cur = t;
+                            sum = x;
+                        }
+                        continue;
                     }
-                    continue;
-                }
-                int t[8];
+                    int t[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) t[i] = lut[keys.index(i, pq[u], sq[u], a.reach, other)];
-                bool rises = true, falls = true;
+                    for (int i = 0; i < 8; ++i) t[i] = lut[keys.index(i, pq[u], sq[u], a.reach, other)];
+                    bool rises = true, falls = true;
 #pragma unroll
-                for (int i = 1; i < 8; ++i) {
-                    rises = rises && t[i] >= t[i - 1];
-                    falls = falls && t[i] <= t[i - 1];
-                }
-                if (__ballot(!(rises || falls)) == 0) {
-                    float x[8], old[8];
-                    int to[8];
-                    x[0] = f[0];
+                    for (int i = 1; i < 8; ++i) {
+                        rises = rises && t[i] >= t[i - 1];
+                        falls = falls && t[i] <= t[i - 1];
+                    }
+                    if (__ballot(!(rises || falls)) == 0) {
+                        float x[8], old[8];
+                        int to[8];
+                        x[0] = f[0];
 #pragma unroll
-                    for (int i = 1; i < 8; ++i) x[i] = t[i] == t[i - 1] ? x[i - 1] + f[i] : f[i];
+                        for (int i = 1; i < 8; ++i) x[i] = t[i] == t[i - 1] ? x[i - 1] + f[i] : f[i];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) to[i] = (i < 7 && t[i] == t[(i + 1) & 7] ? a.buckets : t[i]) * 64;
+                        for (int i = 0; i < 8; ++i) to[i] = (i < 7 && t[i] == t[(i + 1) & 7] ? a.buckets : t[i]) * 64;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) old[i] = acc[to[i]];
+                        for (int i = 0; i < 8; ++i) old[i] = acc[to[i]];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[to[i]] = old[i] + x[i];
-                } else {
+                        for (int i = 0; i < 8; ++i) acc[to[i]] = old[i] + x[i];
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[t[i] * 64] += f[i];
+                        for (int i = 0; i < 8; ++i) acc[t[i] * 64] += f[i];
+                    }
                 }
             }
         }
@@ -326,8 +329,8 @@ __global__ __launch_bounds__(256) void k_relative_bias_backward(const RelativeAr
 #pragma unroll
         for (int m = 1; m < 8; m *= 2) sum += __shfl_xor(sum, m);
         if (t < a.buckets && part == 0) {
-            if (a.batch * a.splits * a.cblocks == 1) a.dtable[(int64_t)t * a.heads + h] = (float)sum;
-            else a.part[(((b * a.splits + split) * a.cblocks + group) * a.heads + h) * a.buckets + t] = (float)sum;
+            if (a.loop >= a.batch && a.splits * a.cblocks == 1) a.dtable[(int64_t)t * a.heads + h] = (float)sum;
+            else a.part[(((part_of_batch * a.splits + split) * a.cblocks + group) * a.heads + h) * a.buckets + t] = (float)sum;
         }
     }
 }
@@ -682,15 +685,16 @@ hipError_t launch_relative_bias(int dtype, RelativeArgs a, hipStream_t s) {
 int64_t relative_bias_backward_plan(RelativeArgs& a) {
     a.tx = pow2_from(up(a.nk, 8), 8);
     a.waves = a.buckets <= 127 ? 2 : 1;
-    const int64_t heads = std::max<int64_t>(1, a.batch * a.heads), keys = std::max<int64_t>(1, up(a.nk, 8 * a.tx));
+    const int64_t batch = std::max<int64_t>(1, a.batch), heads = batch * a.heads, keys = std::max<int64_t>(1, up(a.nk, 8 * a.tx));
     const int64_t most = 256 * std::max<int64_t>(1, std::min<int64_t>(6, 163840 / (int64_t)bias_backward_lds(a)));
     a.splits = (int)std::max<int64_t>(1, std::min(most / (heads * up(keys, a.waves)), up(a.nq, 128)));
-    a.span = std::max<int64_t>(1, std::min(keys, up(heads * keys * a.splits, most * a.waves)));
+    a.span = std::max<int64_t>(1, std::min(up(keys, a.waves), up(heads * keys * a.splits, most * a.waves)));
     a.cblocks = (int)up(keys, a.span * a.waves);
-    return heads * a.splits * a.cblocks;
+    a.loop = std::max<int64_t>(1, std::min(batch, heads * a.cblocks / most));     // small entries, many of them: several to each
+    return up(batch, a.loop) * a.heads * a.splits * a.cblocks;
 }
 namespace {
-int64_t bias_slots(const RelativeArgs& a) { return a.batch * a.splits * a.cblocks; }
+int64_t bias_slots(const RelativeArgs& a) { return up(a.batch, a.loop) * a.splits * a.cblocks; }
 }  // namespace
 size_t relative_bias_part_floats(RelativeArgs a) {
     relative_bias_backward_plan(a);

@@ -153,6 +153,24 @@ def test_entries_and_shared_axes():
         assert np.array_equal(host(R.relative_bias_backward(one, b, *places)), want)
 
 
+@pytest.mark.parametrize("own_places", [False, True])
+def test_many_small_entries(own_places):
+    """More entries than work-groups, as windows are: several of them to a work-group, and the last with fewer."""
+    b = R.Buckets.logarithmic(12, 30, other=True)
+    n, nq, nk, heads = 1100, 9, 21, 3
+    shape = (n,) if own_places else ()
+    places = [integers(shape + (m,), lo, hi, s) for m, lo, hi, s in ((nq, -20, 20, 1), (nk, -20, 20, 2), (nq, 0, 2, 3), (nk, 0, 2, 4))]
+    d = padded(whole((n, heads, nq, nk), 5, "bf16"))
+    x = host(d)
+    at = lambda e: [host(t[e] if own_places else t).astype(np.int64) for t in places]
+    want = sum(O.table_gradient(np.moveaxis(x[e], 0, -1), O.buckets(b.lut.tolist(), b.rows, *at(e)), b.rows) for e in range(n))
+    assert np.array_equal(host(R.relative_bias_backward(d, b, *places)), want)
+    table = normal((b.rows, heads), 6)
+    got = R.relative_bias(table, b, *places, base=d, dtype="bf16")
+    for e in (0, 511, n - 1):
+        near(got[e], x[e] + O.relative_bias(host(table), O.buckets(b.lut.tolist(), b.rows, *at(e))), "bf16")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_gradients_of_longer_calls(dtype):
     """Splits and tiles: every row of the table within the float32 sums' bound, and the same bits again."""
