@@ -200,6 +200,11 @@ struct Rows {
         return entry * t.batch + token0 * t.token + (int64_t)(step * q.slots) * t.head;
     }
     static __device__ __forceinline__ int64_t own(const CrossTensor& t, const Lane& x) { return x.token * t.token + x.head * t.head; }
+    // the same of the row's number in contiguous codes and powers
+    __device__ __forceinline__ int64_t number(const NormArgs& a, const NormSide& q, int64_t token0) const {
+        return (entry * a.n + token0) * q.heads + step * q.slots;
+    }
+    static __device__ __forceinline__ int own_number(const NormSide& q, const Lane& x) { return x.token * q.heads + x.head; }
 };
 
 // The angles' part of an item: the position is asked for early, the sines follow when the rows are on their way.
@@ -235,6 +240,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && !HOLD ? 4 : 3) void k_norm_r
     weights8<HALVES>(gain, q.gain, a.weight_bf16, x, 1.f);
     weights8<HALVES>(shift, q.shift, a.weight_bf16, x, 0.f);
     const int64_t own_x = Rows::own(q.x, x), own_y = Rows::own(q.y, x);
+    const int own_number = Rows::own_number(q, x);
     Raw<T, HALVES> raw[U];
     auto load = [&](const Place& at, Rows& row, int left) {
 #pragma unroll
@@ -289,15 +295,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && !HOLD ? 4 : 3) void k_norm_r
                         hi = codes4(v[u][4], v[u][5], v[u][6], v[u][7], inverse);
                     }
                     if (!live[u]) continue;
-                    const int64_t place = (at[u].entry * a.n + token) * q.heads + at[u].step * q.slots + x.head;
-                    int8_t* to = q.codes + place * a.d;
+                    const int64_t number = at[u].number(a, q, token0);
+                    int8_t* to = q.codes + number * a.d + own_number * a.d;
                     if constexpr (HALVES) {
                         *reinterpret_cast<uint32_t*>(to + x.lo) = lo;
                         *reinterpret_cast<uint32_t*>(to + x.hi) = hi;
                     } else {
                         *reinterpret_cast<uint2*>(to + x.lo) = make_uint2(lo, hi);
                     }
-                    if (x.l == 0) q.powers[place] = (uint8_t)byte;
+                    if (x.l == 0) (q.powers + number)[own_number] = (uint8_t)byte;
                 }
             }
 #pragma unroll
@@ -360,6 +366,7 @@ __global__ __launch_bounds__(256) void k_norm_rotate_backward(const NormArgs a) 
 #pragma unroll
     for (int e = 0; e < 8; ++e) total[0][e] = total[1][e] = 0.f;
     const int64_t own_x = Rows::own(q.x, x), own_y = Rows::own(q.y, x), own_dx = Rows::own(q.dx, x);
+    const int own_number = Rows::own_number(q, x);
     Input<T, HALVES, HELD> in[U];
     Raw<T, HALVES> dy[U];
     auto load = [&](const Place& at, Rows& row, int left) {
@@ -369,8 +376,8 @@ __global__ __launch_bounds__(256) void k_norm_rotate_backward(const NormArgs a) 
             dy[u].clear();
             if (u < left && at.token < a.n && row.step * q.slots + x.head < q.heads) {
                 if constexpr (HELD) {
-                    const int64_t place = (row.entry * a.n + at.token) * q.heads + row.step * q.slots + x.head;
-                    const int8_t* from = q.codes + place * a.d;
+                    const int64_t number = row.number(a, q, at.token0);
+                    const int8_t* from = q.codes + number * a.d + own_number * a.d;
                     if constexpr (HALVES) {
                         in[u].lo = *reinterpret_cast<const uint32_t*>(from + x.lo);
                         in[u].hi = *reinterpret_cast<const uint32_t*>(from + x.hi);
@@ -379,7 +386,7 @@ __global__ __launch_bounds__(256) void k_norm_rotate_backward(const NormArgs a) 
                         in[u].lo = both.x;
                         in[u].hi = both.y;
                     }
-                    in[u].byte = q.powers[place];
+                    in[u].byte = (q.powers + number)[own_number];
                 } else {
                     in[u].raw.load(static_cast<const T*>(q.x.data) + row.of(q, q.x, at.token0) + own_x, x.lo, x.hi);
                 }
@@ -519,10 +526,11 @@ int64_t plan(NormArgs& a, int dtype, bool backward) {
     int64_t work[2], total = 0;
     for (int i = 0; i < 2; ++i) {
         NormSide& q = a.side[i];
-        // An item should have at least four rows for its angles, which take as long as one: several entries, or, where
-        // each has its own positions, fewer heads at once (of 128 bytes at least) and several head steps.
+        // An item should have several rows for its angles, which take as long as one, and a second group of rows to ask
+        // for: several entries, or, where each has its own positions, fewer heads at once (of 128 bytes at least) and up to
+        // eight head steps (four: 30.8 us in place of 28.2 for the forward to 8 bits above).
         const int least = shared ? rows : pow2_from((int)up(128, a.d * (dtype == 1 ? 2 : 4)), rows);
-        q.slots = pow2_from(shared ? q.heads : std::max((int)up(q.heads, 4), std::min(least, q.heads)), rows);
+        q.slots = pow2_from(shared ? q.heads : std::max((int)up(q.heads, 8), std::min(least, q.heads)), rows);
         q.steps = (int)up(q.heads, q.slots);
         q.tiles = up(a.n, rows / q.slots);
         work[i] = a.batch * q.tiles * q.steps;
