@@ -9,7 +9,7 @@
 // instructions for a wave's rows in the forward, 240 in the backward and with codes.  2 x 6000 tokens, 16 + 16 heads of 128, rms: 40 us (0.20 GB, 4.9
 // TB/s; a 1 GiB copy reaches 5.1).  384 x 384 tokens, 4 + 4 heads of 32, layer: 36.5 us (0.15 GB, 4.1 TB/s; neighbouring
 // pairs 34.4: half rows of 32 bytes are two accesses to each line) and backward 52 (0.23 GB, 4.3 TB/s).  4 x 2048 tokens with positions of
-// their own, 16 + 4 heads of 128, to and from 8 bits: 30 and 32 us (0.11 GB each, 3.5 and 3.3 TB/s: an item has the rows of a
+// their own, 16 + 4 heads of 128, to and from 8 bits: 28 and 33 us (0.11 GB each, 3.8 and 3.2 TB/s: an item has the rows of a
 // token alone, and waits for its position and its rows once each).  4 single tokens: 5.6 us, a chain of two loads.
 #include <algorithm>
 #include <type_traits>

@@ -2,7 +2,8 @@
 //
 // Both forms of the forward are a look-up in LDS beside a stream of stores (and of the base's loads).  The gradient is
 // a sum by bucket: every lane adds into a column of LDS of its own, so that no two lanes meet, the order of the
-// sums is fixed, and no two lanes of a wave share a bank.
+// sums is fixed, and no two lanes of a wave share a bank.  They read, add and write: LDS's own float additions take about
+// 200 cycles of a compute unit for a wave's 64 (169 us for the gradient of 1300 x 1300 x 16 that takes 39 now).
 #include <algorithm>
 #include <type_traits>
 
@@ -200,14 +201,14 @@ __global__ __launch_bounds__(256) void k_relative_bias(const RelativeArgs a) {
     }
 }
 
-// A work-group: one head of a.loop entries, the rows of one split; a wave: a.span times the keys of its lanes.  A lane has a column of LDS
-// for itself, a place for each bucket and one for what is not to be kept.
+// A work-group: one head of a.loop entries, the rows of one split; a wave: a.span times the keys of its lanes.  A lane has
+// a column of LDS for itself, a place for each bucket and one for what is not to be kept.
 //   Away from the diagonal a lane's eight keys have one distance index: their sum stays in a register while its bucket
 //   does not change.  Near it a lane's buckets usually rise or fall: equal neighbours are added up, and the eight
 //   places, all different then, are read, added to and written together.  Otherwise one after the other.
 // Bound by waiting: seven to twelve waves a compute unit, as LDS holds their columns, with one set of loads ahead each.  bf16, 16
-// heads, 66 buckets: 1300 x 1300 32 us in one chain, 39 in five (54 MB, 1.7 and 1.4 TB/s); 32 buckets, 2048 x 3000 73 us (2.7 TB/s); 1500 windows of 32 x 128, 4 heads, 38 us
-// (a work-group for each entry: 63, and 14 for their sums in place of 5).
+// heads, 66 buckets: 1300 x 1300 32 us in one chain, 39 in five (54 MB, 1.7 and 1.4 TB/s); 32 buckets, 2048 x 3000 73 us (2.7 TB/s);
+// 1500 windows of 32 x 128, 4 heads, 38 us (a work-group for each entry: 63, and 14 for their sums in place of 5).
 template <typename T, bool SEG>
 __global__ __launch_bounds__(256) void k_relative_bias_backward(const RelativeArgs a) {
     extern __shared__ float val[];

@@ -115,36 +115,37 @@ def _call(sides, positions, freqs, norm, pairs, eps):
                 raise ValueError(f"weights of {name}, which is missing")
             result.append(None)
             continue
-        if len(x.shape) != 4:
+        shape = x.shape
+        if len(shape) != 4:
             raise ValueError("q and k must be [batch][n][heads][d]")
-        heads = x.shape[2]
-        s = NormRotateSide(heads)
+        heads = shape[2]
         if isinstance(x, _c8.Checkpoint8) != held:
             raise ValueError("q and k are both tensors or both checkpoints")
-        if held:
-            if x.shape != (batch, n, heads, d) or x.dtype != dtype or x.device != device or x.group != d:
-                raise ValueError(f"{name} must be a checkpoint of a {dtype} {[batch, n, heads, d]} tensor on {device} in groups of {d}")
-            s.codes, s.powers = x.codes.data_ptr(), x.powers.data_ptr()
-        else:
-            s.x = _checked(name, x, dtype, device, (batch, n, heads, d))
+        addresses = []
         for what, t in (("gain", gain), ("shift", shift)):
             if t is None:
+                addresses.append(None)
                 continue
             if t.dtype not in _DTYPES or t.device != device or t.shape != (d,) or not t.is_contiguous():
                 raise ValueError(f"{what} of {name} must be contiguous float32 or bfloat16 [{d}] on {device}, not {t.dtype} {list(t.shape)} on {t.device}")
             if weight is not None and t.dtype != weight:
                 raise ValueError("gains and shifts must be of one type")
             weight = t.dtype
-            setattr(s, what, t.data_ptr())
-        result.append(s)
+            addresses.append(t.data_ptr())
+        if held:
+            if shape != (batch, n, heads, d) or x.dtype != dtype or x.device != device or x.group != d:
+                raise ValueError(f"{name} must be a checkpoint of a {dtype} {[batch, n, heads, d]} tensor on {device} in groups of {d}")
+            result.append(NormRotateSide(heads, CrossAttnTensor(), *addresses, x.codes.data_ptr(), x.powers.data_ptr()))
+        else:
+            result.append(NormRotateSide(heads, _checked(name, x, dtype, device, (batch, n, heads, d)), *addresses))
     if weight is not None:
         w.weight_dtype = _DTYPES[weight]
     return w, result
 
 
-def _tensor_of(t):
-    s = t.stride()
-    return CrossAttnTensor(t.data_ptr(), s[0], s[1], s[2])
+def _dense(t, n, heads, d):
+    """cross_attn_tensor_t of a contiguous [batch][n][heads][d] tensor."""
+    return CrossAttnTensor(t.data_ptr(), n * heads * d, heads * d, d)
 
 
 def norm_rotate(q, k, positions=None, freqs=None, gain_q=None, gain_k=None, shift_q=None, shift_k=None, norm="rms",
@@ -161,26 +162,30 @@ def norm_rotate(q, k, positions=None, freqs=None, gain_q=None, gain_k=None, shif
     first = q if q is not None else k
     if not isinstance(first, torch.Tensor):
         raise ValueError("q and k must be tensors")
+    ys, to, held = [], [], []
     with on_stream(first.device, stream) as s:
-        ys, held = [], []
         for x, side, out, name in ((q, sq, out_q, "out_q"), (k, sk, out_k, "out_k")):
             if x is None:
                 if out is not None:
                     raise ValueError(f"{name} without its input")
                 ys.append(None)
+                to.append(None)
                 held.append(None)
                 continue
-            y = x.new_empty(x.shape) if out is None else out
-            ys.append((y, _tensor_of(y) if out is None else _checked(name, y, x.dtype, x.device, x.shape)))
+            shape = x.shape
+            if out is None:
+                out = x.new_empty(shape)
+                to.append(_dense(out, w.n, shape[2], w.d))
+            else:
+                to.append(_checked(name, out, x.dtype, x.device, shape))
+            ys.append(out)
             if checkpoint:
-                c = _c8.Checkpoint8(torch.empty(x.shape, dtype=torch.int8, device=x.device),
-                                    torch.empty(tuple(x.shape[:3]) + (1,), dtype=torch.uint8, device=x.device), x.shape[3], x.dtype)
+                c = _c8.Checkpoint8(torch.empty(shape, dtype=torch.int8, device=x.device),
+                                    torch.empty((w.batch, w.n, shape[2], 1), dtype=torch.uint8, device=x.device), w.d, x.dtype)
                 side.codes, side.powers = c.codes.data_ptr(), c.powers.data_ptr()
                 held.append(c)
-        yq, yk = ys
-        _check(lib().norm_rotate_forward(w, sq, sk, yq and yq[1], yk and yk[1], s))
-    out = (yq and yq[0], yk and yk[0])
-    return out + tuple(held) if checkpoint else out
+        _check(lib().norm_rotate_forward(w, sq, sk, to[0], to[1], s))
+    return tuple(ys + held) if checkpoint else tuple(ys)
 
 
 def norm_rotate_backward(q, k, dyq, dyk, positions=None, freqs=None, gain_q=None, gain_k=None, shift_q=None, shift_k=None,
@@ -189,22 +194,26 @@ def norm_rotate_backward(q, k, dyq, dyk, positions=None, freqs=None, gain_q=None
     gain_q, gain_k, shift_q, shift_k as float32 [d] (None where there is no such weight)."""
     w, (sq, sk) = _call((("q", q, gain_q, shift_q), ("k", k, gain_k, shift_k)), positions, freqs, norm, pairs, eps)
     first = q if q is not None else k
+    weights = {"gain_q": gain_q, "gain_k": gain_k, "shift_q": shift_q, "shift_k": shift_k}
+    there = [name for name, t in weights.items() if t is not None]
     with on_stream(first.device, stream) as s:
-        grads, dxs, gs = {}, [], []
-        for x, dy, name, gain, shift in ((q, dyq, "q", gain_q, shift_q), (k, dyk, "k", gain_k, shift_k)):
+        grads = dict.fromkeys(weights)
+        if there:                                   # (one allocation for all of them)
+            grads.update(zip(there, torch.empty((len(there), w.d), dtype=torch.float32, device=first.device).unbind()))
+        dxs, gs = [], []
+        for x, dy, name in ((q, dyq, "q"), (k, dyk, "k")):
             if (x is None) != (dy is None):
                 raise ValueError(f"{name} and dy{name} are both given or both None")
-            for what, t in (("gain_", gain), ("shift_", shift)):
-                grads[what + name] = None if t is None else torch.empty(w.d, dtype=torch.float32, device=first.device)
             if x is None:
                 dxs.append(None)
                 gs.append(None)
                 continue
-            td = _checked("dy" + name, dy, x.dtype, x.device, tuple(x.shape))
-            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            shape = x.shape
+            td = _checked("dy" + name, dy, x.dtype, x.device, shape)
+            dx = torch.empty(shape, dtype=x.dtype, device=x.device)
             dxs.append(dx)
-            gs.append(NormRotateGrad(td, _tensor_of(dx), _ptr(grads["gain_" + name]), _ptr(grads["shift_" + name])))
+            gs.append(NormRotateGrad(td, _dense(dx, w.n, shape[2], w.d), _ptr(grads["gain_" + name]), _ptr(grads["shift_" + name])))
         n = norm_rotate_backward_workspace_size(w, sq, sk)
         ws = torch.empty(n, dtype=torch.uint8, device=first.device) if n else None
         _check(lib().norm_rotate_backward(w, sq, sk, gs[0], gs[1], _ptr(ws), n, s))
-    return dxs[0], dxs[1], {n: grads[n] for n in ("gain_q", "gain_k", "shift_q", "shift_k")}
+    return dxs[0], dxs[1], grads
