@@ -10,7 +10,7 @@
 // TB/s; a 1 GiB copy reaches 5.1).  384 x 384 tokens, 4 + 4 heads of 32, layer: 36.5 us (0.15 GB, 4.1 TB/s; neighbouring
 // pairs 34.4: half rows of 32 bytes are two accesses to each line) and backward 52 (0.23 GB, 4.3 TB/s).  4 x 2048 tokens with positions of
 // their own, 16 + 4 heads of 128, to and from 8 bits: 28 and 33 us (0.11 GB each, 3.8 and 3.2 TB/s: an item has the rows of a
-// token alone, and waits for its position and its rows once each).  4 single tokens: 5.6 us, a chain of two loads.
+// token alone, and waits for its position and its rows once each).  4 single tokens: 4.2 us, a chain of two loads.
 #include <algorithm>
 #include <type_traits>
 
@@ -523,14 +523,16 @@ int64_t up(int64_t n, int64_t d) { return (n + d - 1) / d; }
 int64_t plan(NormArgs& a, int dtype, bool backward) {
     const int rows = 64 / lanes_of(a.d);                        // of a wave at once
     const bool shared = a.positions_batch == 0 || a.rot == 0;
+    const bool few = a.batch * a.n * (a.side[0].heads + a.side[1].heads) < 4096 * (int64_t)rows;
     int64_t work[2], total = 0;
     for (int i = 0; i < 2; ++i) {
         NormSide& q = a.side[i];
         // An item should have several rows for its angles, which take as long as one, and a second group of rows to ask
         // for: several entries, or, where each has its own positions, fewer heads at once (of 128 bytes at least) and up to
-        // eight head steps (four: 30.8 us in place of 28.2 for the forward to 8 bits above).
-        const int least = shared ? rows : pow2_from((int)up(128, a.d * (dtype == 1 ? 2 : 4)), rows);
-        q.slots = pow2_from(shared ? q.heads : std::max((int)up(q.heads, 8), std::min(least, q.heads)), rows);
+        // eight head steps (four: 30.8 us in place of 28.2 for the forward to 8 bits above).  Not where the rows are too few
+        // to fill the waves: there steps are latency (4 single tokens of 16 + 4 heads of 64: eight steps 7.5 us, two 4.2).
+        const int least = shared || few ? rows : pow2_from((int)up(128, a.d * (dtype == 1 ? 2 : 4)), rows);
+        q.slots = pow2_from(shared || few ? q.heads : std::max((int)up(q.heads, 8), std::min(least, q.heads)), rows);
         q.steps = (int)up(q.heads, q.slots);
         q.tiles = up(a.n, rows / q.slots);
         work[i] = a.batch * q.tiles * q.steps;
