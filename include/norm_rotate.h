@@ -73,7 +73,7 @@ typedef struct {
 
 /* yq and yk from the two sides (k and yk, or q and yq, may be NULL).  Errors: EINVAL
  * for null or misaligned pointers, sizes, strides, types, eps; EUNSUPPORTED for 2^31
- * entries or tokens, strides of 2^40; EHIP for a failed launch. */
+ * entries or tokens, 2^44 values, strides of 2^40; EHIP for a failed launch. */
 int norm_rotate_forward(const norm_rotate_view_t* v, const norm_rotate_side_t* q, const norm_rotate_side_t* k,
                         const cross_attn_tensor_t* yq, const cross_attn_tensor_t* yk, void* stream);
 

@@ -52,7 +52,7 @@ typedef struct {
  * base: NULL for 0.  The values behind the nk-th of a row are neither read nor
  * written.  Data needs its type's alignment (16-byte alignment and strides that are
  * multiples of 8 are fastest).  Errors: EINVAL for null or misaligned pointers,
- * sizes, strides, types; EUNSUPPORTED for nq or nk of 2^24, strides of 2^40 or more
+ * sizes, strides, types; EUNSUPPORTED for nq or nk of 2^24, 2^48 values, strides of 2^40 or more
  * than 2^24 - 1 work-groups; EHIP for a failed launch. */
 int relative_bias(const relative_view_t* v, const void* table, const cross_attn_bias_t* base,
                   const cross_attn_bias_t* out, void* stream);

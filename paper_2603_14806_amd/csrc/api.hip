@@ -1629,6 +1629,7 @@ int relative_check(const relative_view_t* v, bool pair) {
     if (v->reach < 0 || v->reach > 4095) return fail(TRI_MUL_EINVAL, "reach = %d outside [0, 4095]", v->reach);
     const int64_t most = int64_t(1) << 24;
     if (v->batch >= most || v->nq >= most || v->nk >= most) return fail(TRI_MUL_EUNSUPPORTED, "batch, nq or nk of 2^24 or more");
+    if ((__int128)v->batch * v->heads * v->nq * v->nk >= (__int128)1 << 48) return fail(TRI_MUL_EUNSUPPORTED, "2^48 values");  // (the plans count in 64 bits)
     if (!v->lut) return fail(TRI_MUL_EINVAL, "null lut");
     if (!v->seg_q != !v->seg_k) return fail(TRI_MUL_EINVAL, "segments of the queries and the keys are both given or both NULL");
     if ((v->nq && !v->pos_q) || (v->nk && !v->pos_k)) return fail(TRI_MUL_EINVAL, "null positions");
@@ -1802,6 +1803,7 @@ int norm_check(const norm_rotate_view_t* v, const norm_rotate_side_t* q, const n
         if (!aligned16(x->gain) || !aligned16(x->shift)) return fail(TRI_MUL_EINVAL, "gain and shift must be 16-byte aligned");
         if (!x->codes != !x->powers) return fail(TRI_MUL_EINVAL, "codes and powers are both given or both NULL");
         if (!aligned16(x->codes)) return fail(TRI_MUL_EINVAL, "codes must be 16-byte aligned");
+        if ((__int128)v->batch * v->n * x->heads * v->d >= (__int128)1 << 44) return fail(TRI_MUL_EUNSUPPORTED, "2^44 values");  // (a wave's rows are counted in 32 bits)
     }
     return TRI_MUL_OK;
 }

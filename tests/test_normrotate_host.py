@@ -182,3 +182,10 @@ def test_python_refusals():
         N.norm_rotate(x.half(), None)
     with pytest.raises(ValueError, match="heads"):
         N.norm_rotate_backward(x[0], None, x[0], None)
+
+
+def test_more_values_than_counted_refused(lib):
+    """Products of the sizes that wrap to zero in 64 bits are refused before anything is divided by them."""
+    for batch, n in ((1 << 30, 1 << 30), (1 << 18, 1 << 18)):
+        for rc in calls(lib, view(batch=batch, n=n, d=256, rot=0), side(heads=1024)):
+            assert rc == EUNSUPPORTED and "2^44" in T.last_error()

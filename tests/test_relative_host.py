@@ -183,3 +183,17 @@ def test_python_refusals():
         R.relative_bias_backward(torch.zeros(4, 4), b, p, p)
     with pytest.raises(ValueError, match="channels"):
         R.relative_pair_backward(torch.zeros(4, 4), b, p, p)
+
+
+def test_more_values_than_counted_refused(lib):
+    """Products of the sizes that wrap to zero in 64 bits are refused before anything is divided by them."""
+    n = ctypes.c_size_t()
+    for size in (1 << 23, 1 << 13):
+        v = view(batch=size, nq=size, nk=size, heads=1024)
+        far = bias(batch=1 << 30, head=1 << 30, row=1 << 30)
+        assert lib.relative_bias(v, 16, None, far, None) == EUNSUPPORTED and "2^48" in T.last_error()
+        assert lib.relative_bias_backward_workspace_size(v, n) == EUNSUPPORTED and "2^48" in T.last_error()
+        assert lib.relative_bias_backward(v, far, 16, 256, 1 << 30, None) == EUNSUPPORTED and "2^48" in T.last_error()
+    v = view(batch=1, nq=1 << 23, nk=1 << 23, heads=1024)
+    assert lib.relative_pair(v, 16, None, 0, 16, 1 << 33, None) == EUNSUPPORTED and "2^48" in T.last_error()
+    assert lib.relative_pair_backward(v, 16, 1 << 33, 16, 256, 1 << 30, None) == EUNSUPPORTED and "2^48" in T.last_error()
