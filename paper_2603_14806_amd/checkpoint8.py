@@ -79,6 +79,13 @@ class Checkpoint8:
     __slots__ = ("codes", "powers", "group", "dtype")
 
     def __init__(self, codes, powers, group, dtype):
+        if not 8 <= group <= 256 or group % 8 or dtype not in _DTYPES:
+            raise ValueError(f"group must be a multiple of 8 up to 256 and dtype float32 or bfloat16, not {group} and {dtype}")
+        shape = codes.shape[:-1] + (-(-codes.shape[-1] // group),)
+        if codes.dtype != torch.int8 or powers.dtype != torch.uint8 or powers.shape != shape or powers.device != codes.device:
+            raise ValueError(f"codes must be int8 and powers uint8 {list(shape)} on {codes.device}, not {codes.dtype} and {powers.dtype} {list(powers.shape)} on {powers.device}")
+        if not codes.is_contiguous() or not powers.is_contiguous():
+            raise ValueError("codes and powers must be contiguous")
         self.codes, self.powers, self.group, self.dtype = codes, powers, group, dtype
 
     @property

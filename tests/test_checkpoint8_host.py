@@ -93,3 +93,22 @@ def test_python_refusals():
         C.pack(x)
     with pytest.raises(ValueError, match="float32 or bfloat16"):
         C.pack(x.half())
+
+
+def test_codes_that_do_not_fit_refused():
+    """A Checkpoint8 of one's own (read from a file, cut from another): what the kernels assume of it is checked."""
+    def codes(*shape, dtype=torch.int8):
+        return torch.zeros(shape, dtype=dtype)
+
+    def powers(*shape, dtype=torch.uint8):
+        return torch.zeros(shape, dtype=dtype)
+    ok = C.Checkpoint8(codes(3, 5, 40), powers(3, 5, 2), 32, torch.bfloat16)
+    assert ok.shape == (3, 5, 40)
+    C.Checkpoint8(codes(0, 40), powers(0, 2), 32, torch.float32)
+    for c, p, group, dtype in ((codes(3, 40), powers(3, 1), 32, torch.float32), (codes(3, 40), powers(4, 2), 32, torch.float32),
+                               (codes(3, 40, dtype=torch.uint8), powers(3, 2), 32, torch.float32), (codes(3, 40), powers(3, 2, dtype=torch.int8), 32, torch.float32),
+                               (codes(3, 40), powers(3, 2), 32, torch.float16), (codes(3, 40), powers(3, 2), 0, torch.float32), (codes(3, 40), powers(3, 2), 36, torch.float32),
+                               (codes(3, 40), powers(3, 2), 264, torch.float32), (codes(3, 80)[:, ::2], powers(3, 2), 32, torch.float32),
+                               (codes(3, 40), powers(3, 4)[:, :2], 32, torch.float32)):
+        with pytest.raises(ValueError):
+            C.Checkpoint8(c, p, group, dtype)
