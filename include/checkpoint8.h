@@ -13,8 +13,11 @@
  * byte 255, and the whole group reads back as NaN).  The scale is a power of two
  * so that x 2^-k is exact and a code has one value whoever computes it; a value
  * has 7 significant bits, so reading it back as bf16 or fp32 is exact too.  The
- * error is half a step, 2^(k-1) <= amax / 127 (amax / 254 at best; a step at most
- * where k would be 122, so that no finite value reads back as infinity).
+ * error is at most half a step, 2^(k-1), and that at most amax / 127 (amax / 254 at
+ * best) except at the ends of k's range: groups whose amax is below 127 2^-128 are
+ * held at k = -127 and are off by up to 2^-128 (from an amax of 2^-128 down by the
+ * values themselves: all codes are 0), and where k would be 122 the error is a step
+ * at most, so that no finite value reads back as infinity.
  *
  * norm_rotate.h writes this form in its forward pass (a group for each head's
  * row) and reads it in its backward.

@@ -40,6 +40,27 @@ def test_error_and_idempotence():
     assert oracle.checkpoint8(tiny, 8)[1][0, 0] == 0
 
 
+def test_error_at_the_ends_of_the_range():
+    """Where k is held at -127 (amax below 127 2^-128) half a step is 2^-128, which may be more than amax / 127, and from
+    amax = 2^-128 down nothing is left; where it is held at 121, a step."""
+    rng = np.random.default_rng(2)
+    border = 127 * 2.0 ** -128
+    top = np.concatenate([2.0 ** rng.uniform(-149, -118, 400), border * np.array([1 - 2.0 ** -20, 1, 1 + 2.0 ** -20]), 2.0 ** np.arange(-149.0, -120)])
+    x = (top[:, None] * rng.uniform(-1, 1, (len(top), 8)))
+    x[:, 3] = top
+    x = x.astype(np.float32).astype(np.float64)
+    top = np.abs(x).max(-1)
+    codes, powers = oracle.checkpoint8(x, 8)
+    error = np.abs(oracle.checkpoint8_values(codes, powers, 8) - x).max(-1)
+    small = top < border
+    assert (powers[small, 0] == 0).all() and (error[small] <= 2.0 ** -128).all() and (error[~small] <= top[~small] / 127).all()
+    assert (error[small] > top[small] / 127).any() and (codes[top <= 2.0 ** -128] == 0).all()
+    big = float(np.finfo(np.float32).max)
+    x = rng.uniform(0.99, 1, (50, 8)) * big
+    codes, powers = oracle.checkpoint8(x, 8)
+    assert (powers == 248).all() and (np.abs(oracle.checkpoint8_values(codes, powers, 8) - x) <= 2.0 ** 121).all()
+
+
 @pytest.fixture(scope="module")
 def lib():
     if not os.path.exists(T.LIB_PATH):

@@ -79,6 +79,20 @@ def test_extremes():
     assert torch.isnan(b[1, 32:64]).all() and torch.equal(a[0], b[0]) and torch.equal(a[1, 64:], b[1, 64:]) and torch.equal(a[1, :32], b[1, :32])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_smallest_groups(dtype):
+    """Groups whose power is held at 2^-127: codes, powers and values as the oracle's, and errors of at most 2^-128."""
+    g = torch.Generator().manual_seed(8)
+    top = torch.exp2(torch.rand((300, 1), generator=g, dtype=torch.float64) * 29 - 149)         # up to 2^-120
+    x = (top * (2 * torch.rand((300, 40), generator=g, dtype=torch.float64) - 1)).to(TORCH[dtype]).cuda()
+    for group in (8, 32):
+        same(C.pack(x, group), x, group)
+    c = C.pack(x, 8)
+    error = np.abs(host(c.unpack()) - host(x)).reshape(300, 5, 8).max(-1)
+    held = np.abs(host(x)).reshape(300, 5, 8).max(-1) < 127 * 2.0 ** -128
+    assert held.any() and (c.powers.cpu().numpy()[held] == 0).all() and (error[held] <= 2.0 ** -128).all()
+
+
 def test_large_streams_and_graphs():
     x = values((1 << 14, 1030), 5, "bf16").cuda()
     want = C.pack(x)
