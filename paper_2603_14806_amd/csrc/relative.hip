@@ -635,13 +635,15 @@ size_t values_bytes(const RelativeArgs& a) {            // of one head: values_b
 }
 }  // namespace
 
+constexpr int kBaseHeads = 2;      // the most heads at once with a base
+
 int64_t relative_bias_plan(RelativeArgs& a) {
     a.tx = pow2_from(up(a.nk, 8), 16);
     const int rows = 256 / a.tx;
     // Heads at once: without a base eight share an index (1300 x 1300, 16 heads, bf16: 17.9 us; two at once 20.0).  With one,
     // two: each head is two streams, and heads are often as far apart as memory channels repeat (2048 x 3000, 16 heads: 96
     // us; four at once 129, one 96).
-    a.hb = pow2_from(a.heads, a.base.data ? 2 : 8);
+    a.hb = pow2_from(a.heads, a.base.data ? kBaseHeads : 8);
     while (a.hb > 1 && a.hb * values_bytes(a) > 40960) a.hb /= 2;
     a.cblocks = (int)up(a.nk, 8 * a.tx);
     auto groups = [&]() { return a.batch * up(a.heads, a.hb) * a.cblocks * up(a.nq, rows); };
@@ -666,8 +668,9 @@ hipError_t launch_relative_bias(int dtype, RelativeArgs a, hipStream_t s) {
     auto pick = [&](auto zero, auto heads) {
         using T = decltype(zero);
         constexpr int HB = decltype(heads)::value;
-        return seg ? base ? go(k_relative_bias<T, true, true, HB>) : go(k_relative_bias<T, true, false, HB>)
-                   : base ? go(k_relative_bias<T, false, true, HB>) : go(k_relative_bias<T, false, false, HB>);
+        if constexpr (HB <= kBaseHeads)
+            if (base) return seg ? go(k_relative_bias<T, true, true, HB>) : go(k_relative_bias<T, false, true, HB>);
+        return seg ? go(k_relative_bias<T, true, false, HB>) : go(k_relative_bias<T, false, false, HB>);
     };
     auto by_heads = [&](auto zero) {
         switch (a.hb) {
