@@ -21,7 +21,6 @@ struct Place {
 // Lane `lane` of group `slot`; FLAT: all rows are one.
 template <bool FLAT>
 __device__ __forceinline__ Place place(const CheckpointArgs& a, int64_t slot, int lane) {
-    Place p;
     if (slot >= a.slots) return Place{0, 0, 0, 0};
     int64_t row = 0, g = slot;
     if constexpr (!FLAT) {
