@@ -156,3 +156,27 @@ def test_layer_backward_from_a_checkpoint(direction):
             torch.cuda.synchronize()
             assert torch.equal(a[0], b[0]) and all(torch.equal(a[1][n], b[1][n]) for n in b[1])
     layer.close()
+
+
+def test_layer_backward_from_a_checkpoint_of_f32_values():
+    """A z that was fp32 when it was packed: its values are exact in the layer's bf16.  (A layer in fp32 has no backward, from
+    a tensor or from a checkpoint.)"""
+    N = 38
+    z = synth.pair_tensor(N, dtype="f32", seed=5, device="cuda")
+    mask = synth.token_mask(N, 6, device="cuda")
+    held = C.pack(z, 64)
+    stands = held.unpack("bf16")
+    assert held.dtype == torch.float32 and torch.equal(stands.float(), held.unpack())
+    for out_dtype in ("f32", "bf16"):
+        layer, _ = make_layer("bf16", out_dtype, affine=True)
+        dout = torch.randn((N, N, 128), generator=torch.Generator().manual_seed(7)).to(TORCH[out_dtype]).cuda()
+        for call, g, more in ((layer.backward, dout, {}), (layer.residual_backward, dout.to(torch.bfloat16), dict(p=0.25, seed=9, share="columns"))):
+            a, b = call(held, g, mask, "incoming", **more), call(stands, g, mask, "incoming", **more)
+            assert a[0].dtype == torch.bfloat16 and torch.equal(a[0], b[0]) and all(torch.equal(a[1][n], b[1][n]) for n in b[1])
+        layer.close()
+    layer, _ = make_layer("f32")
+    for x in (held, z):
+        with pytest.raises(T.TriMulError) as e:
+            layer.backward(x, torch.zeros_like(z), mask)
+        assert e.value.code == T.TRI_MUL_EUNSUPPORTED
+    layer.close()

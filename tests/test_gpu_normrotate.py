@@ -16,7 +16,7 @@ from oracle import normrotate as O
 from paper_2603_14806_amd import checkpoint8 as C
 from paper_2603_14806_amd import normrotate as N
 from paper_2603_14806_amd import trimul as T
-from tests.gpu_util import host, needs_gpu
+from tests.gpu_util import host, needs_gpu, say
 
 pytestmark = [pytest.mark.gpu, needs_gpu]
 
@@ -149,6 +149,41 @@ def test_many_rows_and_the_same_bits():
         check_backward(got[1], got[2]["gain_k"], None, k, dyk, phase, d, gain, "layer", "halves", "bf16", "k")
         again = N.norm_rotate_backward(q, k, dyq, dyk, pos, freqs, **how)
         assert torch.equal(got[0], again[0]) and torch.equal(got[2]["gain_q"], again[2]["gain_q"]) and torch.equal(got[2]["gain_k"], again[2]["gain_k"])
+
+
+# batch, n, heads of q and of k, d, rot: enough rows to fill the card's waves, positions of each entry's own, so that a wave takes
+# a few heads of several tokens in several steps, the last of them (9, 3, 20, 10 heads) and the last tokens only in part
+MANY = [(2, 423, 16, 4, 128, 64), (3, 459, 9, 3, 128, 128), (5, 443, 20, 10, 24, 16), (3, 191, 20, 10, 80, 48), (2, 347, 9, 3, 200, 200),
+        (7, 331, 20, 10, 32, 32), (2, 843, 16, 4, 64, 8)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("i", range(len(MANY)))
+def test_many_rows_with_positions_of_their_own(i, dtype):
+    """Values, codes and gradients against the oracle, and from the codes as from the values they stand for.  A lane adds at
+    most 16 rows: eight steps an item, two items a wave."""
+    case = MANY[i]
+    b, n, h, hk, d, rot = case
+    lanes = max(4, 1 << (d // 8 - 1).bit_length())
+    assert b * n * (h + hk) >= 4096 * (64 // lanes)
+    for j, (norm, pairs) in enumerate((("rms", "adjacent"), ("layer", "halves")) if i % 2 else (("layer", "adjacent"), ("rms", "halves"))):
+        q, k, pos, freqs, phase, w = setup(case, i, dtype, "f32" if (i + j) % 2 else dtype, "any")
+        how = dict(norm=norm, pairs=pairs, eps=EPS, **w)
+        yq, yk, cq, ck = N.norm_rotate(q, k, pos, freqs, checkpoint=True, **how)
+        plain = N.norm_rotate(q, k, pos, freqs, **how)
+        assert torch.equal(plain[0], yq) and torch.equal(plain[1], yk)
+        dyq, dyk = normal(q.shape, 100 + i, dtype), normal(k.shape, 200 + i, dtype)
+        dq, dk, grads = N.norm_rotate_backward(q, k, dyq, dyk, pos, freqs, **how)
+        for x, y, c, dy, dx, name in ((q, yq, cq, dyq, dq, "q"), (k, yk, ck, dyk, dk, "k")):
+            what = f"{case} {norm} {pairs} {name}"
+            check_forward(y, x, phase, rot, w["gain_" + name], w["shift_" + name], norm, pairs, dtype, what)
+            check_backward(dx, grads["gain_" + name], grads["shift_" + name], x, dy, phase, rot, w["gain_" + name], norm, pairs, dtype, what, 16)
+            codes, powers = oracle.checkpoint8(host(x), d)
+            assert np.array_equal(c.codes.cpu().numpy(), codes) and np.array_equal(c.powers.cpu().numpy(), powers), what
+        a = N.norm_rotate_backward(cq, ck, dyq, dyk, pos, freqs, **how)
+        e = N.norm_rotate_backward(cq.unpack(), ck.unpack(), dyq, dyk, pos, freqs, **how)
+        assert torch.equal(a[0], e[0]) and torch.equal(a[1], e[1]) and all((a[2][m] is None and e[2][m] is None) or torch.equal(a[2][m], e[2][m]) for m in e[2])
+        say(f"  {case} {norm} {pairs}")
 
 
 def test_far_positions_keep_their_angle():
