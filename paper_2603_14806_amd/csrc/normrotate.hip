@@ -10,7 +10,10 @@
 // TB/s; a 1 GiB copy reaches 5.1).  384 x 384 tokens, 4 + 4 heads of 32, layer: 36.5 us (0.15 GB, 4.1 TB/s; neighbouring
 // pairs 34.4: half rows of 32 bytes are two accesses to each line) and backward 52 (0.23 GB, 4.3 TB/s).  4 x 2048 tokens with positions of
 // their own, 16 + 4 heads of 128, to and from 8 bits: 28 and 33 us (0.11 GB each, 3.8 and 3.2 TB/s: an item has the rows of a
-// token alone, and waits for its position and its rows once each).  4 single tokens: 4.2 us, a chain of two loads.
+// token alone, and waits for its position and its rows once each).  4 single tokens: 4.2 us, a chain of two loads; 8192 with
+// positions of their own 33 us (42 MB), since token slots of a wave are of one entry and stay empty (15 with one position for all).
+// fp32: 2 x 6000 tokens 81 and 121 us (0.39 and 0.59 GB, 4.9 TB/s), 384 x 384 tokens 64 and 111 us (4.7 and 4.1 TB/s), 4 x 2048
+// to and from 8 bits 46 and 48 us (0.19 GB, 4.1 and 3.9 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -538,9 +541,11 @@ int64_t plan(NormArgs& a, int dtype, bool backward) {
         work[i] = a.batch * q.tiles * q.steps;
         total += work[i];
     }
-    // Waves that go round: 16 for each compute unit, 12 in the backward (what registers allow).  A forward whose entries have
-    // their own positions has short items, and a wave for each.
-    const int64_t waves = backward ? 3072 : 4096;
+    // Waves that go round: 16 for each compute unit, 12 in the backward, as many as its registers let be there at once.  (The
+    // forward in fp32 or with codes has 12 there at once too, and takes its last quarter in a second round: 2 x 6000 tokens,
+    // 16 + 16 heads of 128, fp32 81 us where 12 take 72, bf16 to 8 bits 70 and 58.5.)  A forward whose entries have their own
+    // positions has short items, and a wave for each.
+    const int64_t waves = 256 * (backward ? 12 : 16);
     for (int i = 0; i < 2; ++i) {
         NormSide& q = a.side[i];
         q.chunk = shared && q.heads ? std::min(a.batch, up(std::max<int64_t>(4, total / (8 * waves)), q.steps)) : 1;

@@ -132,8 +132,10 @@ template <bool SEG> struct Keys {
 
 // A work-group: HB heads, a.tx threads along the keys (eight each), 256 / a.tx rows at a time, a.loop times.  Where all
 // lanes of a wave have keys of one distance index each, as away from the diagonal, a head is one look-up.
-// Bound by memory, and by each work-group's start (table and positions into LDS, about 5 us): bf16, 16 heads, 1300 x 1300 18.5 us
-// (54 MB written, 2.9 TB/s), 2048 x 3000 46 us (0.20 GB, 4.3 TB/s), the same with a base 96 us (0.39 GB, 4.1 TB/s).
+// Bound by memory, and by each work-group's start (table and positions into LDS: about 5 us at a reach of 32, and with the reach
+// more of it: 8 x 1786 x 523, 3 heads, bf16, 19 us at 128 and 27 at 1000, 45 MB).  16 heads, bf16: 1300 x 1300 18 us (54 MB
+// written, 3.0 TB/s), 2048 x 3000 46 us (0.20 GB, 4.3 TB/s), the same with a base 101 us (0.39 GB, 3.9 TB/s); fp32: 36 us (3.0 TB/s),
+// 122 us (0.39 GB, 3.2 TB/s) and 224 us (0.79 GB, 3.5 TB/s).
 template <typename T, bool SEG, bool BASE, int HB>
 __global__ __launch_bounds__(256) void k_relative_bias(const RelativeArgs a) {
     extern __shared__ float val[];
@@ -421,7 +423,7 @@ __global__ __launch_bounds__(256) void k_relative_pair(const RelativeArgs a) {
 // when it does.  32 pairs are on their way while 32 are added; where their buckets rise or fall, as near the diagonal,
 // equal neighbours are added up and the places, all different then, are read, added to and written together.
 // Bound by waiting and issue: 66 buckets of 128 channels leave LDS for four waves a compute unit, one a SIMD.  1000 x 1000 bf16
-// 91 us (0.26 GB, 2.8 TB/s; 9 buckets, 16 waves, 54), 500 x 700 fp32 63 us (0.18 GB, 2.8 TB/s).
+// 90 us in five chains, 93 in one (0.26 GB, 2.8 TB/s; 9 buckets, 16 waves, 83), 500 x 700 fp32 63 us (0.18 GB, 2.8 TB/s).
 template <typename T, int V, bool SEG>
 __global__ __launch_bounds__(256) void k_relative_pair_backward(const RelativeArgs a) {
     extern __shared__ float val[];
@@ -640,9 +642,10 @@ constexpr int kBaseHeads = 2;      // the most heads at once with a base
 int64_t relative_bias_plan(RelativeArgs& a) {
     a.tx = pow2_from(up(a.nk, 8), 16);
     const int rows = 256 / a.tx;
-    // Heads at once: without a base eight share an index (1300 x 1300, 16 heads, bf16: 17.9 us; two at once 20.0).  With one,
-    // two: each head is two streams, and heads are often as far apart as memory channels repeat (2048 x 3000, 16 heads: 96
-    // us; four at once 129, one 96).
+    // Heads at once: without a base eight share an index, with one, two: each head is two streams, and heads are often as far
+    // apart as memory channels repeat.  Measured with 16 heads, without a base by two, four and eight at once: bf16, 1300 x
+    // 1300 18.6, 17.7 and 17.7 us, 2048 x 3000 51, 44 and 46; fp32 36.3, 36.9 and 36.3, and 111, 126 and 122, where the
+    // streams meet as with a base.  With one by one, two and four, 2048 x 3000: bf16 110, 101 and 114 us, fp32 245, 224 and 225.
     a.hb = pow2_from(a.heads, a.base.data ? kBaseHeads : 8);
     while (a.hb > 1 && a.hb * values_bytes(a) > 40960) a.hb /= 2;
     a.cblocks = (int)up(a.nk, 8 * a.tx);
@@ -787,7 +790,8 @@ size_t pair_backward_lds(const RelativeArgs& a, int vector) { return (size_t)a.w
 
 // Tiles, as many as LDS lets the compute units have at once (one each for 66 buckets; one more than fit would take a
 // second round): whole rows, so that each has its share of the diagonal and reads long pieces (1000 x 1000 x 128 bf16:
-// 71 us; tiles of 64 columns, with fewer sums to join, 94), and parts of a row where there are fewer rows than tiles.
+// 90 us in five chains, 93 in one; tiles of 64 columns 138 and 112; 500 x 700 x 128 fp32 63 and 78), and parts of a row where
+// there are fewer rows than tiles.
 int64_t relative_pair_backward_plan(RelativeArgs& a, int vector) {
     a.hblocks = (int)up(a.heads, 64 * vector);
     a.waves = std::min(4, std::max(1, 143360 / ((a.buckets + 1) * 256 * vector)));
