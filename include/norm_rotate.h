@@ -30,7 +30,8 @@
  * independent: NaN or infinities show in their own row (and in dgain and dshift, which
  * sum over all rows: the dy of padding has to be 0 and its x finite).  Squares, sums and
  * weights' gradients in fp32 and wider, in a fixed order; angles in 64 bits; one
- * rounding of y and dx.
+ * rounding of y and dx.  A row whose squares pass fp32's range (values from about
+ * 10^18 on) has u and r of 0, or NaN where its sum passes it too.
  */
 #ifndef NORM_ROTATE_H
 #define NORM_ROTATE_H

@@ -221,6 +221,30 @@ def test_rows_are_independent():
             assert torch.equal(dx[keep], dx2[keep])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_squares_past_the_range(dtype):
+    """Rows whose squares float32 does not hold: u and r are 0, so y is the turned shift, dx 0, and nothing of them is in dgain; the
+    others keep their bits."""
+    x, dy = normal((2, 5, 3, 40), 1, dtype), normal((2, 5, 3, 40), 2, dtype)
+    pos, freqs, gain, shift = torch.arange(5, dtype=torch.int32).cuda(), N.frequencies(40), normal((40,), 3, mean=1.0), normal((40,), 4)
+    how = dict(gain_q=gain, shift_q=shift)
+    y, _ = N.norm_rotate(x, None, pos, freqs, **how)
+    dx, _, _ = N.norm_rotate_backward(x, None, dy, None, pos, freqs, **how)
+    z = x.clone()
+    z[0, 3, 1] *= 2.0 ** 100
+    y2, _, c, _ = N.norm_rotate(z, None, pos, freqs, checkpoint=True, **how)
+    dx2, _, grads = N.norm_rotate_backward(z, None, dy, None, pos, freqs, **how)
+    keep = torch.ones((2, 5, 3), dtype=torch.bool, device="cuda")
+    keep[0, 3, 1] = False
+    assert torch.equal(y[keep], y2[keep]) and torch.equal(dx[keep], dx2[keep]) and (dx2[0, 3, 1] == 0).all()
+    x[0, 3, 1] = 0
+    zero, _ = N.norm_rotate(x, None, pos, freqs, **how)
+    assert torch.equal(y2[0, 3, 1], zero[0, 3, 1])
+    assert torch.equal(grads["gain_q"], N.norm_rotate_backward(x, None, dy, None, pos, freqs, **how)[2]["gain_q"])
+    codes, powers = oracle.checkpoint8(host(z), 40)
+    assert np.array_equal(c.codes.cpu().numpy(), codes) and np.array_equal(c.powers.cpu().numpy(), powers)
+
+
 def test_in_place_strides_and_repeated_inputs():
     pos, freqs = torch.arange(6, dtype=torch.int32).cuda(), N.frequencies(32)
     wide = normal((3, 6, 2, 4, 64), 1, "bf16")
